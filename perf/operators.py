@@ -16,7 +16,7 @@ groups of 32 dimensions per row:
     scales of V  [16 row pairs][J][2] bf16
 
 A nibble n of a group with scale s stands for s * (n - 8); s = e / -8 with e the group's element of largest magnitude
-(the positive one of two alike).
+(the positive one of two alike), and 0 where |e| is under 2^-123.
 """
 import math
 import random
@@ -179,7 +179,8 @@ def _quantise(x):
     g = x.float().unflatten(-1, (-1, 32))
     hi, lo = g.amax(-1, keepdim=True), g.amin(-1, keepdim=True)
     e = torch.where(hi >= -lo, hi, lo)
-    s = torch.where(torch.isfinite(e), e / -8, torch.full_like(e, math.nan)).to(BF16)
+    s = torch.where(torch.isfinite(e), e / -8, torch.full_like(e, math.nan))
+    s = torch.where(s.abs() < 2.0 ** -126, torch.zeros_like(s), s).to(BF16)
     f = s.float()
     n = torch.round(g / torch.where(f == 0, torch.ones_like(f), f)).clamp(-8, 7) + 8
     n = torch.where(torch.isfinite(f) & (f != 0), n, torch.full_like(n, 8.0))
@@ -485,7 +486,7 @@ def _exact_quantised(x):
     at = g.abs().argmax(-1, keepdim=True)
     e = g.gather(-1, at).abs()
     e = torch.where((g == e).any(-1, keepdim=True), e, -e)
-    s = (e / -8).to(BF16).double()
+    s = torch.where(e.abs() < 2.0 ** -123, torch.zeros_like(e), (e / -8).to(BF16).double())
     n = torch.clamp(torch.round(g / torch.where(s == 0, torch.ones_like(s), s)), -8, 7)
     return (s * n).view(x.shape)
 
