@@ -345,6 +345,117 @@ svl_status svl_decode_step(svl_model* model, int32_t B, const int32_t* tokens, v
                            int32_t* cache_len, const uint8_t* layer_gate, const uint8_t* group_gate, float* logits,
                            int32_t* next_token, void* workspace, size_t workspace_bytes, void* stream);
 
+/* ------------------------------------------------------------------------
+ * A KV cache in 4 bits, attention over it, and beam search (the paper leaves
+ * decode open, Sec. 5, and calls quantisation orthogonal to its method). These
+ * calls need no model.
+ *
+ * One layer's cache is caller-owned device memory of svl_kv4_cache_size()
+ * bytes, 16-byte aligned, with n_slots sequences of up to max_len positions:
+ * 4.5 bits per value. Every 32 consecutive dimensions of a row of K or V form
+ * a group: with e its value of largest magnitude (of +a and -a: +a), the bf16
+ * scale is s = e / -8 and a value x is held as the code
+ * n = clamp(rint(x / s) + 8, 0, 15) (rint: half to even), which stands for
+ * s * (n - 8). A group with |e| < 2^-123 is held as zeros, one with a value
+ * that is not finite as NaNs. The bytes are [n_slots][n_kv_heads] tiles of 32
+ * positions (36 * d_head bytes each; csrc/kv4.cuh has their order), so that
+ * several layers' caches one after the other are one cache of
+ * n_layers * n_slots slots. What a position holds before it is written, and
+ * what lies past the positions a call names, is never used.
+ * d_head is 64 or 128 (else SVL_ERR_UNSUPPORTED), n_slots at most 65,535. */
+typedef struct svl_kv4_desc {
+  int32_t n_slots;
+  int32_t n_kv_heads;
+  int32_t d_head;
+  int32_t max_len;
+} svl_kv4_desc;
+
+/* Bytes of one layer's cache (0 on bad arguments). */
+size_t svl_kv4_cache_size(const svl_kv4_desc* desc);
+
+/* Quantises rows of K and V into the cache. k, v: `rows` rows of
+ * n_kv_heads * d_head bf16 values, ld_k and ld_v elements apart. Slot b takes
+ * rows row_off[b] .. row_off[b+1] - 1 (row_off [n_slots + 1] int32, device; NULL:
+ * one row per slot, rows == n_slots) at positions start[b], start[b] + 1, ...
+ * (start [n_slots] int32, device; NULL: 0). A row at a negative position (an
+ * idle slot) is not stored; neither is one at max_len or above, which also
+ * sets SVL_DEV_BAD_INDEX in *status (uint32, device, or NULL). Rows outside
+ * row_off are not read. Positions keep what they held unless they are written.
+ * Requires 16-byte aligned k, v and cache, ld_k and ld_v multiples of 8 and at
+ * least n_kv_heads * d_head (else SVL_ERR_INVALID_ARG). Asynchronous on
+ * `stream`, as all calls here. */
+svl_status svl_kv4_write(const svl_kv4_desc* desc, void* cache, const void* k, int64_t ld_k, const void* v,
+                         int64_t ld_v, int64_t rows, const int32_t* row_off, const int32_t* start,
+                         uint32_t* status, void* stream);
+
+/* Reads the same rows back as bf16 (s * (n - 8), rounded to nearest even); a
+ * row whose position is outside [0, max_len) reads as zeros. Arguments as for
+ * svl_kv4_write. */
+svl_status svl_kv4_read(const svl_kv4_desc* desc, const void* cache, int64_t rows, const int32_t* row_off,
+                        const int32_t* start, void* k, int64_t ld_k, void* v, int64_t ld_v, void* stream);
+
+/* Attention of the newest rows of every slot over its cache. `rows` query rows
+ * per slot (1 to 16; one when decoding, more for drafted tokens): row r of
+ * slot b is row b * rows + r of q (n_heads * d_head bf16 values, ld_q elements
+ * apart) and sits at position start[b] + r, whose K and V the cache already
+ * holds (svl_kv4_write with the same start). Query head h reads KV head
+ * h / (n_heads / n_kv_heads). The row at position p sees position j if j <= p
+ * and, with window > 0, j > p - window or j < sinks: the last `window`
+ * positions and the first `sinks`. softmax(scale * q . k) in float32, out
+ * [n_slots * rows] rows of n_heads * d_head bf16, ld_out elements apart. A row at a
+ * negative position sees nothing and a row at max_len or above has no place
+ * in the cache: both give zeros.
+ * Requires 16-byte aligned q, out and cache, ld_q and ld_out multiples of 8 and
+ * at least n_heads * d_head, n_heads a multiple of n_kv_heads, window and sinks
+ * not negative (else SVL_ERR_INVALID_ARG). Workspace:
+ * svl_kv4_attention_workspace_size() bytes, 256-byte aligned. */
+size_t svl_kv4_attention_workspace_size(const svl_kv4_desc* desc, int32_t n_heads, int32_t rows);
+svl_status svl_kv4_attention(const svl_kv4_desc* desc, const void* cache, int32_t n_heads, int32_t rows,
+                             const void* q, int64_t ld_q, const int32_t* start, int32_t window, int32_t sinks,
+                             float scale, void* out, int64_t ld_out, void* workspace, size_t workspace_bytes,
+                             void* stream);
+
+/* Beam search's selection for n_samples samples of `beams` beams (1 to 16)
+ * over a vocabulary: the `take` best continuations (1 to 32, at most vocab) of
+ * each sample. logits [n_samples * beams] rows of vocab float32, ld elements
+ * apart; beam_scores [n_samples, beams] float32: the beams' log-probabilities so
+ * far (-inf: a beam that offers nothing, as all but the first before the
+ * first step). Beam w offers for every id v the score
+ *   logit[w, v] + (beam_scores[w] - lse_w),  lse_w = log sum_v exp logit[w, v]
+ * (float32, each operation rounded). A finished beam (finished [n_samples,
+ * beams] uint8, or NULL: none) offers itself alone: its score, unchanged, and
+ * the id eos. Scores order the continuations, the larger first; equal scores:
+ * the lower beam first; within a beam: the larger logit, then the lower id.
+ * Logits may be -inf (an id that is not allowed). A beam with a NaN or +inf
+ * logit, or with no logit above -inf, offers scores of -inf (ids 0, 1, ...),
+ * and a score that comes out as NaN counts as -inf: entries with the score
+ * -inf are no continuations.
+ * Outputs [n_samples, take]: scores_out float32, parent int32 (the beam within
+ * its sample), token int32, finished_out uint8 or NULL: 1 where the parent
+ * was finished or the token is eos (eos < 0: no id is). With take == beams
+ * they are the next step's beam_scores, svl_kv4_reorder's parent, the ids to
+ * feed and the next `finished`. No output may overlap an input. Workspace:
+ * svl_beam_select_workspace_size() bytes, 256-byte aligned. */
+size_t svl_beam_select_workspace_size(int32_t n_samples, int32_t beams, int32_t vocab, int32_t take);
+svl_status svl_beam_select(int32_t n_samples, int32_t beams, int32_t vocab, int32_t take, const float* logits,
+                           int64_t ld, const float* beam_scores, const uint8_t* finished, int32_t eos,
+                           float* scores_out, int32_t* parent, int32_t* token, uint8_t* finished_out,
+                           void* workspace, size_t workspace_bytes, void* stream);
+
+/* Reorders the slots after a selection, in place, in the caches of n_layers
+ * layers that lie one after the other. Slots belong to samples of `beams` (1 to
+ * 16) each: slot b * beams + w takes over what slot b * beams + parent[b * beams +
+ * w] held (parent [n_slots] int32, device; any map, permutations and repeated
+ * parents alike) at positions from[b] and above, up to the parent's len
+ * (len [n_slots] int32, device: positions per slot before the call; from
+ * [n_slots / beams] int32, device: positions below it are the same in all
+ * beams, as a shared prompt's are, and stay; NULL: 0). Both ends widen to
+ * whole tiles of 32 positions: from[b] rounds down. A slot whose parent is out
+ * of range keeps its rows and sets SVL_DEV_BAD_INDEX in *status (or NULL). */
+svl_status svl_kv4_reorder(const svl_kv4_desc* desc, void* cache, int32_t n_layers, int32_t beams,
+                           const int32_t* parent, const int32_t* from, const int32_t* len, uint32_t* status,
+                           void* stream);
+
 /* svl_score_select without a workspace argument. The paper has no
  *  counterpart: this exists for callers that cannot allocate device memory
  *  for a workspace -- code running during CUDA stream capture (where

@@ -11,6 +11,7 @@
 
 #include "gemm.cuh"
 #include "kernels.cuh"
+#include "kv4.cuh"
 
 using namespace svl;
 
@@ -1513,6 +1514,186 @@ svl_status svl_decode_step(svl_model* m, int32_t B, const int32_t* tokens, void*
   StepCtx kx{static_cast<__nv_bfloat16*>(kv_cache), max_len, 1, cache_len, tokens, next_token};
   return prefill_impl(m, B, B, X, cu, pos, layer_gate, group_gate, SVL_LOGITS_LAST, logits, base + xb + cb + pb,
                       ws_bytes - (xb + cb + pb), stream, nullptr, &kx);
+}
+
+namespace {
+constexpr int kKv4MaxSlots = 65535;
+
+// Checks a cache's description; SVL_OK also fills `c` (cache == nullptr: sizes only).
+svl_status kv4_cache(const svl_kv4_desc* d, const void* cache, bool sizes_only, Kv4Cache* c) {
+  if (!d || d->n_slots <= 0 || d->n_kv_heads <= 0 || d->max_len <= 0 || d->d_head <= 0) return SVL_ERR_INVALID_ARG;
+  if ((d->d_head != 64 && d->d_head != 128) || d->n_slots > kKv4MaxSlots || d->n_kv_heads > kKv4MaxSlots)
+    return SVL_ERR_UNSUPPORTED;
+  if (!sizes_only && (!cache || !aligned16(cache))) return SVL_ERR_INVALID_ARG;
+  c->data = static_cast<uint8_t*>(const_cast<void*>(cache));
+  c->n_slots = d->n_slots;
+  c->kv = d->n_kv_heads;
+  c->dh = d->d_head;
+  c->max_len = d->max_len;
+  c->tiles = (d->max_len - 1) / kKv4Tile + 1;
+  return SVL_OK;
+}
+
+svl_status kv4_rows(const svl_kv4_desc* d, const void* cache, const void* k, int64_t ld_k, const void* v, int64_t ld_v,
+                    int64_t rows, const int32_t* row_off, const int32_t* start, Kv4Rows* a) {
+  std::memset(a, 0, sizeof(*a));
+  const svl_status st = kv4_cache(d, cache, false, &a->c);
+  if (st != SVL_OK) return st;
+  const int64_t cols = static_cast<int64_t>(d->n_kv_heads) * d->d_head;
+  if (!k || !v || !aligned16(k) || !aligned16(v) || ld_k < cols || ld_v < cols || (ld_k & 7) || (ld_v & 7) || rows < 0 ||
+      rows > INT32_MAX)
+    return SVL_ERR_INVALID_ARG;
+  if (!row_off && rows != d->n_slots) return SVL_ERR_SHAPE;
+  a->rows = rows;
+  a->n = d->n_slots;
+  a->slot_step = 1;
+  a->row_off = row_off;
+  a->start = start;
+  a->k_row = ld_k;
+  a->v_row = ld_v;
+  a->v_col = 1;
+  return SVL_OK;
+}
+
+int device_sms() {
+  int dev = 0, sms = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess ||
+      cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess)
+    return 0;
+  return sms;
+}
+}  // namespace
+
+size_t svl_kv4_cache_size(const svl_kv4_desc* desc) {
+  Kv4Cache c;
+  if (kv4_cache(desc, nullptr, true, &c) != SVL_OK) return 0;
+  return static_cast<size_t>(c.n_slots) * c.kv * c.tiles * kv4_tile_bytes(c.dh);
+}
+
+svl_status svl_kv4_write(const svl_kv4_desc* desc, void* cache, const void* k, int64_t ld_k, const void* v,
+                         int64_t ld_v, int64_t rows, const int32_t* row_off, const int32_t* start, uint32_t* status,
+                         void* stream) {
+  Kv4Rows a;
+  const svl_status st = kv4_rows(desc, cache, k, ld_k, v, ld_v, rows, row_off, start, &a);
+  if (st != SVL_OK || rows == 0) return st;
+  a.k = static_cast<const __nv_bfloat16*>(k);
+  a.v = static_cast<const __nv_bfloat16*>(v);
+  a.status = status;
+  g_launches++;
+  if (launch_kv4_write(a, static_cast<cudaStream_t>(stream)) != cudaSuccess) return SVL_ERR_CUDA;
+  return last_error();
+}
+
+svl_status svl_kv4_read(const svl_kv4_desc* desc, const void* cache, int64_t rows, const int32_t* row_off,
+                        const int32_t* start, void* k, int64_t ld_k, void* v, int64_t ld_v, void* stream) {
+  Kv4Rows a;
+  const svl_status st = kv4_rows(desc, cache, k, ld_k, v, ld_v, rows, row_off, start, &a);
+  if (st != SVL_OK || rows == 0) return st;
+  a.k_out = static_cast<__nv_bfloat16*>(k);
+  a.v_out = static_cast<__nv_bfloat16*>(v);
+  g_launches++;
+  if (launch_kv4_read(a, static_cast<cudaStream_t>(stream)) != cudaSuccess) return SVL_ERR_CUDA;
+  return last_error();
+}
+
+size_t svl_kv4_attention_workspace_size(const svl_kv4_desc* desc, int32_t n_heads, int32_t rows) {
+  Kv4Cache c;
+  if (kv4_cache(desc, nullptr, true, &c) != SVL_OK || n_heads <= 0 || n_heads % c.kv || rows <= 0 ||
+      rows > kKv4MaxRows)
+    return 0;
+  return std::max<size_t>(kv4_attn_workspace(c, n_heads, rows), 256);
+}
+
+svl_status svl_kv4_attention(const svl_kv4_desc* desc, const void* cache, int32_t n_heads, int32_t rows, const void* q,
+                             int64_t ld_q, const int32_t* start, int32_t window, int32_t sinks, float scale, void* out,
+                             int64_t ld_out, void* ws, size_t ws_bytes, void* stream) {
+  Kv4Attn a;
+  std::memset(&a, 0, sizeof(a));
+  svl_status st = kv4_cache(desc, cache, false, &a.c);
+  if (st != SVL_OK) return st;
+  const int64_t cols = static_cast<int64_t>(n_heads) * a.c.dh;
+  if (n_heads <= 0 || n_heads % a.c.kv || rows <= 0 || !q || !out || !start || !aligned16(q) || !aligned16(out) ||
+      ld_q < cols || ld_out < cols || (ld_q & 7) || (ld_out & 7) || window < 0 || sinks < 0)
+    return SVL_ERR_INVALID_ARG;
+  if (rows > kKv4MaxRows) return SVL_ERR_UNSUPPORTED;
+  if ((st = check_ws(ws, ws_bytes, kv4_attn_workspace(a.c, n_heads, rows))) != SVL_OK) return st;
+  a.A = n_heads;
+  a.rows = rows;
+  a.q = static_cast<const __nv_bfloat16*>(q);
+  a.ldq = ld_q;
+  a.out = static_cast<__nv_bfloat16*>(out);
+  a.ldo = ld_out;
+  a.start = start;
+  a.window = window;
+  a.sinks = sinks;
+  a.scale = scale;
+  a.ws = ws;
+  if ((a.num_sms = device_sms()) <= 0) return SVL_ERR_CUDA;
+  g_launches++;
+  if (launch_kv4_attention(a, static_cast<cudaStream_t>(stream)) != cudaSuccess) return SVL_ERR_CUDA;
+  return last_error();
+}
+
+size_t svl_beam_select_workspace_size(int32_t n_samples, int32_t beams, int32_t vocab, int32_t take) {
+  if (n_samples <= 0 || beams <= 0 || beams > kKv4MaxBeams || vocab <= 0 || take <= 0 || take > kBeamMaxTake ||
+      take > vocab)
+    return 0;
+  return beam_workspace(n_samples, beams, vocab, take);
+}
+
+svl_status svl_beam_select(int32_t n_samples, int32_t beams, int32_t vocab, int32_t take, const float* logits,
+                           int64_t ld, const float* beam_scores, const uint8_t* finished, int32_t eos,
+                           float* scores_out, int32_t* parent, int32_t* token, uint8_t* finished_out, void* ws,
+                           size_t ws_bytes, void* stream) {
+  if (n_samples <= 0 || beams <= 0 || vocab <= 0 || take <= 0 || !logits || ld < vocab || !beam_scores || !scores_out ||
+      !parent || !token || eos >= vocab)
+    return SVL_ERR_INVALID_ARG;
+  if (take > vocab) return SVL_ERR_SHAPE;
+  if (beams > kKv4MaxBeams || take > kBeamMaxTake || static_cast<int64_t>(n_samples) * beams > INT32_MAX / 64)
+    return SVL_ERR_UNSUPPORTED;
+  const svl_status st = check_ws(ws, ws_bytes, beam_workspace(n_samples, beams, vocab, take));
+  if (st != SVL_OK) return st;
+  BeamArgs a;
+  std::memset(&a, 0, sizeof(a));
+  a.S = n_samples;
+  a.W = beams;
+  a.V = vocab;
+  a.K = take;
+  a.logits = logits;
+  a.ld = ld;
+  a.scores = beam_scores;
+  a.finished = finished;
+  a.eos = eos;
+  a.scores_out = scores_out;
+  a.parent = parent;
+  a.token = token;
+  a.finished_out = finished_out;
+  a.ws = ws;
+  g_launches += 2;
+  if (launch_beam_select(a, static_cast<cudaStream_t>(stream)) != cudaSuccess) return SVL_ERR_CUDA;
+  return last_error();
+}
+
+svl_status svl_kv4_reorder(const svl_kv4_desc* desc, void* cache, int32_t n_layers, int32_t beams,
+                           const int32_t* parent, const int32_t* from, const int32_t* len, uint32_t* status,
+                           void* stream) {
+  Kv4Reorder a;
+  std::memset(&a, 0, sizeof(a));
+  const svl_status st = kv4_cache(desc, cache, false, &a.c);
+  if (st != SVL_OK) return st;
+  if (n_layers <= 0 || beams <= 0 || !parent || !len) return SVL_ERR_INVALID_ARG;
+  if (a.c.n_slots % beams) return SVL_ERR_SHAPE;
+  if (beams > kKv4MaxBeams || static_cast<int64_t>(n_layers) * (a.c.n_slots / beams) > kKv4MaxSlots)
+    return SVL_ERR_UNSUPPORTED;
+  a.layers = n_layers;
+  a.W = beams;
+  a.parent = parent;
+  a.from = from;
+  a.len = len;
+  a.status = status;
+  g_launches++;
+  if (launch_kv4_reorder(a, static_cast<cudaStream_t>(stream)) != cudaSuccess) return SVL_ERR_CUDA;
+  return last_error();
 }
 
 svl_status svl_quantize_rows_e4m3(const void* src, const void* gain, int64_t rows, int32_t cols, int64_t ld_src,

@@ -32,7 +32,9 @@ SYMBOLS = ["svl_model_create", "svl_model_destroy", "svl_workspace_size", "svl_s
            "svl_tag_name", "svl_score_select_noalloc", "svl_profile_launches", "svl_selftest_wait_timeout",
            "svl_workspace_size_for", "svl_score_select_paper", "svl_pack_controlled", "svl_controlled_prefill",
            "svl_kv_cache_size", "svl_gated_prefill_kv", "svl_decode_workspace_size", "svl_decode_step",
-           "svl_quantize_rows_e4m3", "svl_gemm_e4m3", "svl_layer_stage", "svl_ksplit_plan"]
+           "svl_quantize_rows_e4m3", "svl_gemm_e4m3", "svl_layer_stage", "svl_ksplit_plan", "svl_kv4_cache_size",
+           "svl_kv4_write", "svl_kv4_read", "svl_kv4_attention_workspace_size", "svl_kv4_attention",
+           "svl_beam_select_workspace_size", "svl_beam_select", "svl_kv4_reorder"]
 
 TAGS = ["budget_embed", "score", "select", "pack", "projector", "schedule", "rmsnorm", "qkv_gemm", "attention",
         "o_gemm", "gateup_gemm", "down_gemm", "lm_head", "host_copy", "quant"]
@@ -60,6 +62,11 @@ class Weights(ctypes.Structure):
                 ("lm_head", ctypes.c_void_p), ("layers", ctypes.POINTER(LayerWeights)),
                 ("llm_bud_w1", ctypes.c_void_p), ("llm_bud_w2", ctypes.c_void_p), ("kap_w1", ctypes.c_void_p),
                 ("kap_w2", ctypes.c_void_p), ("gate_w", ctypes.c_void_p), ("gate_c", ctypes.c_void_p)]
+
+
+class Kv4Desc(ctypes.Structure):
+    """A layer's 4-bit KV cache: slots, KV heads, head width (64 or 128), positions per slot."""
+    _fields_ = [(n, ctypes.c_int32) for n in ("n_slots", "n_kv_heads", "d_head", "max_len")]
 
 
 def lib():
@@ -132,6 +139,23 @@ def lib():
         L.svl_layer_stage.restype = ctypes.c_int
         L.svl_ksplit_plan.argtypes = [i32] * 5
         L.svl_ksplit_plan.restype = i32
+        desc = ctypes.POINTER(Kv4Desc)
+        L.svl_kv4_cache_size.argtypes = [desc]
+        L.svl_kv4_cache_size.restype = sz
+        L.svl_kv4_write.argtypes = [desc, vp, vp, i64, vp, i64, i64, vp, vp, vp, vp]
+        L.svl_kv4_write.restype = ctypes.c_int
+        L.svl_kv4_read.argtypes = [desc, vp, i64, vp, vp, vp, i64, vp, i64, vp]
+        L.svl_kv4_read.restype = ctypes.c_int
+        L.svl_kv4_attention_workspace_size.argtypes = [desc, i32, i32]
+        L.svl_kv4_attention_workspace_size.restype = sz
+        L.svl_kv4_attention.argtypes = [desc, vp, i32, i32, vp, i64, vp, i32, i32, ctypes.c_float, vp, i64, vp, sz, vp]
+        L.svl_kv4_attention.restype = ctypes.c_int
+        L.svl_beam_select_workspace_size.argtypes = [i32] * 4
+        L.svl_beam_select_workspace_size.restype = sz
+        L.svl_beam_select.argtypes = [i32] * 4 + [vp, i64, vp, vp, i32, vp, vp, vp, vp, vp, sz, vp]
+        L.svl_beam_select.restype = ctypes.c_int
+        L.svl_kv4_reorder.argtypes = [desc, vp, i32, i32, vp, vp, vp, vp, vp]
+        L.svl_kv4_reorder.restype = ctypes.c_int
         _lib = L
     return _lib
 
@@ -253,6 +277,52 @@ def svl_decode_step(model, B, tokens, kv_cache, max_len, cache_len, layer_gate, 
     _check("svl_decode_step", lib().svl_decode_step(
         model, int(B), _p(tokens), _p(kv_cache), int(max_len), _p(cache_len), _p(layer_gate), _p(group_gate),
         _p(logits), _p(next_token), _p(workspace), int(workspace_bytes), _stream(stream)))
+
+
+def svl_kv4_cache_size(desc: Kv4Desc) -> int:
+    return int(lib().svl_kv4_cache_size(desc))
+
+
+def svl_kv4_write(desc: Kv4Desc, cache, k, ld_k, v, ld_v, rows, row_off, start, status, stream=None):
+    """Quantises rows of K and V into the slots' positions (see svl.h)."""
+    _check("svl_kv4_write", lib().svl_kv4_write(desc, _p(cache), _p(k), int(ld_k), _p(v), int(ld_v), int(rows),
+                                                _p(row_off), _p(start), _p(status), _stream(stream)))
+
+
+def svl_kv4_read(desc: Kv4Desc, cache, rows, row_off, start, k, ld_k, v, ld_v, stream=None):
+    _check("svl_kv4_read", lib().svl_kv4_read(desc, _p(cache), int(rows), _p(row_off), _p(start), _p(k), int(ld_k),
+                                              _p(v), int(ld_v), _stream(stream)))
+
+
+def svl_kv4_attention_workspace_size(desc: Kv4Desc, n_heads, rows) -> int:
+    return int(lib().svl_kv4_attention_workspace_size(desc, int(n_heads), int(rows)))
+
+
+def svl_kv4_attention(desc: Kv4Desc, cache, n_heads, rows, q, ld_q, start, window, sinks, scale, out, ld_out, workspace,
+                      workspace_bytes, stream=None):
+    """Attention of each slot's newest rows over its cache, with an optional
+    sliding window and first positions that stay visible (see svl.h)."""
+    _check("svl_kv4_attention", lib().svl_kv4_attention(
+        desc, _p(cache), int(n_heads), int(rows), _p(q), int(ld_q), _p(start), int(window), int(sinks), float(scale),
+        _p(out), int(ld_out), _p(workspace), int(workspace_bytes), _stream(stream)))
+
+
+def svl_beam_select_workspace_size(n_samples, beams, vocab, take) -> int:
+    return int(lib().svl_beam_select_workspace_size(int(n_samples), int(beams), int(vocab), int(take)))
+
+
+def svl_beam_select(n_samples, beams, vocab, take, logits, ld, beam_scores, finished, eos, scores_out, parent, token,
+                    finished_out, workspace, workspace_bytes, stream=None):
+    """The best continuations of every sample's beams (see svl.h)."""
+    _check("svl_beam_select", lib().svl_beam_select(
+        int(n_samples), int(beams), int(vocab), int(take), _p(logits), int(ld), _p(beam_scores), _p(finished), int(eos),
+        _p(scores_out), _p(parent), _p(token), _p(finished_out), _p(workspace), int(workspace_bytes), _stream(stream)))
+
+
+def svl_kv4_reorder(desc: Kv4Desc, cache, n_layers, beams, parent, start_from, length, status, stream=None):
+    """Slots take over their parents' rows, in place, in all layers (see svl.h)."""
+    _check("svl_kv4_reorder", lib().svl_kv4_reorder(desc, _p(cache), int(n_layers), int(beams), _p(parent),
+                                                    _p(start_from), _p(length), _p(status), _stream(stream)))
 
 
 def svl_pack_controlled(model, B, n_vis_total, n_text_total, vis_feats, vis_off, kept_idx, kept_off, text_ids,
