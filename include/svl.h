@@ -37,7 +37,9 @@
  * inference rule, Sec. 3.1 and Sec. 3.3), svl_pack_controlled and
  * svl_controlled_prefill (the LLM-side compute controller, Sec. 3.2, Eq. 7),
  * svl_gated_prefill_kv and svl_decode_step (gated decode with a KV cache,
- * which the paper leaves open, Sec. 5), gemm_format = SVL_GEMM_E4M3 with
+ * which the paper leaves open, Sec. 5), svl_kv4_* and svl_beam_select with
+ * svl_gated_prefill_kv4 and svl_decode_step_kv4 (a KV cache in 4 bits, sliding
+ * window and beam search), gemm_format = SVL_GEMM_E4M3 with
  * svl_quantize_rows_e4m3 and svl_gemm_e4m3 (FP8 gated projections; Sec. 5
  * calls quantisation orthogonal to the method), svl_prefill_from_host (the
  * path from host buffers), svl_flops (Eq. 8 on the host) and the profiling and
@@ -347,8 +349,8 @@ svl_status svl_decode_step(svl_model* model, int32_t B, const int32_t* tokens, v
 
 /* ------------------------------------------------------------------------
  * A KV cache in 4 bits, attention over it, and beam search (the paper leaves
- * decode open, Sec. 5, and calls quantisation orthogonal to its method). These
- * calls need no model.
+ * decode open, Sec. 5, and calls quantisation orthogonal to its method). Only
+ * the last two, which run a model over such a cache, need one.
  *
  * One layer's cache is caller-owned device memory of svl_kv4_cache_size()
  * bytes, 16-byte aligned, with n_slots sequences of up to max_len positions:
@@ -455,6 +457,31 @@ svl_status svl_beam_select(int32_t n_samples, int32_t beams, int32_t vocab, int3
 svl_status svl_kv4_reorder(const svl_kv4_desc* desc, void* cache, int32_t n_layers, int32_t beams,
                            const int32_t* parent, const int32_t* from, const int32_t* len, uint32_t* status,
                            void* stream);
+
+/* svl_gated_prefill_kv and svl_decode_step over a 4-bit cache: the caches of
+ * the model's n_layers layers one after the other (n_layers *
+ * svl_kv4_cache_size of {slots, n_kv_heads, d_head, max_len} bytes), max_len <=
+ * the model's max_seq.
+ * The prefill has room for `beams` slots per sample: sample b's prompt goes to
+ * slot b * beams (svl_kv4_reorder with parent 0 hands it to the others), and
+ * cache_len[b * beams + w] is its length for every w < beams. Prompt rows past
+ * max_len are not stored and set SVL_DEV_BAD_INDEX.
+ * The decode step takes one token per slot, with the slots' gates (layer_gate
+ * [n_slots, L], group_gate [n_slots, L, G]): like svl_decode_step, and with
+ * window > 0 the attention of every layer sees the last `window` positions and
+ * the first `sinks` only (svl_kv4_attention). The new rows are quantised
+ * before they are attended to; those of gated-off groups are not written.
+ * Workspace of the step: svl_decode_kv4_workspace_size() bytes, 256-byte
+ * aligned. */
+svl_status svl_gated_prefill_kv4(svl_model* model, int32_t B, int32_t t_cap, void* X, const int32_t* cu_seqlens,
+                                 const int32_t* pos, const uint8_t* layer_gate, const uint8_t* group_gate,
+                                 int32_t logits_mode, float* logits, void* cache, int32_t max_len, int32_t beams,
+                                 int32_t* cache_len, void* workspace, size_t workspace_bytes, void* stream);
+size_t svl_decode_kv4_workspace_size(const svl_model* model, int32_t n_slots, int32_t max_len);
+svl_status svl_decode_step_kv4(svl_model* model, int32_t n_slots, const int32_t* tokens, void* cache,
+                               int32_t max_len, int32_t* cache_len, const uint8_t* layer_gate,
+                               const uint8_t* group_gate, int32_t window, int32_t sinks, float* logits,
+                               int32_t* next_token, void* workspace, size_t workspace_bytes, void* stream);
 
 /* svl_score_select without a workspace argument. The paper has no
  *  counterpart: this exists for callers that cannot allocate device memory

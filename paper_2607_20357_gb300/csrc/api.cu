@@ -879,7 +879,7 @@ struct StageSel {
 
 // KV cache of a prefill (store each layer's K, V) or a decode step (one new
 // row per sample: embedding of the fed token, attention against the cache,
-// greedy next token).
+// greedy next token). The cache is bf16 (kv) or, with kv4, in 4 bits.
 struct StepCtx {
   __nv_bfloat16* kv;  // [2][L][B][max_len][dkv]
   int max_len;
@@ -887,7 +887,15 @@ struct StepCtx {
   int* cache_len;        // [B] decode: positions so far (advanced by one)
   const int* tokens;     // [B] decode: fed token ids
   int* next_token;       // [B] decode: greedy next token, or nullptr
+  const Kv4Cache* kv4 = nullptr;  // layer 0's; the layers' caches lie one after the other
+  int beams = 1;                  // prefill: slots per sample
+  int window = 0, sinks = 0;
+  void* attn_ws = nullptr;
 };
+
+size_t kv4_layer_bytes(const Kv4Cache& c) {
+  return static_cast<size_t>(c.n_slots) * c.kv * c.tiles * kv4_tile_bytes(c.dh);
+}
 
 // The gated decoder forward. With `ctl` (compute controller, Sec. 3.2) the
 // gate arrays are outputs: they start all on, the controller kernel writes
@@ -1204,7 +1212,52 @@ svl_status prefill_impl(svl_model* m, int32_t B, int32_t t_cap, void* X, const i
 
     if (want(l, SVL_LAYER_ATTN)) {
     const size_t layer_kv = static_cast<size_t>(B) * (kvx ? kvx->max_len : 0) * dkv;
-    if (decode) {
+    Kv4Cache c4{};
+    if (kvx && kvx->kv4) {
+      // the new rows go into the 4-bit cache (the prompt's attention below works on the rows themselves)
+      c4 = *kvx->kv4;
+      c4.data += static_cast<size_t>(l) * kv4_layer_bytes(c4);
+      Kv4Rows ra;
+      std::memset(&ra, 0, sizeof(ra));
+      ra.c = c4;
+      ra.rows = t_cap;
+      ra.n = B;
+      ra.slot_step = kvx->beams;
+      ra.row_off = decode ? nullptr : cu_seqlens;
+      ra.start = decode ? kvx->cache_len : nullptr;
+      ra.k = kb;
+      ra.v = vb;
+      ra.k_row = dkv;
+      ra.v_row = 1;
+      ra.v_col = L.t_pad;
+      ra.status = m->d_status;
+      ra.gate = HeadGate{layer_gate, group_gate, nl, l, d.n_prefix, d.n_groups};
+      Launch L1(m, SVL_TAG_COPY, s);
+      next_launch(false);
+      if (launch_kv4_write(ra, s) != cudaSuccess) return SVL_ERR_CUDA;
+    }
+    if (decode && kvx->kv4) {
+      Kv4Attn ka;
+      std::memset(&ka, 0, sizeof(ka));
+      ka.c = c4;
+      ka.A = d.n_heads;
+      ka.rows = 1;
+      ka.q = qb;
+      ka.ldq = hq;
+      ka.out = ao;
+      ka.ldo = hq;
+      ka.start = kvx->cache_len;
+      ka.window = kvx->window;
+      ka.sinks = kvx->sinks;
+      ka.scale = static_cast<float>(1.0 / std::sqrt(static_cast<double>(dh)));
+      ka.gate = HeadGate{layer_gate, group_gate, nl, l, d.n_prefix, d.n_groups};
+      ka.ws = kvx->attn_ws;
+      ka.num_sms = m->num_sms;
+      Launch L1(m, SVL_TAG_ATTENTION, s);
+      ka.late = !f8;
+      next_launch(ka.late);
+      if (launch_kv4_attention(ka, s) != cudaSuccess) return SVL_ERR_CUDA;
+    } else if (decode) {
       DecAttnArgs da;
       std::memset(&da, 0, sizeof(da));
       da.B = B;
@@ -1236,7 +1289,7 @@ svl_status prefill_impl(svl_model* m, int32_t B, int32_t t_cap, void* X, const i
       next_launch(da.late);
       if (launch_decode_attn(da, s) != cudaSuccess) return SVL_ERR_CUDA;
     } else {
-      if (kvx) {
+      if (kvx && !kvx->kv4) {
         KvArgs ka;
         ka.B = B;
         ka.dkv = dkv;
@@ -1402,6 +1455,9 @@ svl_status prefill_impl(svl_model* m, int32_t B, int32_t t_cap, void* X, const i
     Launch L1(m, SVL_TAG_LMHEAD, s);
     if (launch_decode_finish(B, d.vocab, logits, kvx->next_token, kvx->cache_len, kvx->max_len, s) != cudaSuccess)
       return SVL_ERR_CUDA;
+  } else if (kvx && kvx->kv4) {
+    g_launches++;
+    if (launch_kv4_lengths(cu_seqlens, B, kvx->beams, kvx->cache_len, s) != cudaSuccess) return SVL_ERR_CUDA;
   } else if (kvx && kvx->cache_len) {
     launch_offsets_diff(cu_seqlens, kvx->cache_len, B, s);  // cache length = prompt length
     g_launches++;
@@ -1497,6 +1553,21 @@ size_t svl_decode_workspace_size(const svl_model* m, int32_t B) {
   return head + pre_layout(m->d, B, B).total;
 }
 
+namespace {
+// The step's rows, cu_seqlens and positions live at the head of the workspace.
+svl_status decode_step(svl_model* m, int32_t B, const uint8_t* layer_gate, const uint8_t* group_gate, float* logits,
+                       void* ws, size_t ws_bytes, void* stream, const StepCtx& kx) {
+  uint8_t* base = static_cast<uint8_t*>(ws);
+  const size_t xb = align256(2 * static_cast<size_t>(B) * m->d.d_model), cb = align256(4 * (B + 1)),
+               pb = align256(4 * B);
+  void* X = base;
+  int32_t* cu = reinterpret_cast<int32_t*>(base + xb);
+  int32_t* pos = reinterpret_cast<int32_t*>(base + xb + cb);
+  return prefill_impl(m, B, B, X, cu, pos, layer_gate, group_gate, SVL_LOGITS_LAST, logits, base + xb + cb + pb,
+                      ws_bytes - (xb + cb + pb), stream, nullptr, &kx);
+}
+}  // namespace
+
 svl_status svl_decode_step(svl_model* m, int32_t B, const int32_t* tokens, void* kv_cache, int32_t max_len,
                            int32_t* cache_len, const uint8_t* layer_gate, const uint8_t* group_gate, float* logits,
                            int32_t* next_token, void* ws, size_t ws_bytes, void* stream) {
@@ -1504,16 +1575,8 @@ svl_status svl_decode_step(svl_model* m, int32_t B, const int32_t* tokens, void*
       !layer_gate || !group_gate || !logits || !aligned16(kv_cache) || !ws)
     return SVL_ERR_INVALID_ARG;
   if (ws_bytes < svl_decode_workspace_size(m, B)) return SVL_ERR_WORKSPACE;
-  // the step's rows, cu_seqlens and positions live at the head of the workspace
-  uint8_t* base = static_cast<uint8_t*>(ws);
-  const size_t xb = align256(2 * static_cast<size_t>(B) * m->d.d_model), cb = align256(4 * (B + 1)),
-               pb = align256(4 * B);
-  void* X = base;
-  int32_t* cu = reinterpret_cast<int32_t*>(base + xb);
-  int32_t* pos = reinterpret_cast<int32_t*>(base + xb + cb);
   StepCtx kx{static_cast<__nv_bfloat16*>(kv_cache), max_len, 1, cache_len, tokens, next_token};
-  return prefill_impl(m, B, B, X, cu, pos, layer_gate, group_gate, SVL_LOGITS_LAST, logits, base + xb + cb + pb,
-                      ws_bytes - (xb + cb + pb), stream, nullptr, &kx);
+  return decode_step(m, B, layer_gate, group_gate, logits, ws, ws_bytes, stream, kx);
 }
 
 namespace {
@@ -1694,6 +1757,58 @@ svl_status svl_kv4_reorder(const svl_kv4_desc* desc, void* cache, int32_t n_laye
   g_launches++;
   if (launch_kv4_reorder(a, static_cast<cudaStream_t>(stream)) != cudaSuccess) return SVL_ERR_CUDA;
   return last_error();
+}
+
+namespace {
+svl_status model_kv4(const svl_model* m, int32_t n_slots, int32_t max_len, const void* cache, Kv4Cache* c) {
+  const svl_kv4_desc d{n_slots, m->d.n_kv_heads, m->d.d_model / m->d.n_heads, max_len};
+  return kv4_cache(&d, cache, false, c);
+}
+
+// Where a step's attention scratch starts in a decode workspace (its other parts come first).
+size_t decode_kv4_attn_at(const svl_model* m, int32_t B) { return align256(svl_decode_workspace_size(m, B)); }
+}  // namespace
+
+svl_status svl_gated_prefill_kv4(svl_model* m, int32_t B, int32_t t_cap, void* X, const int32_t* cu_seqlens,
+                                 const int32_t* pos, const uint8_t* layer_gate, const uint8_t* group_gate,
+                                 int32_t logits_mode, float* logits, void* cache, int32_t max_len, int32_t beams,
+                                 int32_t* cache_len, void* ws, size_t ws_bytes, void* stream) {
+  if (!m || B <= 0 || !cache_len || max_len <= 0 || max_len > m->d.max_seq || beams <= 0) return SVL_ERR_INVALID_ARG;
+  if (B > kKv4MaxSlots / beams) return SVL_ERR_UNSUPPORTED;
+  Kv4Cache c;
+  const svl_status st = model_kv4(m, B * beams, max_len, cache, &c);
+  if (st != SVL_OK) return st;
+  StepCtx kx{nullptr, max_len, 0, cache_len, nullptr, nullptr};
+  kx.kv4 = &c;
+  kx.beams = beams;
+  return prefill_impl(m, B, t_cap, X, cu_seqlens, pos, layer_gate, group_gate, logits_mode, logits, ws, ws_bytes,
+                      stream, nullptr, &kx);
+}
+
+size_t svl_decode_kv4_workspace_size(const svl_model* m, int32_t n_slots, int32_t max_len) {
+  if (!m || n_slots <= 0) return 0;
+  const svl_kv4_desc d{n_slots, m->d.n_kv_heads, m->d.d_model / m->d.n_heads, max_len};
+  const size_t attn = svl_kv4_attention_workspace_size(&d, m->d.n_heads, 1);
+  return attn ? decode_kv4_attn_at(m, n_slots) + attn : 0;
+}
+
+svl_status svl_decode_step_kv4(svl_model* m, int32_t n_slots, const int32_t* tokens, void* cache, int32_t max_len,
+                               int32_t* cache_len, const uint8_t* layer_gate, const uint8_t* group_gate,
+                               int32_t window, int32_t sinks, float* logits, int32_t* next_token, void* ws,
+                               size_t ws_bytes, void* stream) {
+  if (!m || n_slots <= 0 || !tokens || max_len <= 0 || max_len > m->d.max_seq || !cache_len || !layer_gate ||
+      !group_gate || !logits || window < 0 || sinks < 0)
+    return SVL_ERR_INVALID_ARG;
+  Kv4Cache c;
+  svl_status st = model_kv4(m, n_slots, max_len, cache, &c);
+  if (st != SVL_OK) return st;
+  if ((st = check_ws(ws, ws_bytes, svl_decode_kv4_workspace_size(m, n_slots, max_len))) != SVL_OK) return st;
+  StepCtx kx{nullptr, max_len, 1, cache_len, tokens, next_token};
+  kx.kv4 = &c;
+  kx.window = window;
+  kx.sinks = sinks;
+  kx.attn_ws = at<uint8_t>(ws, decode_kv4_attn_at(m, n_slots));
+  return decode_step(m, n_slots, layer_gate, group_gate, logits, ws, decode_kv4_attn_at(m, n_slots), stream, kx);
 }
 
 svl_status svl_quantize_rows_e4m3(const void* src, const void* gain, int64_t rows, int32_t cols, int64_t ld_src,

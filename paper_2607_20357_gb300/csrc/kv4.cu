@@ -155,6 +155,15 @@ static cudaError_t row_launch(void (*kernel)(Kv4Rows), const Kv4Rows& a, cudaStr
 cudaError_t launch_kv4_write(const Kv4Rows& a, cudaStream_t s) { return row_launch(kv4_write_kernel, a, s); }
 cudaError_t launch_kv4_read(const Kv4Rows& a, cudaStream_t s) { return row_launch(kv4_read_kernel, a, s); }
 
+__global__ void kv4_lengths_kernel(const int* cu_seqlens, int n, int beams, int* len) {
+  pdl_begin(false);
+  const int i = blockIdx.x * blockDim.x + threadIdx.x;
+  if (i < n) len[i] = cu_seqlens[i / beams + 1] - cu_seqlens[i / beams];
+}
+cudaError_t launch_kv4_lengths(const int* cu_seqlens, int B, int beams, int* len, cudaStream_t s) {
+  return launch_pdl(kv4_lengths_kernel, dim3((B * beams + 127) / 128), 128, 0, s, cu_seqlens, B * beams, beams, len);
+}
+
 // One thread per 16 bytes of a tile, for all slots of a sample: each reads what the
 // moved slots take over before it writes any of them, so the slots change in place
 // whatever the parents are.

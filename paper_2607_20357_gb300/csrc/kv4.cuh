@@ -67,6 +67,9 @@ struct Kv4Rows {
 cudaError_t launch_kv4_write(const Kv4Rows& a, cudaStream_t s);
 cudaError_t launch_kv4_read(const Kv4Rows& a, cudaStream_t s);
 
+// len[b * beams + w] = cu_seqlens[b + 1] - cu_seqlens[b]
+cudaError_t launch_kv4_lengths(const int* cu_seqlens, int B, int beams, int* len, cudaStream_t s);
+
 struct Kv4Attn {
   Kv4Cache c;
   int A, rows;

@@ -34,7 +34,8 @@ SYMBOLS = ["svl_model_create", "svl_model_destroy", "svl_workspace_size", "svl_s
            "svl_kv_cache_size", "svl_gated_prefill_kv", "svl_decode_workspace_size", "svl_decode_step",
            "svl_quantize_rows_e4m3", "svl_gemm_e4m3", "svl_layer_stage", "svl_ksplit_plan", "svl_kv4_cache_size",
            "svl_kv4_write", "svl_kv4_read", "svl_kv4_attention_workspace_size", "svl_kv4_attention",
-           "svl_beam_select_workspace_size", "svl_beam_select", "svl_kv4_reorder"]
+           "svl_beam_select_workspace_size", "svl_beam_select", "svl_kv4_reorder", "svl_gated_prefill_kv4",
+           "svl_decode_kv4_workspace_size", "svl_decode_step_kv4"]
 
 TAGS = ["budget_embed", "score", "select", "pack", "projector", "schedule", "rmsnorm", "qkv_gemm", "attention",
         "o_gemm", "gateup_gemm", "down_gemm", "lm_head", "host_copy", "quant"]
@@ -156,6 +157,12 @@ def lib():
         L.svl_beam_select.restype = ctypes.c_int
         L.svl_kv4_reorder.argtypes = [desc, vp, i32, i32, vp, vp, vp, vp, vp]
         L.svl_kv4_reorder.restype = ctypes.c_int
+        L.svl_gated_prefill_kv4.argtypes = [vp, i32, i32, vp, vp, vp, vp, vp, i32, vp, vp, i32, i32, vp, vp, sz, vp]
+        L.svl_gated_prefill_kv4.restype = ctypes.c_int
+        L.svl_decode_kv4_workspace_size.argtypes = [vp, i32, i32]
+        L.svl_decode_kv4_workspace_size.restype = sz
+        L.svl_decode_step_kv4.argtypes = [vp, i32, vp, vp, i32, vp, vp, vp, i32, i32, vp, vp, vp, sz, vp]
+        L.svl_decode_step_kv4.restype = ctypes.c_int
         _lib = L
     return _lib
 
@@ -323,6 +330,25 @@ def svl_kv4_reorder(desc: Kv4Desc, cache, n_layers, beams, parent, start_from, l
     """Slots take over their parents' rows, in place, in all layers (see svl.h)."""
     _check("svl_kv4_reorder", lib().svl_kv4_reorder(desc, _p(cache), int(n_layers), int(beams), _p(parent),
                                                     _p(start_from), _p(length), _p(status), _stream(stream)))
+
+
+def svl_gated_prefill_kv4(model, B, t_cap, X, cu_seqlens, pos, layer_gate, group_gate, logits_mode, logits, cache,
+                          max_len, beams, cache_len, workspace, workspace_bytes, stream=None):
+    _check("svl_gated_prefill_kv4", lib().svl_gated_prefill_kv4(
+        model, int(B), int(t_cap), _p(X), _p(cu_seqlens), _p(pos), _p(layer_gate), _p(group_gate),
+        int(logits_mode), _p(logits), _p(cache), int(max_len), int(beams), _p(cache_len), _p(workspace),
+        int(workspace_bytes), _stream(stream)))
+
+
+def svl_decode_kv4_workspace_size(model, n_slots, max_len) -> int:
+    return int(lib().svl_decode_kv4_workspace_size(model, int(n_slots), int(max_len)))
+
+
+def svl_decode_step_kv4(model, n_slots, tokens, cache, max_len, cache_len, layer_gate, group_gate, window, sinks,
+                        logits, next_token, workspace, workspace_bytes, stream=None):
+    _check("svl_decode_step_kv4", lib().svl_decode_step_kv4(
+        model, int(n_slots), _p(tokens), _p(cache), int(max_len), _p(cache_len), _p(layer_gate), _p(group_gate),
+        int(window), int(sinks), _p(logits), _p(next_token), _p(workspace), int(workspace_bytes), _stream(stream)))
 
 
 def svl_pack_controlled(model, B, n_vis_total, n_text_total, vis_feats, vis_off, kept_idx, kept_off, text_ids,
@@ -572,3 +598,59 @@ class GatedPrefill:
             svl_gated_prefill(self.handle, B, max(nv + nt, 1), out["X"], out["cu_seqlens"], out["pos"],
                               gates[0], gates[1], logits_mode, out["logits"], ws, wsb, stream)
         return out
+
+    def beam_search(self, batch: dict, beams: int, steps: int, eos: int = -1, window: int = 0, sinks: int = 0) -> dict:
+        """Beam search over a 4-bit KV cache: prefill, then `steps` tokens for
+        each of `beams` beams per sample under the prompt's gates, with
+        attention to the last `window` positions and the first `sinks` only
+        if window > 0. A beam that takes the id `eos` is finished and stands
+        for itself from then on (eos < 0: none does).
+
+        Returns tensors on the device, the best beam first: tokens
+        [B, beams, steps] int32 (a finished beam's tail is eos), scores
+        [B, beams] float32 (log-probabilities, summed), finished [B, beams]
+        uint8, cache_len [B * beams]. Nothing waits for the device between
+        the steps."""
+        d, B, W = self.dims, batch["B"], int(beams)
+        if W < 1 or steps < 1:
+            raise ValueError(f"beams {beams}, steps {steps}: at least one of each")
+        dev = batch["vis"].device
+        nv, nt = batch["vis"].shape[0], int(batch["text_ids"].shape[0])
+        prompt = (batch["vis_off"][1:] - batch["vis_off"][:-1]) + (batch["text_off"][1:] - batch["text_off"][:-1])
+        max_len = min(int(prompt.max()) + steps, self.desc.max_seq)
+        desc = Kv4Desc(B * W, d.n_kv_heads, d.d_head, max_len)
+        u8 = dict(dtype=torch.uint8, device=dev)
+        i32 = dict(dtype=torch.int32, device=dev)
+        cache = torch.empty(d.n_layers * svl_kv4_cache_size(desc), **u8)
+        cache_len = torch.empty(B * W, **i32)
+        out = self.run(batch, stages=("select", "pack"))
+        ws, wsb = self.workspace(B, nv, nt, dev, ("prefill",))
+        svl_gated_prefill_kv4(self.handle, B, max(nv + nt, 1), out["X"], out["cu_seqlens"], out["pos"],
+                              batch["layer_gate"], batch["group_gate"], SVL_LOGITS_LAST, out["logits"], cache, max_len,
+                              W, cache_len, ws, wsb)
+        prompt_len = cache_len[::W].contiguous()
+        layer_gate = batch["layer_gate"].repeat_interleave(W, 0).contiguous()
+        group_gate = batch["group_gate"].repeat_interleave(W, 0).contiguous()
+        size = max(svl_beam_select_workspace_size(B, 1, d.vocab, W), svl_beam_select_workspace_size(B, W, d.vocab, W))
+        bws = torch.empty(max(size, 1), **u8)
+        dws = torch.empty(svl_decode_kv4_workspace_size(self.handle, B * W, max_len), **u8)
+        logits = torch.empty(B * W, d.vocab, dtype=torch.float32, device=dev)
+        scores = torch.zeros(B, 1, dtype=torch.float32, device=dev)
+        finished, tokens, parents = None, torch.empty(steps, B, W, **i32), torch.empty(steps, B, W, **i32)
+        for t in range(steps):
+            if t:
+                svl_decode_step_kv4(self.handle, B * W, tokens[t - 1], cache, max_len, cache_len, layer_gate,
+                                    group_gate, window, sinks, logits, None, dws, dws.numel())
+            next_scores, next_finished = torch.empty(B, W, dtype=torch.float32, device=dev), torch.empty(B, W, **u8)
+            svl_beam_select(B, W if t else 1, d.vocab, W, logits if t else out["logits"], d.vocab, scores, finished, eos,
+                            next_scores, parents[t], tokens[t], next_finished, bws, bws.numel())
+            scores, finished = next_scores, next_finished
+            if t + 1 < steps:  # (after the prefill every beam takes over the prompt from the first)
+                svl_kv4_reorder(desc, cache, d.n_layers, W, parents[t], prompt_len if t else None, cache_len, None)
+        # each beam's tokens, from its last one back
+        at = torch.arange(W, device=dev).expand(B, W)
+        path = []
+        for t in range(steps - 1, -1, -1):
+            path.append(tokens[t].gather(1, at))
+            at = parents[t].long().gather(1, at)
+        return {"tokens": torch.stack(path[::-1], -1), "scores": scores, "finished": finished, "cache_len": cache_len}
