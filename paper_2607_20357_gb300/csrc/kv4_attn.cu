@@ -3,66 +3,696 @@
 // over the positions j that the row at position pos sees: j <= pos, and with a
 // window W > 0 only j > pos - W or j < sinks. A row with pos < 0 sees nothing
 // and a row with pos >= max_len has no place in the cache: both give zeros.
+//
+// Bound by the cache's bytes (d_head * 9 / 8 per position and KV head) if a value
+// costs no more than about three instructions' lanes on its way from memory, which
+// is what decides the design:
+//  - The products run on mma.m16n8k16 with 16-bit operands and float32 sums:
+//    S = K q with 16 positions as rows and 8 columns, O^T = V^T P with 16
+//    dimensions as rows. A column is a query head of the KV head or one of its
+//    rows (drafted tokens); up to eight share one pass over the cache. (tcgen05 has
+//    128 rows and takes its operands from shared memory, to which every
+//    dequantised value would have to be written first.)
+//  - K's codes become float16 operands by masking alone (see kv4.cuh): n * 2^-24
+//    and n * 2^-20, both exact; q is scaled by a power of two to fill float16's
+//    range (bf16 has fewer bits, so that it is exact but for elements under 2^-29
+//    of the head's largest), times 2^-4 where it meets the second kind. The -8 of
+//    s * (n - 8) costs nothing: the accumulators start at -8 * sum q of the group.
+//    The scales multiply the 32-dimension partial sums in float32.
+//  - V's codes become bf16 operands n - 8 (128 + n by masking, less 136; taken off
+//    O at the end instead, the 8 would leave the rounding of sums of 8 s in
+//    dimensions much smaller than their group). Its scales multiply the weights.
+//    Weights and products are pairs of bf16 numbers, of 16 bits together and with
+//    float32's range: float16 (one product instead of two, 15 % faster) would lose
+//    weights under 2^-38 of the largest, which are all there is in a dimension where
+//    the rows of larger weight hold zeros.
+//
+// Work is cut by tiles, not by heads or slots, so that ragged lengths and few slots
+// fill the GPU alike: the tiles of all (slot, KV head, column tile) items in a row
+// are divided evenly over the SMs and there over the warps. A warp walks its tiles
+// with an online softmax, its next tiles on their way into a ring of its own in
+// shared memory (cp.async). Items that end up in several warps are put together
+// from their parts in order: in shared memory within a CTA, by a second launch
+// across CTAs.
+#include <cuda_fp16.h>
+
 #include "kv4.cuh"
 
 namespace svl {
 
-constexpr int kSimpleThreads = 32;
+constexpr int kAttnWarps = 16, kAttnThreads = kAttnWarps * 32;
+constexpr int kCols = 8;
+constexpr int kMaxCtas = 256;
+constexpr int kMergeThreads = 128;
 
-// A warp per (slot, row, head), a lane per d_head / 32 dimensions.
-template <int DH>
-__global__ void __launch_bounds__(kSimpleThreads) kv4_attn_kernel(Kv4Attn a) {
-  constexpr int J = DH / 32;
-  pdl_begin(a.late);
-  const int b = blockIdx.z, r = blockIdx.y, h = blockIdx.x, lane = threadIdx.x;
-  const int grp = a.A / a.c.kv, kvh = h / grp;
-  if (!gate_on(a.gate, b, a.gate.G ? h / (a.A / a.gate.G) : 0)) return;
-  const int64_t row = static_cast<int64_t>(b) * a.rows + r;
-  const int64_t pos = static_cast<int64_t>(a.start[b]) + r;
-  const int end = pos >= 0 && pos < a.c.max_len ? static_cast<int>(pos) + 1 : 0;
-  const int lo = a.window > 0 && end > a.window ? end - a.window : 0;
-  float q[J], o[J], m = -INFINITY, l = 0.f;
-#pragma unroll
-  for (int j = 0; j < J; ++j) {
-    q[j] = __bfloat162float(a.q[row * a.ldq + h * DH + 32 * j + lane]) * a.scale;
-    o[j] = 0.f;
-  }
-  const int g = lane / 4;
-  for (int p = 0; p < end; ++p) {
-    if (p >= a.sinks && p < lo) p = lo;
-    const uint8_t* tile = kv4_tile(a.c, b, kvh, p / kKv4Tile);
-    const int i = p % kKv4Tile;
-    float x = 0.f, v[J];
-#pragma unroll
-    for (int j = 0; j < J; ++j) {
-      const int nk = tile[((i * 4 + lane / 8) * J + j) * 4 + lane % 8 / 2] >> (4 * (lane & 1)) & 15;
-      const int nv = tile[kv4_v_codes(DH) + ((((i / 8) * 8 + g) * 4 + i % 8 / 2) * J + j) * 4 + (i & 1) * 2 +
-                          lane % 4 / 2] >> (4 * (lane & 1)) & 15;
-      const float sk = __bfloat162float(reinterpret_cast<const __nv_bfloat16*>(tile + kv4_k_scales(DH))[i * J + j]);
-      const float sv =
-          __bfloat162float(reinterpret_cast<const __nv_bfloat16*>(tile + kv4_v_scales(DH))[(i / 2 * J + j) * 2 + (i & 1)]);
-      x = fmaf(q[j], sk * (nk - 8), x);
-      v[j] = sv * (nv - 8);
-    }
-#pragma unroll
-    for (int off = 16; off > 0; off >>= 1) x += __shfl_xor_sync(0xffffffffu, x, off);
-    const float mn = fmaxf(m, x), corr = expf(m - mn), e = expf(x - mn);
-    l = l * corr + e;
-#pragma unroll
-    for (int j = 0; j < J; ++j) o[j] = fmaf(e, v[j], o[j] * corr);
-    m = mn;
-  }
-  const float inv = l == 0.f ? 0.f : 1.f / l;
-#pragma unroll
-  for (int j = 0; j < J; ++j) a.out[row * a.ldo + h * DH + 32 * j + lane] = __float2bfloat16_rn(o[j] * inv);
+struct AttnParams {
+  Kv4Attn a;
+  int ncols;      // columns of an item: min(8, rows * heads per KV head)
+  int col_tiles;  // items per KV head
+  int min_tiles;  // least tiles of a CTA that has any
+  float* part;    // [CTAs][2][ncols * (d_head + 2)]: parts of items shared with other CTAs, the one from
+                  // the CTA before and the one that the next goes on with
+  int4* meta;     // [CTAs]: {slot (-1: none), item} of the latter; whether there is one of the former
+                  // (0: none, 1: it goes on, 2: it ends here)
+};
+
+// The tiles of a slot that any of its rows sees: `sink` tiles from 0 on, then those from `first`.
+struct Span {
+  int n, sink, first;
+};
+SVL_DEVINL Span slot_span(const Kv4Attn& a, int slot) {
+  const int64_t start = a.start[slot];
+  const int64_t last = start + a.rows < a.c.max_len ? start + a.rows : a.c.max_len;  // end of the last row's sight
+  Span s{1, 1, 0};  // nothing visible: one tile, all masked, gives the zeros
+  if (start >= a.c.max_len || last <= 0) return s;
+  const int hi = static_cast<int>(last), lowest = static_cast<int>(start > 0 ? start : 0) + 1;
+  const int lo = a.window > 0 && lowest > a.window ? lowest - a.window : 0;
+  const int end = (hi - 1) / kKv4Tile + 1;
+  s.first = lo / kKv4Tile;
+  const int sinks = a.sinks < hi ? a.sinks : hi;
+  const int st = sinks > 0 ? (sinks - 1) / kKv4Tile + 1 : 0;
+  s.sink = st < s.first ? st : s.first;
+  s.n = s.sink + end - s.first;
+  return s;
 }
 
-size_t kv4_attn_workspace(const Kv4Cache&, int, int) { return 0; }
+// KV heads of a slot that run.
+SVL_DEVINL int slot_heads(const Kv4Attn& a, int slot) {
+  if (!a.gate.group_gate) return a.c.kv;
+  int n = 0;
+  for (int g = 0; g < a.gate.G; ++g) n += gate_on(a.gate, slot, g) ? a.c.kv / a.gate.G : 0;
+  return n;
+}
+// The i-th of them.
+SVL_DEVINL int slot_head(const Kv4Attn& a, int slot, int i) {
+  if (!a.gate.group_gate) return i;
+  const int per = a.c.kv / a.gate.G;
+  for (int g = 0; g < a.gate.G; ++g) {
+    if (!gate_on(a.gate, slot, g)) continue;
+    if (i < per) return g * per + i;
+    i -= per;
+  }
+  return 0;
+}
+
+// A place in the row of all tiles.
+struct Cursor {
+  int slot, item, tile, items;  // items of the slot
+  int head;                     // KV head of the item
+  Span span;
+};
+SVL_DEVINL void cursor_slot(const AttnParams& p, Cursor& c) {
+  c.items = slot_heads(p.a, c.slot) * p.col_tiles;
+  c.span = slot_span(p.a, c.slot);
+}
+SVL_DEVINL void cursor_head(const AttnParams& p, Cursor& c) {
+  c.head = slot_head(p.a, c.slot, p.col_tiles == 1 ? c.item : c.item / p.col_tiles);
+}
+SVL_DEVINL void cursor_next(const AttnParams& p, Cursor& c) {
+  if (++c.tile < c.span.n) return;
+  c.tile = 0;
+  if (++c.item >= c.items) {
+    c.item = 0;
+    do {
+      if (++c.slot >= p.a.c.n_slots) return;
+      cursor_slot(p, c);
+    } while (c.items == 0);
+  }
+  cursor_head(p, c);
+}
+SVL_DEVINL int cursor_tile(const Cursor& c) {
+  return c.tile < c.span.sink ? c.tile : c.span.first + c.tile - c.span.sink;
+}
+
+SVL_DEVINL void cp16(uint32_t smem, const void* gmem) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem), "l"(gmem) : "memory");
+}
+SVL_DEVINL void cp_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+SVL_DEVINL void cp_wait() {
+  asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
+}
+
+// D = A B + C, 16 x 8 x 16, float32 sums, float16 or bf16 operands.
+SVL_DEVINL void mma16816(float* d, uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1,
+                         const float* c) {
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, "
+      "{%10, %11, %12, %13};"
+      : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(c[0]), "f"(c[1]), "f"(c[2]), "f"(c[3]));
+}
+SVL_DEVINL void mma16816_bf16(float* d, uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, "
+      "{%0, %1, %2, %3};"
+      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+// An 8 x 8 matrix of 16-bit values, two neighbours of a row per lane, transposed.
+SVL_DEVINL uint32_t transpose8(uint32_t x) {
+  uint32_t y;
+  asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+  return y;
+}
+SVL_DEVINL uint32_t pack_f16x2(float lo, float hi) {
+  const __half2 h = __floats2half2_rn(lo, hi);
+  return *reinterpret_cast<const uint32_t*>(&h);
+}
+SVL_DEVINL float bf16_lo(uint32_t u) { return __uint_as_float(u << 16); }
+SVL_DEVINL float bf16_hi(uint32_t u) { return __uint_as_float(u & 0xffff0000u); }
+constexpr uint32_t kLow = 0x000f000fu, kHigh = 0x00f000f0u;
+SVL_DEVINL __nv_bfloat162 as_bf16x2(uint32_t u) { return *reinterpret_cast<__nv_bfloat162*>(&u); }
+SVL_DEVINL uint32_t bits_of(__nv_bfloat162 x) { return *reinterpret_cast<uint32_t*>(&x); }
+// The lowest nibble of each half, less 8, as bf16.
+SVL_DEVINL uint32_t v_codes(uint32_t x) {
+  return bits_of(__hadd2(as_bf16x2((x & kLow) | 0x43004300u), as_bf16x2(0xc308c308u)));  // 128 + n, -136
+}
+SVL_DEVINL uint32_t bits_below(int n) { return n <= 0 ? 0u : (n >= 32 ? ~0u : (1u << n) - 1u); }
+SVL_DEVINL float max_quads(float x) {  // over the eight lanes that share lane % 4
+#pragma unroll
+  for (int off = 4; off <= 16; off <<= 1) x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, off));
+  return x;
+}
+
+constexpr float kTwo24 = 16777216.f;
+
+template <int J>
+struct Words {
+  uint32_t w[J];
+};
+template <int J>
+SVL_DEVINL Words<J> lds_words(const uint8_t* p) {
+  Words<J> r;
+  if constexpr (J == 4) {
+    const uint4 u = *reinterpret_cast<const uint4*>(p);
+    r.w[0] = u.x;
+    r.w[1] = u.y;
+    r.w[2] = u.z;
+    r.w[3] = u.w;
+  } else {
+    const uint2 u = *reinterpret_cast<const uint2*>(p);
+    r.w[0] = u.x;
+    r.w[1] = u.y;
+  }
+  return r;
+}
+
+// Writes four neighbouring output dimensions of column `col` of an item.
+SVL_DEVINL void store_out(const AttnParams& p, int slot, int head, int col, int d, float4 o) {
+  const int grp = p.a.A / p.a.c.kv, r = col / grp, h = head * grp + col - r * grp;
+  __nv_bfloat16* out = p.a.out + (static_cast<int64_t>(slot) * p.a.rows + r) * p.a.ldo + h * p.a.c.dh + d;
+  *reinterpret_cast<uint2*>(out) = make_uint2(pack_bf16x2(o.x, o.y), pack_bf16x2(o.z, o.w));
+}
+
+// A part of an item holds, per column, the output of its positions alone (ncols *
+// d_head floats), then the maximum (times log2 e) and the sum of their weights.
+static int part_floats(int ncols, int dh) { return (ncols * (dh + 2) + 3) & ~3; }  // (whole float4s)
+
+SVL_DEVINL void add_scaled(float4& o, float f, float4 x) {
+  o.x = fmaf(f, x.x, o.x);
+  o.y = fmaf(f, x.y, o.y);
+  o.z = fmaf(f, x.z, o.z);
+  o.w = fmaf(f, x.w, o.w);
+}
+// The weight 2^(m - M) l of a part beside the others' maximum M (0: it saw nothing).
+SVL_DEVINL float part_weight(float m, float l, float M) { return l == 0.f ? 0.f : l * ex2(m - M); }
+
+template <int DH, int NS>
+__global__ void __launch_bounds__(kAttnThreads, 1) kv4_attn_kernel(AttnParams p, int slot_floats) {
+  constexpr int J = DH / 32, TB = kv4_tile_bytes(DH);
+  extern __shared__ __align__(128) uint8_t smem[];  // per warp: ring of NS tiles; then per warp a part
+  __shared__ int64_t scan[kAttnWarps];
+  __shared__ Cursor at_cursor[kAttnWarps];
+  __shared__ int4 w_meta[kAttnWarps];  // {slot, item of the part in the ring (-1: none), state of the other part, -}
+  __shared__ int4 w_first[kAttnWarps];  // slot, item and KV head of that other part
+  const Kv4Attn& a = p.a;
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int g = lane >> 2, t = lane & 3;
+  uint8_t* ring = smem + warp * (NS * TB);
+  float* first_part = reinterpret_cast<float*>(smem + kAttnWarps * (NS * TB)) + warp * slot_floats;
+  float* last_part = reinterpret_cast<float*>(ring);
+  pdl_begin(false);
+
+  // ---- this warp's share of all tiles
+  const int per = (a.c.n_slots + kAttnThreads - 1) / kAttnThreads;
+  const int s0 = min(tid * per, a.c.n_slots), s1 = min(s0 + per, a.c.n_slots);
+  int64_t mine = 0;
+  for (int s = s0; s < s1; ++s) mine += static_cast<int64_t>(slot_heads(a, s)) * p.col_tiles * slot_span(a, s).n;
+  int64_t incl = mine;
+#pragma unroll
+  for (int off = 1; off < 32; off <<= 1) {
+    const int64_t x = __shfl_up_sync(0xffffffffu, incl, off);
+    if (lane >= off) incl += x;
+  }
+  if (lane == 31) scan[warp] = incl;
+  if (tid < kAttnWarps) w_meta[tid] = make_int4(-1, 0, 0, 0);
+  __syncthreads();
+  int64_t total = 0, before = incl - mine;
+  for (int w = 0; w < kAttnWarps; ++w) {
+    if (w < warp) before += scan[w];
+    total += scan[w];
+  }
+  int64_t cta_tiles = (total + gridDim.x - 1) / gridDim.x;
+  if (cta_tiles < p.min_tiles) cta_tiles = p.min_tiles;
+  const int64_t cta0 = min(total, cta_tiles * blockIdx.x), cta1 = min(total, cta0 + cta_tiles);
+  const int64_t share = (cta1 - cta0 + kAttnWarps - 1) / kAttnWarps;
+  // the thread that owns a warp's first tile finds its place
+  for (int w = 0; w < kAttnWarps; ++w) {
+    const int64_t x = cta0 + w * share;
+    if (x < cta1 && x >= before && x < before + mine) {
+      int64_t rest = x - before;
+      Cursor c;
+      for (c.slot = s0;; ++c.slot) {
+        cursor_slot(p, c);
+        const int64_t n = static_cast<int64_t>(c.items) * c.span.n;
+        if (rest < n) break;
+        rest -= n;
+      }
+      c.item = static_cast<int>(rest / c.span.n);
+      c.tile = static_cast<int>(rest - static_cast<int64_t>(c.item) * c.span.n);
+      cursor_head(p, c);
+      at_cursor[w] = c;
+    }
+  }
+  __syncthreads();
+  const int64_t w0 = cta0 + warp * share;
+  const int n = w0 < cta1 ? static_cast<int>(min(share, cta1 - w0)) : 0;
+
+  // ---- the tiles
+  if (n > 0) {
+    Cursor cur = at_cursor[warp], req = cur;
+    const uint32_t ring_s = smem_u32(ring);
+    auto request = [&](int stage) {
+      const uint8_t* src = kv4_tile(a.c, req.slot, req.head, cursor_tile(req));
+#pragma unroll
+      for (int i = 0; i < (TB / 16 + 31) / 32; ++i) {
+        const int c = i * 32 + lane;
+        if (TB / 16 % 32 == 0 || c < TB / 16) cp16(ring_s + stage * TB + c * 16, src + c * 16);
+      }
+    };
+    int asked = 0;
+    for (; asked < NS - 1; ++asked) {
+      if (asked < n) {
+        request(asked);
+        if (asked + 1 < n) cursor_next(p, req);
+      }
+      cp_commit();
+    }
+    uint32_t q[J][4];
+    float qsum[J][2], factor[2], m[2], l[2], o[J][2][4];
+    int end[2], low[2];
+    int col0 = 0;
+    bool started = false;
+    for (int i = 0; i < n; ++i) {
+      cp_wait<NS - 2>();
+      __syncwarp();  // the tile is here for every lane, and the one before has been read by all
+      if (asked < n) {
+        request(asked % NS);
+        if (++asked < n) cursor_next(p, req);
+      }
+      cp_commit();
+      if (i == 0 || cur.tile == 0) {
+        // a new item: its columns' queries as operands
+        started = cur.tile == 0;
+        const int grp = a.A / a.c.kv;
+        const int head = cur.head;
+        col0 = cur.item % p.col_tiles * kCols;
+        const int cols = min(kCols, a.rows * grp - col0);
+        uint4 raw[J];
+        float big = 0.f;
+#pragma unroll
+        for (int j = 0; j < J; ++j) raw[j] = make_uint4(0, 0, 0, 0);
+        if (g < cols) {
+          const int r = (col0 + g) / grp, h = head * grp + col0 + g - r * grp;
+          const uint4* src = reinterpret_cast<const uint4*>(
+              a.q + (static_cast<int64_t>(cur.slot) * a.rows + r) * a.ldq + h * DH + 8 * t);
+#pragma unroll
+          for (int j = 0; j < J; ++j) raw[j] = src[4 * j];
+        }
+#pragma unroll
+        for (int j = 0; j < J; ++j) {
+          const uint32_t u[4] = {raw[j].x, raw[j].y, raw[j].z, raw[j].w};
+#pragma unroll
+          for (int k = 0; k < 4; ++k) big = fmaxf(big, fmaxf(fabsf(bf16_lo(u[k])), fabsf(bf16_hi(u[k]))));
+        }
+        big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, 1));
+        big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, 2));
+        // the largest to [2^14, 2^15)
+        const int eb = min(max(static_cast<int>(__float_as_uint(big) >> 23), 14), 254);
+        const float up = __uint_as_float(static_cast<uint32_t>(268 - eb) << 23);
+        const float f = a.scale * 1.4426950408889634f * 1024.f * __uint_as_float(static_cast<uint32_t>(eb) << 23);
+#pragma unroll
+        for (int j = 0; j < J; ++j) {
+          const uint32_t u[4] = {raw[j].x, raw[j].y, raw[j].z, raw[j].w};  // dimensions 2 k, 2 k + 1 of the eight
+          q[j][0] = pack_f16x2(bf16_lo(u[0]) * up, bf16_lo(u[2]) * up);                      // 0, 4
+          q[j][1] = pack_f16x2(bf16_lo(u[1]) * up, bf16_lo(u[3]) * up);                      // 2, 6
+          q[j][2] = pack_f16x2(bf16_hi(u[0]) * up * 0.0625f, bf16_hi(u[2]) * up * 0.0625f);  // 1, 5
+          q[j][3] = pack_f16x2(bf16_hi(u[1]) * up * 0.0625f, bf16_hi(u[3]) * up * 0.0625f);  // 3, 7
+          float s = 0.f;
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            const float2 x = __half22float2(*reinterpret_cast<const __half2*>(&q[j][k]));
+            s += k < 2 ? x.x + x.y : 16.f * (x.x + x.y);
+          }
+          s += __shfl_xor_sync(0xffffffffu, s, 1);
+          s += __shfl_xor_sync(0xffffffffu, s, 2);
+          s *= -8.f / kTwo24;
+          // from the operand's columns (lane / 4) to the accumulators' (2 t, 2 t + 1)
+          qsum[j][0] = __shfl_sync(0xffffffffu, s, 8 * t);
+          qsum[j][1] = __shfl_sync(0xffffffffu, s, 8 * t + 4);
+        }
+        factor[0] = __shfl_sync(0xffffffffu, f, 8 * t);
+        factor[1] = __shfl_sync(0xffffffffu, f, 8 * t + 4);
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+          const int64_t pos = static_cast<int64_t>(a.start[cur.slot]) + (col0 + 2 * t + c) / grp;
+          // (-1: no such column)
+          end[c] = 2 * t + c >= cols ? -1 : (pos >= 0 && pos < a.c.max_len ? static_cast<int>(pos) + 1 : 0);
+          low[c] = a.window > 0 && end[c] > a.window ? end[c] - a.window : 0;
+          m[c] = -INFINITY;
+          l[c] = 0.f;
+        }
+#pragma unroll
+        for (int j = 0; j < J; ++j)
+#pragma unroll
+          for (int k = 0; k < 8; ++k) o[j][k >> 2][k & 3] = 0.f;
+      }
+
+      uint8_t* tile = ring + (i % NS) * TB;
+      const int p0 = cursor_tile(cur) * kKv4Tile;
+      uint32_t sight[2];  // of the tile's positions
+#pragma unroll
+      for (int c = 0; c < 2; ++c)
+        sight[c] = (bits_below(end[c] - p0) & ~bits_below(low[c] - p0)) | bits_below(min(a.sinks, end[c]) - p0);
+      const bool whole = __all_sync(0xffffffffu, (end[0] < 0 || sight[0] == ~0u) && (end[1] < 0 || sight[1] == ~0u));
+
+      // whether a scale of V is not finite (a stored NaN, or what lies where nothing was written)
+      bool odd = false;
+#pragma unroll
+      for (int k = 0; k < J / 2; ++k) {
+        const uint32_t x = reinterpret_cast<const uint32_t*>(tile + kv4_v_scales(DH))[lane * (J / 2) + k];
+        odd |= (x & 0x7f80u) == 0x7f80u || (x & 0x7f800000u) == 0x7f800000u;
+      }
+      odd = __any_sync(0xffffffffu, odd);
+
+      // scores of the tile's 32 positions
+      float s[2][4];
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const Words<J> wa = lds_words<J>(tile + ((16 * h + g) * 4 + t) * J * 4);
+        const Words<J> wb = lds_words<J>(tile + ((16 * h + g + 8) * 4 + t) * J * 4);
+        const uint8_t* sk = tile + kv4_k_scales(DH) + (16 * h + g) * J * 2;
+        uint32_t ka[J / 2], kb[J / 2];
+#pragma unroll
+        for (int k = 0; k < J / 2; ++k) {
+          ka[k] = reinterpret_cast<const uint32_t*>(sk)[k];
+          kb[k] = reinterpret_cast<const uint32_t*>(sk + 8 * J * 2)[k];
+        }
+#pragma unroll
+        for (int j = 0; j < J; ++j) {
+          const float c0[4] = {qsum[j][0], qsum[j][1], qsum[j][0], qsum[j][1]};
+          float d[4];
+          const uint32_t x = wa.w[j], y = wb.w[j], x8 = x >> 8, y8 = y >> 8;
+          mma16816(d, x & kLow, y & kLow, x8 & kLow, y8 & kLow, q[j][0], q[j][1], c0);
+          mma16816(d, x & kHigh, y & kHigh, x8 & kHigh, y8 & kHigh, q[j][2], q[j][3], d);
+          const float fa = j & 1 ? bf16_hi(ka[j / 2]) : bf16_lo(ka[j / 2]);
+          const float fb = j & 1 ? bf16_hi(kb[j / 2]) : bf16_lo(kb[j / 2]);
+          s[h][0] = j ? fmaf(fa, d[0], s[h][0]) : fa * d[0];
+          s[h][1] = j ? fmaf(fa, d[1], s[h][1]) : fa * d[1];
+          s[h][2] = j ? fmaf(fb, d[2], s[h][2]) : fb * d[2];
+          s[h][3] = j ? fmaf(fb, d[3], s[h][3]) : fb * d[3];
+        }
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          s[h][k] *= factor[k & 1];
+          if (!whole && !(sight[k & 1] >> (16 * h + 8 * (k >> 1) + g) & 1u)) s[h][k] = -INFINITY;
+        }
+      }
+      // the running maximum moves when it is passed by more than a factor of two
+      float top[2];
+#pragma unroll
+      for (int c = 0; c < 2; ++c) top[c] = max_quads(fmaxf(fmaxf(s[0][c], s[0][c + 2]), fmaxf(s[1][c], s[1][c + 2])));
+      if (__any_sync(0xffffffffu, top[0] > m[0] + 1.f || top[1] > m[1] + 1.f)) {
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+          const float mn = fmaxf(m[c], top[c]);
+          const float f = mn == -INFINITY ? 1.f : ex2(m[c] - mn);
+          m[c] = mn;
+          l[c] *= f;
+#pragma unroll
+          for (int j = 0; j < J; ++j)
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+              o[j][k][c] *= f;
+              o[j][k][c + 2] *= f;
+            }
+        }
+      }
+      const float ref[2] = {m[0] == -INFINITY ? 0.f : m[0], m[1] == -INFINITY ? 0.f : m[1]};
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        // weights as pairs of bf16 numbers, positions 2 t, 2 t + 1 and those + 8 of the operand's column
+        uint32_t hi[2], lo[2];
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+          const float w0 = ex2(s[h][2 * x] - ref[0]), w1 = ex2(s[h][2 * x + 1] - ref[1]);
+          l[0] += w0;
+          l[1] += w1;
+          const uint32_t u = pack_bf16x2(w0, w1);
+          hi[x] = transpose8(u);
+          lo[x] = transpose8(pack_bf16x2(w0 - bf16_lo(u), w1 - bf16_hi(u)));
+        }
+        const Words<J> v0 = lds_words<J>(tile + kv4_v_codes(DH) + (((h * 2) * 8 + g) * 4 + t) * J * 4);
+        const Words<J> v1 = lds_words<J>(tile + kv4_v_codes(DH) + (((h * 2 + 1) * 8 + g) * 4 + t) * J * 4);
+        const Words<J> u0 = lds_words<J>(tile + kv4_v_scales(DH) + (8 * h + t) * J * 4);
+        const Words<J> u1 = lds_words<J>(tile + kv4_v_scales(DH) + (8 * h + 4 + t) * J * 4);
+#pragma unroll
+        for (int j = 0; j < J; ++j) {
+          // times the scales: the rounded product, and what it leaves
+          uint32_t ph[2], pl[2];
+#pragma unroll
+          for (int x = 0; x < 2; ++x) {
+            const __nv_bfloat162 u = as_bf16x2(x ? u1.w[j] : u0.w[j]), w = as_bf16x2(hi[x]);
+            const __nv_bfloat162 prod = __hmul2(w, u);
+            ph[x] = bits_of(prod);
+            pl[x] = bits_of(__hfma2(as_bf16x2(lo[x]), u, __hfma2(w, u, __hneg2(prod))));
+            if (odd) {  // what a column does not see does not count, whatever its scale
+              const uint32_t keep = (hi[x] & 0xffffu ? 0xffffu : 0u) | (hi[x] & 0xffff0000u ? 0xffff0000u : 0u);
+              ph[x] &= keep;
+              pl[x] &= keep;
+            }
+          }
+          const uint32_t x = v0.w[j], y = v1.w[j];
+          uint32_t c[4][2];
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            c[k][0] = v_codes(x >> (4 * k));
+            c[k][1] = v_codes(y >> (4 * k));
+          }
+#pragma unroll
+          for (int k = 0; k < 2; ++k) {
+            mma16816_bf16(o[j][k], c[k][0], c[k + 2][0], c[k][1], c[k + 2][1], ph[0], ph[1]);
+            mma16816_bf16(o[j][k], c[k][0], c[k + 2][0], c[k][1], c[k + 2][1], pl[0], pl[1]);
+          }
+        }
+      }
+
+      const bool ended = cur.tile + 1 == cur.span.n;
+      if (ended || i + 1 == n) {
+        // the item's end, or this warp's
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+#pragma unroll
+          for (int off = 4; off <= 16; off <<= 1) l[c] += __shfl_xor_sync(0xffffffffu, l[c], off);
+        }
+        const float inv[2] = {l[0] == 0.f ? 0.f : 1.f / l[0], l[1] == 0.f ? 0.f : 1.f / l[1]};
+        float* part = started ? last_part : first_part;
+        if (started && !ended) {
+          cp_wait<0>();
+          __syncwarp();  // the ring is free
+        }
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+          const int col = 2 * t + c;
+          if (end[c] < 0) continue;
+          if (!(started && ended) && g == 0) {
+            part[p.ncols * DH + 2 * col] = m[c];
+            part[p.ncols * DH + 2 * col + 1] = l[c];
+          }
+#pragma unroll
+          for (int j = 0; j < J; ++j) {
+            const float4 x = make_float4(o[j][0][c] * inv[c], o[j][1][c] * inv[c], o[j][0][c + 2] * inv[c],
+                                         o[j][1][c + 2] * inv[c]);
+            if (started && ended) store_out(p, cur.slot, cur.head, col0 + col, 32 * j + 4 * g, x);
+            else *reinterpret_cast<float4*>(part + col * DH + 32 * j + 4 * g) = x;
+          }
+        }
+        if (lane == 0 && !started) {
+          w_meta[warp].z = ended ? 2 : 1;
+          w_first[warp] = make_int4(cur.slot, cur.item, cur.head, 0);
+        }
+        if (lane == 0 && started && !ended) {
+          w_meta[warp].x = cur.slot;
+          w_meta[warp].y = cur.item;
+        }
+      }
+      if (i + 1 < n) cursor_next(p, cur);
+    }
+    cp_wait<0>();
+  }
+  __syncthreads();
+
+  // ---- items that several warps share: the warp with an item's last part here puts them together
+  const int last = share > 0 ? static_cast<int>((cta1 - cta0 + share - 1) / share) - 1 : -1;
+  float* out_part = p.part + static_cast<size_t>(blockIdx.x) * 2 * slot_floats;
+  if (tid == 0) {
+    int state = 0;
+    for (int w = 0; w <= last && w_meta[w].z; ++w) {
+      state = w_meta[w].z;
+      if (state == 2 || w_meta[w].x >= 0) break;
+    }
+    // the item that goes on in the next CTA, where it starts here
+    int from = last;
+    while (from > 0 && w_meta[from].x < 0 && w_meta[from].z == 1) --from;
+    p.meta[blockIdx.x] = last < 0 ? make_int4(-1, 0, 0, 0) : make_int4(w_meta[from].x, w_meta[from].y, state, 0);
+  }
+  auto part_of = [&](int w, bool first) {
+    return first ? reinterpret_cast<const float*>(smem + kAttnWarps * (NS * TB)) + w * slot_floats
+                 : reinterpret_cast<const float*>(smem + w * (NS * TB));
+  };
+  if (warp <= last && (w_meta[warp].z == 2 || (w_meta[warp].z == 1 && warp == last))) {
+    const bool ends = w_meta[warp].z == 2;
+    int from = warp;  // first warp with a part
+    bool starts = false;
+    while (from > 0 && !starts) {
+      --from;
+      starts = w_meta[from].x >= 0;
+    }
+    const int4 it = w_first[warp];
+    const int c0 = it.y % p.col_tiles * kCols, cols = min(kCols, a.rows * (a.A / a.c.kv) - c0);
+    for (int col = 0; col < cols; ++col) {
+      float M = -INFINITY, L = 0.f;
+      for (int w = from; w <= warp; ++w) M = fmaxf(M, part_of(w, w > from || !starts)[p.ncols * DH + 2 * col]);
+      float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+      const int d = 4 * lane;
+      for (int w = from; w <= warp; ++w) {
+        const float* x = part_of(w, w > from || !starts);
+        const float f = part_weight(x[p.ncols * DH + 2 * col], x[p.ncols * DH + 2 * col + 1], M);
+        L += f;
+        if (d < DH) add_scaled(o, f, *reinterpret_cast<const float4*>(x + col * DH + d));
+      }
+      const float inv = L == 0.f ? 0.f : 1.f / L;
+      o = make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv);
+      if (starts && ends) {
+        if (d < DH) store_out(p, it.x, it.z, c0 + col, d, o);
+      } else {
+        float* y = out_part + (starts ? slot_floats : 0);
+        if (d < DH) *reinterpret_cast<float4*>(y + col * DH + d) = o;
+        if (lane == 0) {
+          y[p.ncols * DH + 2 * col] = M;
+          y[p.ncols * DH + 2 * col + 1] = L;
+        }
+      }
+    }
+  }
+  if (warp == last && w_meta[warp].x >= 0) {
+    const float* x = part_of(warp, false);
+    for (int i = lane; i < slot_floats; i += 32) out_part[slot_floats + i] = x[i];
+  }
+}
+
+// Items shared by CTAs: block (c, column) puts together the one that starts in CTA c and goes on in others.
+template <int DH>
+__global__ void __launch_bounds__(kMergeThreads) kv4_merge_kernel(AttnParams p, int slot_floats) {
+  constexpr int kWarps = kMergeThreads / 32;
+  __shared__ float weight[kMaxCtas];
+  __shared__ int ends;
+  __shared__ float warp_m[kWarps], warp_l[kWarps];
+  __shared__ float4 sum[kWarps][32];
+  pdl_begin(p.a.late);
+  const int c = blockIdx.x, col = blockIdx.y, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int4 it = p.meta[c];
+  if (it.x < 0) return;
+  const int c0 = it.y % p.col_tiles * kCols;
+  if (c0 + col >= p.a.rows * (p.a.A / p.a.c.kv)) return;
+  if (tid == 0) ends = gridDim.x - 1;
+  __syncthreads();
+  for (int i = c + 1 + tid; i < static_cast<int>(gridDim.x); i += kMergeThreads)
+    if (p.meta[i].z == 2) {
+      atomicMin(&ends, i);
+      break;
+    }
+  __syncthreads();
+  const int n = ends - c + 1;
+  auto part = [&](int i) { return p.part + (static_cast<size_t>(c + i) * 2 + (i == 0)) * slot_floats; };
+  float M = -INFINITY;
+  for (int i = tid; i < n; i += kMergeThreads) M = fmaxf(M, part(i)[p.ncols * DH + 2 * col]);
+#pragma unroll
+  for (int off = 16; off > 0; off >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, off));
+  if (lane == 0) warp_m[warp] = M;
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < kWarps; ++w) M = fmaxf(M, warp_m[w]);
+  for (int i = tid; i < n; i += kMergeThreads) {
+    const float* x = part(i) + p.ncols * DH + 2 * col;
+    weight[i] = part_weight(x[0], x[1], M);
+  }
+  __syncthreads();
+  float L = 0.f;
+  float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+  const int d = 4 * lane;
+#pragma unroll 4
+  for (int i = warp; i < n; i += kWarps) {
+    const float f = weight[i];
+    L += f;
+    if (d < DH) add_scaled(o, f, *reinterpret_cast<const float4*>(part(i) + col * DH + d));
+  }
+  sum[warp][lane] = o;
+  if (lane == 0) warp_l[warp] = L;
+  __syncthreads();
+  if (warp > 0) return;
+#pragma unroll
+  for (int w = 1; w < kWarps; ++w) {
+    L += warp_l[w];
+    add_scaled(o, 1.f, sum[w][lane]);
+  }
+  const float inv = L == 0.f ? 0.f : 1.f / L;
+  const int head = slot_head(p.a, it.x, it.y / p.col_tiles);
+  if (d < DH) store_out(p, it.x, head, c0 + col, d, make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv));
+}
+
+static int attn_ncols(const Kv4Cache& c, int A, int rows) {
+  const int cols = rows * (A / c.kv);
+  return cols < kCols ? cols : kCols;
+}
+
+size_t kv4_attn_workspace(const Kv4Cache& c, int A, int rows) {
+  const size_t floats = part_floats(attn_ncols(c, A, rows), c.dh);
+  return kMaxCtas * (2 * floats * sizeof(float) + sizeof(int4));
+}
+
+template <int DH, int NS>
+static cudaError_t launch_attn(const AttnParams& p, int slot_floats, int grid, cudaStream_t s) {
+  const int smem = kAttnWarps * (NS * kv4_tile_bytes(DH) + slot_floats * 4);
+  cudaError_t e = cudaFuncSetAttribute(kv4_attn_kernel<DH, NS>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+  if (e != cudaSuccess) return e;
+  e = launch_pdl(kv4_attn_kernel<DH, NS>, dim3(grid), kAttnThreads, smem, s, p, slot_floats);
+  if (e != cudaSuccess) return e;
+  return launch_pdl(kv4_merge_kernel<DH>, dim3(grid, p.ncols), kMergeThreads, 0, s, p, slot_floats);
+}
 
 cudaError_t launch_kv4_attention(const Kv4Attn& a, cudaStream_t s) {
-  const dim3 grid(a.A, a.rows, a.c.n_slots);
-  return a.c.dh == 128 ? launch_pdl(kv4_attn_kernel<128>, grid, kSimpleThreads, 0, s, a)
-                       : launch_pdl(kv4_attn_kernel<64>, grid, kSimpleThreads, 0, s, a);
+  AttnParams p;
+  p.a = a;
+  p.ncols = attn_ncols(a.c, a.A, a.rows);
+  p.col_tiles = (a.rows * (a.A / a.c.kv) + kCols - 1) / kCols;
+  p.min_tiles = 4;
+  const int slot_floats = part_floats(p.ncols, a.c.dh);
+  const int grid = a.num_sms < kMaxCtas ? a.num_sms : kMaxCtas;
+  p.meta = static_cast<int4*>(a.ws);
+  p.part = reinterpret_cast<float*>(p.meta + kMaxCtas);
+  // as many stages as find room beside the parts
+  if (a.c.dh == 64) return launch_attn<64, 4>(p, slot_floats, grid, s);
+  return p.ncols == 1 ? launch_attn<128, 3>(p, slot_floats, grid, s) : launch_attn<128, 2>(p, slot_floats, grid, s);
 }
 
 }  // namespace svl
