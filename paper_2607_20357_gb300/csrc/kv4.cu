@@ -7,42 +7,74 @@
 // (n = 0), and all sixteen codes are used. s is exact in bf16. A group with a value
 // that is not finite gets the scale NaN and reads back as NaN; one whose |e| is
 // under 2^-123 (a subnormal scale) is held as zeros: s = 0, n = 8.
+//
+// Writing and reading move 5 1/8 bytes per value of K and V; both are bound by
+// that. A warp takes the up to eight rows of one KV head that share an aligned
+// group of eight positions (a "quad" of the cache's pairs of rows): its codes of K
+// and of V are 4 * d_head contiguous bytes each, one 16-byte word per lane at
+// d_head 128, and a lane's values are pieces of 16 bytes (K) and 8 bytes (V) of which
+// the lanes of a group cover 64 contiguous ones.
 #include "kv4.cuh"
 
 namespace svl {
 
-// Slot and position of packed row r; false where it is to be skipped.
-struct RowPlace {
-  int sample, slot, pos;
-};
-SVL_DEVINL bool row_place(const Kv4Rows& a, int64_t r, RowPlace& p) {
-  int first;
-  if (a.row_off) {
-    if (r < a.row_off[0] || r >= a.row_off[a.n]) return false;
-    p.sample = find_sample(a.row_off, a.n, static_cast<int>(r));
-    first = a.row_off[p.sample];
-  } else {
-    p.sample = static_cast<int>(r);
-    first = p.sample;
-  }
-  p.slot = p.sample * a.slot_step;
-  const int64_t pos = (a.start ? a.start[p.sample] : 0) + (r - first);
-  p.pos = static_cast<int>(pos < -1 ? -1 : (pos > a.c.max_len ? a.c.max_len : pos));
-  return true;
+constexpr int kRowWarps = 4, kRowThreads = kRowWarps * 32;
+
+// Units of work of a call: one per sample without row_off, else quads, of which
+// sample b has room for row_off[b + 1] / 8 - row_off[b] / 8 + 2 from number
+// row_off[b] / 8 + 2 b on: enough for its rows wherever they start, and known
+// without a sum over the samples.
+__host__ __device__ inline int64_t row_units(int64_t rows, int n, bool ragged) {
+  return ragged ? rows / 8 + 2 * static_cast<int64_t>(n) : n;
 }
 
-// x / s rounded to the nearest integer, of two the even one, exactly. inv is 1 / s in
-// float32, so t = x * inv is off by less than 2^-20 for |x / s| <= 8. x and s are bf16
-// numbers: where x / s is not half an integer it is at least 2^-9 from one, so t
-// rounded to a multiple of 2^-15 (by 384 = 1.5 * 2^8, whose last place that is) is
-// half an integer exactly where x / s is.
+// A unit's place: positions p + i of a slot, p a multiple of 8, for i0 <= i < i1, from packed rows row + i.
+struct Unit {
+  int sample, i0, i1;
+  int64_t p, row;
+};
+SVL_DEVINL bool find_unit(const Kv4Rows& a, int64_t u, int lane, Unit& q) {
+  int64_t first = u, count = 1;
+  q.sample = static_cast<int>(u);
+  if (a.row_off) {
+    // the last sample whose units start at or before u: 32 places at a time
+    int lo = 0, n = a.n;
+    while (n > 1) {
+      const int step = (n + 31) / 32, b = lo + min(lane * step, n - 1);
+      const bool le = a.row_off[b] / 8 + 2 * static_cast<int64_t>(b) <= u;
+      const int hit = 31 - __clz(__ballot_sync(0xffffffffu, le) | 1u);
+      const int at = min(hit * step, n - 1);
+      n = min(step, n - at);
+      lo += at;
+    }
+    q.sample = lo;
+    first = a.row_off[lo];
+    count = a.row_off[lo + 1] - first;
+    u -= first / 8 + 2 * static_cast<int64_t>(lo);
+  } else {
+    u = 0;
+  }
+  const int64_t start = a.start ? a.start[q.sample] : 0;
+  q.p = ((start >> 3) + u) * 8;  // (rounds down)
+  q.row = first + q.p - start;
+  int64_t end = start + count - q.p;
+  if (end > a.rows - q.row) end = a.rows - q.row;
+  q.i0 = static_cast<int>(start > q.p ? start - q.p : 0);
+  q.i1 = static_cast<int>(end < 8 ? end : 8);
+  return first >= 0 && q.i1 > q.i0;
+}
+
+// x / s rounded to the nearest integer, of two the even one, exactly, at most 7. inv is 1 / s in float32, so t = x * inv
+// is off by less than 2^-20 for |x / s| <= 8. x and s are bf16 numbers: where x / s is not half an integer it is at
+// least 2^-9 from one, so t rounded to a multiple of 2^-15 (by 384 = 1.5 * 2^8, whose last place that is) is half an
+// integer exactly where x / s is.
 SVL_DEVINL float kv4_code(float x, float inv) {
   const float t = __fadd_rn(__fadd_rn(__fmul_rn(x, inv), 384.f), -384.f);
-  return fminf(rintf(t), 7.f) + 8.f;
+  return __fadd_rn(__fadd_rn(fminf(t, 7.f), 12582912.f), -12582912.f);  // 1.5 * 2^23: to an integer
 }
 
-// The scale (bf16 bits) of a group with largest value hi and smallest lo, all of them
-// finite or not, and its reciprocal for kv4_code (0: every code is 8).
+// The scale (bf16 bits) of a group whose largest and smallest values are in hi and lo, of which `finite` says whether
+// all were, and its reciprocal for kv4_code (0: every code is 8).
 SVL_DEVINL uint16_t kv4_scale(float hi, float lo, bool finite, float& inv) {
   const float s = (hi >= -lo ? hi : lo) * -0.125f;
   inv = 0.f;
@@ -52,108 +84,231 @@ SVL_DEVINL uint16_t kv4_scale(float hi, float lo, bool finite, float& inv) {
   return __bfloat16_as_ushort(__float2bfloat16_rn(s));
 }
 
-constexpr int kRowThreads = 128;
+SVL_DEVINL __nv_bfloat162 b2(uint32_t u) { return *reinterpret_cast<__nv_bfloat162*>(&u); }
+SVL_DEVINL uint32_t u2(__nv_bfloat162 x) { return *reinterpret_cast<uint32_t*>(&x); }
+SVL_DEVINL bool finite2(uint32_t u) { return (u & 0x7f80u) != 0x7f80u && (u & 0x7f800000u) != 0x7f800000u; }
 
-// One thread per group of a row.
-__global__ void __launch_bounds__(kRowThreads) kv4_write_kernel(Kv4Rows a) {
-  pdl_begin(false);
-  const int dh = a.c.dh, J = dh / 32, per_row = a.c.kv * J;
-  const int64_t i = static_cast<int64_t>(blockIdx.x) * kRowThreads + threadIdx.x;
-  const int64_t r = i / per_row;
-  if (r >= a.rows) return;
-  const int hj = static_cast<int>(i - r * per_row), h = hj / J, j = hj - h * J;
-  RowPlace at;
-  if (!row_place(a, r, at) || at.pos < 0) return;
-  if (at.pos >= a.c.max_len) {
-    if (hj == 0) report(a.status, SVL_DEV_BAD_INDEX);
-    return;
+// Largest and smallest value of a group and whether it is finite, from a lane's N pairs and the lanes that differ from
+// it in the bits FROM .. TO of their number.
+template <int N, int FROM, int TO>
+SVL_DEVINL uint16_t group_scale(const uint32_t* u, float& inv) {
+  __nv_bfloat162 hi = b2(u[0]), lo = hi;
+  bool fine = finite2(u[0]);
+#pragma unroll
+  for (int i = 1; i < N; ++i) {
+    hi = __hmax2(hi, b2(u[i]));
+    lo = __hmin2(lo, b2(u[i]));
+    fine = fine && finite2(u[i]);
   }
-  if (!gate_on(a.gate, at.sample, a.gate.G ? h / (a.c.kv / a.gate.G) : 0)) return;
-  uint8_t* tile = kv4_tile(a.c, at.slot, h, at.pos / kKv4Tile);
-  const int p = at.pos % kKv4Tile;
+  // both in one word: the largest value and the negative of the smallest
+  uint32_t x = u2(__halves2bfloat162(__hmax(__low2bfloat16(hi), __high2bfloat16(hi)),
+                                     __hneg(__hmin(__low2bfloat16(lo), __high2bfloat16(lo)))));
+  if (!fine) x = 0x7f807f80u;  // +inf beats every value (a NaN would not)
 #pragma unroll
-  for (int which = 0; which < 2; ++which) {
-    float x[32];
-    float hi = -INFINITY, lo = INFINITY;
-    bool fine = true;
+  for (int off = FROM; off <= TO; off <<= 1) x = u2(__hmax2(b2(x), b2(__shfl_xor_sync(0xffffffffu, x, off))));
+  const float2 f = __bfloat1622float2(b2(x));
+  return kv4_scale(f.x, -f.y, (x & 0x7f80u) != 0x7f80u, inv);
+}
+
+// Four codes as 16 bits, lowest first.
+SVL_DEVINL uint32_t four_codes(float x0, float x1, float x2, float x3, float inv) {
+  float n = kv4_code(x3, inv);
+  n = fmaf(n, 16.f, kv4_code(x2, inv));
+  n = fmaf(n, 16.f, kv4_code(x1, inv));
+  n = fmaf(n, 16.f, kv4_code(x0, inv));
+  // (each n is 8 less than its code: 8 * (1 + 16 + 256 + 4096))
+  return __float_as_uint(n + (8388608.f + 34952.f)) & 0xffffu;
+}
+SVL_DEVINL uint32_t four_codes2(uint32_t a, uint32_t b, float inv) {
+  const float2 x = unpack_bf16x2(a), y = unpack_bf16x2(b);
+  return four_codes(x.x, x.y, y.x, y.y, inv);
+}
+
+template <int J>
+SVL_DEVINL void store_words(void* p, const uint32_t* w) {
+  if constexpr (J == 4) *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
+  else *reinterpret_cast<uint2*>(p) = make_uint2(w[0], w[1]);
+}
+template <int J>
+SVL_DEVINL void load_words(const void* p, uint32_t* w) {
+  if constexpr (J == 4) {
+    const uint4 u = *reinterpret_cast<const uint4*>(p);
+    w[0] = u.x;
+    w[1] = u.y;
+    w[2] = u.z;
+    w[3] = u.w;
+  } else {
+    const uint2 u = *reinterpret_cast<const uint2*>(p);
+    w[0] = u.x;
+    w[1] = u.y;
+  }
+}
+
+// A warp per (unit, KV head): block (unit, heads). VT: V is given transposed (row r of dimension c at v[c * v_col + r]),
+// as the QKV projection leaves it.
+template <int DH, bool VT>
+__global__ void __launch_bounds__(kRowThreads) kv4_write_kernel(Kv4Rows a) {
+  constexpr int J = DH / 32;
+  pdl_begin(false);
+  const int lane = threadIdx.x & 31, h = blockIdx.y * (blockDim.x / 32) + (threadIdx.x >> 5);
+  Unit q;
+  if (h >= a.c.kv || !find_unit(a, blockIdx.x, lane, q) || q.p < 0) return;
+  if (!gate_on(a.gate, q.sample, a.gate.G ? h / (a.c.kv / a.gate.G) : 0)) return;
+  if (q.p + q.i1 > a.c.max_len) {
+    if (h == 0 && lane == 0) report(a.status, SVL_DEV_BAD_INDEX);
+    if (q.p + q.i0 >= a.c.max_len) return;
+    q.i1 = static_cast<int>(a.c.max_len - q.p);
+  }
+  uint8_t* tile = kv4_tile(a.c, q.sample * a.slot_step, h, static_cast<int>(q.p / kKv4Tile));
+  const int quad = static_cast<int>(q.p % kKv4Tile) / 8;
+  // what the lane converts: of K row lane / 4, dimensions 32 j + 8 t + 0..7; of V rows 2 t and 2 t + 1, 32 j + 4 g + 0..3
+  const int g = lane >> 2, t = lane & 3;
+  const bool row_in = g >= q.i0 && g < q.i1, even = 2 * t >= q.i0 && 2 * t < q.i1, odd = 2 * t + 1 >= q.i0 && 2 * t + 1 < q.i1;
+  uint4 k[J];
+  uint2 v[2][J];
 #pragma unroll
-    for (int d = 0; d < 32; ++d) {
-      const int64_t c = static_cast<int64_t>(h) * dh + 32 * j + d;
-      x[d] = __bfloat162float(which ? a.v[r * a.v_row + c * a.v_col] : a.k[r * a.k_row + c]);
-      fine = fine && isfinite(x[d]);
-      hi = fmaxf(hi, x[d]);
-      lo = fminf(lo, x[d]);
+  for (int j = 0; j < J; ++j) {
+    k[j] = make_uint4(0, 0, 0, 0);
+    if (row_in) k[j] = *reinterpret_cast<const uint4*>(a.k + (q.row + g) * a.k_row + h * DH + 32 * j + 8 * t);
+  }
+#pragma unroll
+  for (int x = 0; x < 2; ++x)
+#pragma unroll
+    for (int j = 0; j < J; ++j) {
+      v[x][j] = make_uint2(0, 0);
+      if (!(x ? odd : even)) continue;
+      const int64_t c = h * DH + 32 * j + 4 * g;
+      if (VT) {
+        uint16_t y[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          y[i] = reinterpret_cast<const uint16_t*>(a.v)[(c + i) * a.v_col + q.row + 2 * t + x];
+        v[x][j] = make_uint2(y[0] | static_cast<uint32_t>(y[1]) << 16, y[2] | static_cast<uint32_t>(y[3]) << 16);
+      } else {
+        v[x][j] = *reinterpret_cast<const uint2*>(a.v + (q.row + 2 * t + x) * a.v_row + c);
+      }
     }
-    float inv;
-    const uint16_t s = kv4_scale(hi, lo, fine, inv);
-    uint32_t w[4] = {0, 0, 0, 0};  // eight nibbles each
+  {
+    uint32_t w4[J];
+    uint16_t s[J];
 #pragma unroll
-    for (int d = 0; d < 32; ++d)
-      w[d / 8] |= static_cast<uint32_t>(inv == 0.f ? 8.f : kv4_code(x[d], inv)) << (4 * (d % 8));
-    if (which == 0) {
+    for (int j = 0; j < J; ++j) {
+      const uint32_t u4[4] = {k[j].x, k[j].y, k[j].z, k[j].w};
+      float inv;
+      s[j] = group_scale<4, 1, 2>(u4, inv);
+      w4[j] = four_codes2(u4[0], u4[1], inv) | four_codes2(u4[2], u4[3], inv) << 16;
+    }
+    if (row_in) {
+      store_words<J>(tile + ((quad * 8 + g) * 4 + t) * J * 4, w4);
+      if (t == 0) {
+        uint32_t* at = reinterpret_cast<uint32_t*>(tile + kv4_k_scales(DH) + (quad * 8 + g) * J * 2);
 #pragma unroll
-      for (int t = 0; t < 4; ++t) reinterpret_cast<uint32_t*>(tile)[(p * 4 + t) * J + j] = w[t];
-      reinterpret_cast<uint16_t*>(tile + kv4_k_scales(dh))[p * J + j] = s;
-    } else {
-      uint16_t* v = reinterpret_cast<uint16_t*>(tile + kv4_v_codes(dh));
+        for (int j = 0; j < J; j += 2) at[j / 2] = s[j] | static_cast<uint32_t>(s[j + 1]) << 16;
+      }
+    }
+  }
+  uint32_t w4[J], s2[J];
 #pragma unroll
-      for (int g = 0; g < 8; ++g)
-        v[((((p / 8) * 8 + g) * 4 + (p % 8) / 2) * J + j) * 2 + (p & 1)] =
-            static_cast<uint16_t>(w[g / 2] >> (16 * (g & 1)));
-      reinterpret_cast<uint16_t*>(tile + kv4_v_scales(dh))[((p / 2) * J + j) * 2 + (p & 1)] = s;
+  for (int j = 0; j < J; ++j) {
+    w4[j] = s2[j] = 0;
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+      const uint32_t u4[2] = {v[x][j].x, v[x][j].y};
+      float inv;
+      s2[j] |= static_cast<uint32_t>(group_scale<2, 4, 16>(u4, inv)) << (16 * x);
+      w4[j] |= four_codes2(u4[0], u4[1], inv) << (16 * x);
+    }
+  }
+  uint8_t* codes = tile + kv4_v_codes(DH) + (quad * 32 + lane) * J * 4;
+  uint8_t* scales = tile + kv4_v_scales(DH) + (quad * 4 + t) * J * 4;
+  if (even && odd) {
+    store_words<J>(codes, w4);
+    if (g == 0) store_words<J>(scales, s2);
+  } else if (even || odd) {  // the other row of the pair stays
+#pragma unroll
+    for (int j = 0; j < J; ++j) {
+      reinterpret_cast<uint16_t*>(codes)[2 * j + odd] = static_cast<uint16_t>(w4[j] >> (16 * odd));
+      if (g == 0) reinterpret_cast<uint16_t*>(scales)[2 * j + odd] = static_cast<uint16_t>(s2[j] >> (16 * odd));
     }
   }
 }
 
-// One thread per group of a row; positions that the cache does not have read as 0.
+// The lowest nibble of each half, less 8, times the halves of s, as bf16 (the product rounded once).
+SVL_DEVINL uint32_t two_values(uint32_t x, uint32_t s) {
+  return u2(__hmul2(__hadd2(b2((x & 0x000f000fu) | 0x43004300u), b2(0xc308c308u)), b2(s)));
+}
+
+// A warp per (unit, KV head), as for writing; positions that the cache does not have read as 0.
+template <int DH>
 __global__ void __launch_bounds__(kRowThreads) kv4_read_kernel(Kv4Rows a) {
+  constexpr int J = DH / 32;
   pdl_begin(false);
-  const int dh = a.c.dh, J = dh / 32, per_row = a.c.kv * J;
-  const int64_t i = static_cast<int64_t>(blockIdx.x) * kRowThreads + threadIdx.x;
-  const int64_t r = i / per_row;
-  if (r >= a.rows) return;
-  const int hj = static_cast<int>(i - r * per_row), h = hj / J, j = hj - h * J;
-  RowPlace at;
-  if (!row_place(a, r, at)) return;
-  const bool in = at.pos >= 0 && at.pos < a.c.max_len;
-  const uint8_t* tile = in ? kv4_tile(a.c, at.slot, h, at.pos / kKv4Tile) : nullptr;
-  const int p = at.pos % kKv4Tile;
+  const int lane = threadIdx.x & 31, h = blockIdx.y * (blockDim.x / 32) + (threadIdx.x >> 5);
+  Unit q;
+  if (h >= a.c.kv || !find_unit(a, blockIdx.x, lane, q)) return;
+  const int g = lane >> 2, t = lane & 3;
+  const bool held = q.p >= 0 && q.p < a.c.max_len;
+  uint32_t k[J], v[J], sk[J / 2], sv[J];
 #pragma unroll
-  for (int which = 0; which < 2; ++which) {
-    uint32_t w[4] = {0, 0, 0, 0};
-    float s = 0.f;
-    if (in && which == 0) {
+  for (int j = 0; j < J; ++j) k[j] = v[j] = sk[j / 2] = sv[j] = 0;
+  if (held) {
+    const uint8_t* tile = kv4_tile(a.c, q.sample * a.slot_step, h, static_cast<int>(q.p / kKv4Tile));
+    const int quad = static_cast<int>(q.p % kKv4Tile) / 8;
+    load_words<J>(tile + (quad * 32 + lane) * J * 4, k);
+    load_words<J>(tile + kv4_v_codes(DH) + (quad * 32 + lane) * J * 4, v);
 #pragma unroll
-      for (int t = 0; t < 4; ++t) w[t] = reinterpret_cast<const uint32_t*>(tile)[(p * 4 + t) * J + j];
-      s = __bfloat162float(reinterpret_cast<const __nv_bfloat16*>(tile + kv4_k_scales(dh))[p * J + j]);
-    } else if (in) {
-      const uint16_t* v = reinterpret_cast<const uint16_t*>(tile + kv4_v_codes(dh));
+    for (int j = 0; j < J / 2; ++j)
+      sk[j] = reinterpret_cast<const uint32_t*>(tile + kv4_k_scales(DH) + (quad * 8 + g) * J * 2)[j];
+    load_words<J>(tile + kv4_v_scales(DH) + (quad * 4 + t) * J * 4, sv);
+  }
+  auto wanted = [&](int i) { return i >= q.i0 && i < q.i1; };
+  auto in = [&](int i) { return held && q.p + i < a.c.max_len; };  // else zeros
+  if (wanted(g)) {
+    __nv_bfloat16* out = a.k_out + (q.row + g) * a.k_row + h * DH + 8 * t;
 #pragma unroll
-      for (int g = 0; g < 8; ++g)
-        w[g / 2] |= static_cast<uint32_t>(v[((((p / 8) * 8 + g) * 4 + (p % 8) / 2) * J + j) * 2 + (p & 1)])
-                    << (16 * (g & 1));
-      s = __bfloat162float(
-          reinterpret_cast<const __nv_bfloat16*>(tile + kv4_v_scales(dh))[((p / 2) * J + j) * 2 + (p & 1)]);
+    for (int j = 0; j < J; ++j) {
+      const uint32_t s = __byte_perm(sk[j / 2], 0, j & 1 ? 0x3232 : 0x1010);
+      uint32_t y[4];  // dimensions i and i + 4
+#pragma unroll
+      for (int i = 0; i < 4; ++i) y[i] = two_values(k[j] >> (4 * i), s);
+      uint4 o = make_uint4(__byte_perm(y[0], y[1], 0x5410), __byte_perm(y[2], y[3], 0x5410),
+                           __byte_perm(y[0], y[1], 0x7632), __byte_perm(y[2], y[3], 0x7632));
+      if (!in(g)) o = make_uint4(0, 0, 0, 0);
+      *reinterpret_cast<uint4*>(out + 32 * j) = o;
     }
-    __nv_bfloat16* out = which ? a.v_out + r * a.v_row : a.k_out + r * a.k_row;
+  }
 #pragma unroll
-    for (int d = 0; d < 32; ++d) {
-      const int n = static_cast<int>(w[d / 8] >> (4 * (d % 8)) & 15u);
-      out[static_cast<int64_t>(h) * dh + 32 * j + d] = __float2bfloat16_rn(s * static_cast<float>(n - 8));
+  for (int j = 0; j < J; ++j) {
+    uint32_t y[4];  // dimension i of rows 2 t and 2 t + 1
+#pragma unroll
+    for (int i = 0; i < 4; ++i) y[i] = two_values(v[j] >> (4 * i), sv[j]);
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+      const int i = 2 * t + x;
+      if (!wanted(i)) continue;
+      const uint32_t pick = x ? 0x7632 : 0x5410;
+      uint2 o = make_uint2(__byte_perm(y[0], y[1], pick), __byte_perm(y[2], y[3], pick));
+      if (!in(i)) o = make_uint2(0, 0);
+      *reinterpret_cast<uint2*>(a.v_out + (q.row + i) * a.v_row + h * DH + 32 * j + 4 * g) = o;
     }
   }
 }
 
 static cudaError_t row_launch(void (*kernel)(Kv4Rows), const Kv4Rows& a, cudaStream_t s) {
-  const int64_t threads = a.rows * a.c.kv * (a.c.dh / 32);
-  const int64_t blocks = (threads + kRowThreads - 1) / kRowThreads;
-  if (blocks > 0x7fffffff) return cudaErrorInvalidConfiguration;
-  if (blocks == 0) return cudaSuccess;
-  return launch_pdl(kernel, dim3(static_cast<unsigned>(blocks)), kRowThreads, 0, s, a);
+  const int64_t units = row_units(a.rows, a.n, a.row_off != nullptr);
+  if (units > 0x7fffffff) return cudaErrorInvalidConfiguration;
+  if (units == 0) return cudaSuccess;
+  const int warps = a.c.kv < kRowWarps ? a.c.kv : kRowWarps;
+  return launch_pdl(kernel, dim3(static_cast<unsigned>(units), (a.c.kv + warps - 1) / warps), warps * 32, 0, s, a);
 }
 
-cudaError_t launch_kv4_write(const Kv4Rows& a, cudaStream_t s) { return row_launch(kv4_write_kernel, a, s); }
-cudaError_t launch_kv4_read(const Kv4Rows& a, cudaStream_t s) { return row_launch(kv4_read_kernel, a, s); }
+cudaError_t launch_kv4_write(const Kv4Rows& a, cudaStream_t s) {
+  if (a.c.dh == 128) return row_launch(a.v_col == 1 ? kv4_write_kernel<128, false> : kv4_write_kernel<128, true>, a, s);
+  return row_launch(a.v_col == 1 ? kv4_write_kernel<64, false> : kv4_write_kernel<64, true>, a, s);
+}
+cudaError_t launch_kv4_read(const Kv4Rows& a, cudaStream_t s) {
+  return row_launch(a.c.dh == 128 ? kv4_read_kernel<128> : kv4_read_kernel<64>, a, s);
+}
 
 __global__ void kv4_lengths_kernel(const int* cu_seqlens, int n, int beams, int* len) {
   pdl_begin(false);
@@ -164,41 +319,59 @@ cudaError_t launch_kv4_lengths(const int* cu_seqlens, int B, int beams, int* len
   return launch_pdl(kv4_lengths_kernel, dim3((B * beams + 127) / 128), 128, 0, s, cu_seqlens, B * beams, beams, len);
 }
 
-// One thread per 16 bytes of a tile, for all slots of a sample: each reads what the
-// moved slots take over before it writes any of them, so the slots change in place
-// whatever the parents are.
-constexpr int kMoveThreads = 128;
+// Reorder: block (part, KV head, layer and sample) moves its part of the bytes that the sample's slots hold of the head
+// from position `from` on, 16 bytes a thread of all slots: each thread reads what the moved slots take over before it
+// writes any of them, so the slots change in place whatever the parents are. Bound by the bytes read and written (the
+// slots that stay are not touched); a slot's bytes of a head are contiguous.
+constexpr int kMoveThreads = 256;
+template <int W>
 __global__ void __launch_bounds__(kMoveThreads) kv4_reorder_kernel(Kv4Reorder a) {
   pdl_begin(false);
-  const int sample = blockIdx.z % (a.c.n_slots / a.W), layer = blockIdx.z / (a.c.n_slots / a.W);
-  const int head = blockIdx.y, tile = blockIdx.x;
-  const int s0 = sample * a.W;
-  int first = a.from ? a.from[sample] : 0;
-  if (tile < (first > 0 ? first : 0) / kKv4Tile) return;
-  const size_t layer_bytes = static_cast<size_t>(a.c.n_slots) * a.c.kv * a.c.tiles * kv4_tile_bytes(a.c.dh);
-  Kv4Cache c = a.c;
-  c.data += layer * layer_bytes;
-  for (int i = threadIdx.x; i < kv4_tile_bytes(c.dh) / 16; i += kMoveThreads) {
-    uint4 got[kKv4MaxBeams];
-    uint32_t moved = 0;
-    for (int w = 0; w < a.W; ++w) {
-      const int p = a.parent[s0 + w];
-      if (p < 0 || p >= a.W) {
-        report(a.status, SVL_DEV_BAD_INDEX);
-        continue;
-      }
-      if (p == w || tile * kKv4Tile >= a.len[s0 + p]) continue;
-      moved |= 1u << w;
-      got[w] = reinterpret_cast<const uint4*>(kv4_tile(c, s0 + p, head, tile))[i];
+  const int samples = a.c.n_slots / a.W, sample = blockIdx.z % samples, layer = blockIdx.z / samples;
+  const int s0 = sample * a.W, TB = kv4_tile_bytes(a.c.dh);
+  const int first = (a.from ? max(a.from[sample], 0) : 0) / kKv4Tile;
+  // of each slot that moves: the parent, and the tiles that it holds
+  int parent[W], end[W], last = first;
+  bool bad = false;
+#pragma unroll
+  for (int w = 0; w < W; ++w) {
+    end[w] = 0;
+    parent[w] = w < a.W ? a.parent[s0 + w] : w;
+    if (parent[w] == w) continue;
+    if (parent[w] < 0 || parent[w] >= a.W) {
+      bad = true;
+      continue;
     }
-    for (int w = 0; w < a.W; ++w)
-      if (moved >> w & 1u) reinterpret_cast<uint4*>(kv4_tile(c, s0 + w, head, tile))[i] = got[w];
+    end[w] = (min(a.len[s0 + parent[w]], a.c.max_len) + kKv4Tile - 1) / kKv4Tile;
+    last = max(last, end[w]);
+  }
+  if (bad && threadIdx.x == 0 && blockIdx.x == 0 && blockIdx.y == 0) report(a.status, SVL_DEV_BAD_INDEX);
+  const int64_t n = static_cast<int64_t>(last - first) * (TB / 16);
+  const size_t slot = static_cast<size_t>(a.c.kv) * a.c.tiles * TB;
+  uint4* base = reinterpret_cast<uint4*>(a.c.data + (static_cast<size_t>(layer) * a.c.n_slots + s0) * slot +
+                                         (static_cast<size_t>(blockIdx.y) * a.c.tiles + first) * TB);
+  for (int64_t i = blockIdx.x * kMoveThreads + threadIdx.x; i < n; i += gridDim.x * kMoveThreads) {
+    const int tile = first + static_cast<int>(i / (TB / 16));
+    uint4 got[W];
+#pragma unroll
+    for (int w = 0; w < W; ++w)
+      if (tile < end[w]) got[w] = base[parent[w] * (slot / 16) + i];
+#pragma unroll
+    for (int w = 0; w < W; ++w)
+      if (tile < end[w]) base[w * (slot / 16) + i] = got[w];
   }
 }
 
+// Parts of at least 4 KB (a step of a block), as many as give each SM eight blocks.
 cudaError_t launch_kv4_reorder(const Kv4Reorder& a, cudaStream_t s) {
-  const dim3 grid(a.c.tiles, a.c.kv, a.c.n_slots / a.W * a.layers);
-  return launch_pdl(kv4_reorder_kernel, grid, kMoveThreads, 0, s, a);
+  const int64_t heads = static_cast<int64_t>(a.c.kv) * a.layers * (a.c.n_slots / a.W);
+  const int64_t steps = (static_cast<int64_t>(a.c.tiles) * kv4_tile_bytes(a.c.dh) / 16 + kMoveThreads - 1) / kMoveThreads;
+  int64_t parts = (8 * 152 + heads - 1) / heads;
+  parts = parts < steps ? parts : steps;
+  const dim3 grid(static_cast<unsigned>(parts), a.c.kv, a.c.n_slots / a.W * a.layers);
+  if (a.W <= 4) return launch_pdl(kv4_reorder_kernel<4>, grid, kMoveThreads, 0, s, a);
+  if (a.W <= 8) return launch_pdl(kv4_reorder_kernel<8>, grid, kMoveThreads, 0, s, a);
+  return launch_pdl(kv4_reorder_kernel<16>, grid, kMoveThreads, 0, s, a);
 }
 
 }  // namespace svl
