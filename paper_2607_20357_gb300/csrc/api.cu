@@ -1700,7 +1700,7 @@ svl_status svl_kv4_attention(const svl_kv4_desc* desc, const void* cache, int32_
 
 size_t svl_beam_select_workspace_size(int32_t n_samples, int32_t beams, int32_t vocab, int32_t take) {
   if (n_samples <= 0 || beams <= 0 || beams > kKv4MaxBeams || vocab <= 0 || take <= 0 || take > kBeamMaxTake ||
-      take > vocab)
+      take > vocab || vocab > (1 << 30) || static_cast<int64_t>(n_samples) * beams > INT32_MAX / 64)
     return 0;
   return beam_workspace(n_samples, beams, vocab, take);
 }
@@ -1713,7 +1713,8 @@ svl_status svl_beam_select(int32_t n_samples, int32_t beams, int32_t vocab, int3
       !parent || !token || eos >= vocab)
     return SVL_ERR_INVALID_ARG;
   if (take > vocab) return SVL_ERR_SHAPE;
-  if (beams > kKv4MaxBeams || take > kBeamMaxTake || static_cast<int64_t>(n_samples) * beams > INT32_MAX / 64)
+  if (beams > kKv4MaxBeams || take > kBeamMaxTake || vocab > (1 << 30) ||
+      static_cast<int64_t>(n_samples) * beams > INT32_MAX / 64)
     return SVL_ERR_UNSUPPORTED;
   const svl_status st = check_ws(ws, ws_bytes, beam_workspace(n_samples, beams, vocab, take));
   if (st != SVL_OK) return st;

@@ -2,135 +2,301 @@
 // the candidate x_wv + (c_w - lse_w) with lse_w = log sum_v exp x_wv; a finished beam
 // offers itself. The best K of a sample's candidates are taken: larger scores first,
 // of equal ones the lower beam's, within a beam the larger logit's, then the lower
-// id's. (A beam's candidates thus come in the order of its logits, so that only its
-// best K can be taken, and they are known before its lse is.)
+// id's. A beam's candidates thus come in the order of its logits: its best K are
+// found in the one pass over the row that also sums the exponentials.
+//
+// Bound by the logits' bytes (4 per id). A row is cut into parts, a block each, so
+// that few rows fill the GPU; every warp keeps the K best of what it has seen as a
+// sorted list, one key per lane, and a chunk of 512 logits costs it 16 comparisons per
+// lane and a vote unless one of them passes the list's last key (K ln(n / K) times
+// for n logits in any order that is not ascending). Sums of exponentials are kept
+// per lane relative to the running maximum, in two float32 numbers. A second launch
+// joins the parts, a warp per beam, and takes the sample's best.
 #include "kv4.cuh"
 
 namespace svl {
 
-constexpr int kBeamThreads = 512;
+constexpr int kBeamWarps = 8, kBeamThreads = kBeamWarps * 32;
+constexpr int kChunk = 512;         // logits of a warp's step: 16 per lane
+constexpr int kBeamParts = 64;      // most parts of a row
 
-// Orders floats as unsigned integers, -0 like 0 (NaN: see the callers).
+// Orders floats as unsigned integers, -0 like 0.
 SVL_DEVINL uint32_t order_bits(float x) {
   const uint32_t u = __float_as_uint(x + 0.f);
   return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
 SVL_DEVINL float from_order_bits(uint32_t k) { return __uint_as_float(k & 0x80000000u ? k & 0x7fffffffu : ~k); }
 
-// Logit and id as one number: the larger is the better candidate.
+// Logit and id as one number, never 0: the larger is the better candidate.
 SVL_DEVINL uint64_t beam_key(float x, int v) {
   return static_cast<uint64_t>(order_bits(x)) << 32 | (0xffffffffu - static_cast<uint32_t>(v));
 }
 
-SVL_DEVINL uint64_t block_max(uint64_t x, uint64_t* red) {
-#pragma unroll
-  for (int off = 16; off > 0; off >>= 1) {
-    const uint64_t y = __shfl_xor_sync(0xffffffffu, x, off);
-    x = y > x ? y : x;
+// The keys that pass into a warp's list (lane i: the i-th best so far, 0 where there are fewer; lanes from K on
+// hold keys that fell out).
+SVL_DEVINL void list_insert(uint64_t& list, uint64_t key, bool pass, int K, int lane) {
+  uint32_t left = __ballot_sync(0xffffffffu, pass);
+  while (left) {
+    const int src = __ffs(left) - 1;
+    left &= left - 1;
+    const uint64_t x = __shfl_sync(0xffffffffu, key, src);
+    const int pos = __popc(__ballot_sync(0xffffffffu, list > x));
+    const uint64_t up = __shfl_up_sync(0xffffffffu, list, 1);
+    list = lane < pos ? list : (lane == pos ? x : up);
+    // those that still pass
+    const uint64_t last = __shfl_sync(0xffffffffu, list, K - 1);
+    left &= __ballot_sync(0xffffffffu, key > last);
   }
-  if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = x;
-  __syncthreads();
-  x = red[0];
-  for (int i = 1; i < kBeamThreads / 32; ++i) x = red[i] > x ? red[i] : x;
-  __syncthreads();
+}
+
+// 32 keys in descending order over the lanes (bitonic).
+SVL_DEVINL uint64_t warp_sort(uint64_t x, int lane) {
+#pragma unroll
+  for (int size = 2; size <= 32; size <<= 1)
+#pragma unroll
+    for (int step = size >> 1; step > 0; step >>= 1) {
+      const uint64_t y = __shfl_xor_sync(0xffffffffu, x, step);
+      const bool large = ((lane & step) == 0) == ((lane & size) == 0);
+      x = (x > y) == large ? x : y;
+    }
   return x;
 }
 
-// The K best candidates of each beam: keys [S * W][K] and the beam's offset c_w - lse_w.
-__global__ void __launch_bounds__(kBeamThreads) beam_row_kernel(BeamArgs a, uint64_t* keys, float* offset) {
-  __shared__ uint64_t red[kBeamThreads / 32];
-  __shared__ double sums[kBeamThreads / 32];
+// s + t = a + b exactly
+SVL_DEVINL void two_sum(float a, float b, float& s, float& t) {
+  s = __fadd_rn(a, b);
+  const float z = __fadd_rn(s, -a);
+  t = __fadd_rn(__fadd_rn(a, -__fadd_rn(s, -z)), __fadd_rn(b, -z));
+}
+
+// exp(x - m); m = -inf: 0
+SVL_DEVINL float exp_less(float x, float m) {
+  return ex2((x - (m == -INFINITY ? 0.f : m)) * 1.4426950408889634f);
+}
+
+// The parts of a row: their K best keys [parts][K] and sums {m, sum exp(x - m)} (the sum NaN where a logit is NaN or inf).
+struct BeamParts {
+  uint64_t* keys;
+  float2* sums;
+  int parts, part;  // parts of a row, logits of a part (a multiple of kChunk)
+};
+
+// Block (row, part). VEC: rows are 16-byte aligned.
+template <bool VEC>
+__global__ void __launch_bounds__(kBeamThreads) beam_part_kernel(BeamArgs a, BeamParts p) {
+  __shared__ uint64_t lists[kBeamWarps][kBeamMaxTake];
+  __shared__ float wm[kBeamWarps], ws[kBeamWarps];
   pdl_begin(false);
-  const int row = blockIdx.x, tid = threadIdx.x;
+  const int row = blockIdx.x, part = blockIdx.y, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   if (a.finished && a.finished[row]) return;
   const float* x = a.logits + row * a.ld;
-  float m = -INFINITY;
-  bool nan = false;
-  for (int v = tid; v < a.V; v += kBeamThreads) {
-    nan |= isnan(x[v]);
-    m = fmaxf(m, x[v]);
-  }
-  nan = __syncthreads_or(nan);
-  m = from_order_bits(static_cast<uint32_t>(block_max(static_cast<uint64_t>(order_bits(m)), red)));
-  const bool alive = !nan && isfinite(m);
-  if (alive) {
-    double sum = 0;
-    for (int v = tid; v < a.V; v += kBeamThreads) sum += expf(x[v] - m);
+  const int v0 = part * p.part, v1 = min(a.V, v0 + p.part);
+  float m = -INFINITY, s = 0.f, rest = 0.f;
+  uint64_t list = 0, last = 0;  // last: the list's K-th key, in every lane
+  bool first = true;
+  // lane l's k-th value of the chunk at c: id c + 128 (k / 4) + 4 l + k % 4, or c + 32 k + l where rows are not aligned
+  auto load = [&](int c, float* y) {
 #pragma unroll
-    for (int off = 16; off > 0; off >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, off);
-    if ((tid & 31) == 0) sums[tid >> 5] = sum;
-    __syncthreads();
-    if (tid == 0) {
-      for (int i = 1; i < kBeamThreads / 32; ++i) sum += sums[i];
-      offset[row] = a.scores[row] - static_cast<float>(m + log(sum));
-    }
-  } else if (tid == 0) {
-    offset[row] = -INFINITY;
-  }
-  uint64_t last = ~0ull;
-  for (int k = 0; k < a.K; ++k) {
-    uint64_t best = 0;
-    for (int v = tid; v < a.V; v += kBeamThreads) {
-      const uint64_t key = beam_key(alive ? x[v] : 0.f, v);
-      if (key < last && key > best) best = key;
-    }
-    last = block_max(best, red);
-    if (tid == 0) keys[static_cast<int64_t>(row) * a.K + k] = last;
-  }
-}
-
-// Merges a sample's beams: one thread walks the heads of their lists.
-__global__ void beam_merge_kernel(BeamArgs a, const uint64_t* keys, const float* offset) {
-  pdl_begin(false);
-  const int s = blockIdx.x * blockDim.x + threadIdx.x;
-  if (s >= a.S) return;
-  int at[kKv4MaxBeams];
-  for (int w = 0; w < a.W; ++w) at[w] = 0;
-  for (int k = 0; k < a.K; ++k) {
-    float best = 0.f;
-    int bw = -1, bt = 0;
-    bool bf = false;
-    for (int w = 0; w < a.W; ++w) {
-      if (at[w] >= a.K) continue;
-      const int row = s * a.W + w;
-      const bool done = a.finished && a.finished[row];
-      float c;
-      int t = a.eos;
-      if (done) {
-        c = at[w] == 0 ? a.scores[row] : -INFINITY;
+    for (int k = 0; k < 16; k += 4) {
+      if (VEC) {
+        const int v = c + 32 * k + 4 * lane;
+        if (v + 4 <= v1) {
+          const float4 f = *reinterpret_cast<const float4*>(x + v);
+          y[k] = f.x;
+          y[k + 1] = f.y;
+          y[k + 2] = f.z;
+          y[k + 3] = f.w;
+        } else {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) y[k + i] = v + i < v1 ? x[v + i] : -INFINITY;
+        }
       } else {
-        const uint64_t key = keys[static_cast<int64_t>(row) * a.K + at[w]];
-        t = static_cast<int>(0xffffffffu - static_cast<uint32_t>(key));
-        c = from_order_bits(static_cast<uint32_t>(key >> 32)) + offset[row];
-      }
-      if (isnan(c)) c = -INFINITY;
-      if (bw < 0 || c > best) {
-        best = c;
-        bw = w;
-        bt = t;
-        bf = done;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) y[k + i] = c + 32 * (k + i) + lane < v1 ? x[c + 32 * (k + i) + lane] : -INFINITY;
       }
     }
-    ++at[bw];
-    const int64_t o = static_cast<int64_t>(s) * a.K + k;
-    a.scores_out[o] = best;
-    a.parent[o] = bw;
-    a.token[o] = bt;
-    if (a.finished_out) a.finished_out[o] = bf || bt == a.eos;
+  };
+  float y[16];
+  int c = v0 + warp * kChunk;
+  if (c < v1) load(c, y);
+  for (; c < v1; c += kBeamWarps * kChunk) {
+    float z[16];
+    const int next = c + kBeamWarps * kChunk;
+#pragma unroll
+    for (int k = 0; k < 16; ++k) z[k] = y[k];
+    if (next < v1) load(next, y);
+    float top = z[0];
+#pragma unroll
+    for (int k = 1; k < 16; ++k) top = fmaxf(top, z[k]);
+    if (top > m) {
+      const float f = exp_less(m, top);
+      s *= f;
+      rest *= f;
+      m = top;
+    }
+    float sum = 0.f;
+#pragma unroll
+    for (int k = 0; k < 16; ++k) sum += exp_less(z[k], m);
+    float t;
+    two_sum(s, sum, s, t);
+    rest += t;
+    // (the list's last key has the float `bar`; an equal logit of a higher id does not pass)
+    const float bar = from_order_bits(static_cast<uint32_t>(last >> 32));
+    if (!__any_sync(0xffffffffu, last == 0 || top >= bar)) continue;
+#pragma unroll
+    for (int k = 0; k < 16; ++k) {
+      const int v = VEC ? c + 128 * (k / 4) + 4 * lane + k % 4 : c + 32 * k + lane;
+      const uint64_t key = v < v1 ? beam_key(z[k], v) : 0;
+      if (first) {
+        list = warp_sort(key, lane);
+        first = false;
+      } else if (__any_sync(0xffffffffu, key > last)) {
+        list_insert(list, key, key > last, a.K, lane);
+      } else {
+        continue;
+      }
+      last = __shfl_sync(0xffffffffu, list, a.K - 1);
+    }
+  }
+  // ---- the warp's sums, then the block's
+  s += rest;
+  {
+    float M = m;
+#pragma unroll
+    for (int off = 16; off > 0; off >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, off));
+    s = s * exp_less(m, M);  // (0 times 0 where the lane saw nothing)
+#pragma unroll
+    for (int off = 16; off > 0; off >>= 1) s += __shfl_xor_sync(0xffffffffu, s, off);
+    if (lane == 0) {
+      wm[warp] = M;
+      ws[warp] = s;
+    }
+  }
+  if (lane < a.K) lists[warp][lane] = list;
+  __syncthreads();
+  if (warp > 0) return;
+  if (lane >= a.K) list = 0;
+  last = __shfl_sync(0xffffffffu, list, a.K - 1);
+  for (int w = 1; w < kBeamWarps; ++w) {
+    const uint64_t key = lane < a.K ? lists[w][lane] : 0;
+    if (!__any_sync(0xffffffffu, key > last)) continue;
+    list_insert(list, key, key > last, a.K, lane);
+    last = __shfl_sync(0xffffffffu, list, a.K - 1);
+  }
+  const int64_t at = static_cast<int64_t>(row) * p.parts + part;
+  if (lane < a.K) p.keys[at * a.K + lane] = list;
+  if (lane == 0) {
+    float M = -INFINITY, S = 0.f;
+#pragma unroll
+    for (int w = 0; w < kBeamWarps; ++w) M = fmaxf(M, wm[w]);
+#pragma unroll
+    for (int w = 0; w < kBeamWarps; ++w) S += ws[w] * exp_less(wm[w], M);
+    p.sums[at] = make_float2(M, S);
   }
 }
 
-size_t beam_workspace(int S, int W, int, int K) {
-  const size_t rows = static_cast<size_t>(S) * W;
-  return rows * K * sizeof(uint64_t) + rows * sizeof(float);
+// Block per sample, warp per beam: its parts joined, then the sample's best K taken one by one.
+__global__ void __launch_bounds__(kKv4MaxBeams * 32) beam_join_kernel(BeamArgs a, BeamParts p) {
+  __shared__ float cand[kKv4MaxBeams][kBeamMaxTake];
+  __shared__ int token[kKv4MaxBeams][kBeamMaxTake];
+  __shared__ uint8_t done[kKv4MaxBeams];
+  pdl_begin(false);
+  const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
+  const int row = blockIdx.x * a.W + w;
+  const float score = a.scores[row];
+  const bool fin = a.finished && a.finished[row];
+  if (lane == 0) done[w] = fin;
+  float c = -INFINITY;
+  int id = a.eos;
+  if (fin) {
+    if (lane == 0) c = score;
+  } else {
+    const float2* sums = p.sums + static_cast<int64_t>(row) * p.parts;
+    const uint64_t* keys = p.keys + static_cast<int64_t>(row) * p.parts * a.K;
+    uint64_t list = lane < a.K ? keys[lane] : 0;
+    float M = -INFINITY;
+    for (int i = lane; i < p.parts; i += 32) M = fmaxf(M, sums[i].x);
+#pragma unroll
+    for (int off = 16; off > 0; off >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, off));
+    double S = 0;
+    for (int i = lane; i < p.parts; i += 32) {
+      const float2 x = sums[i];
+      S += static_cast<double>(x.y) * exp_less(x.x, M);
+    }
+#pragma unroll
+    for (int off = 16; off > 0; off >>= 1) S += __shfl_xor_sync(0xffffffffu, S, off);
+    const bool alive = S > 0 && M < INFINITY;  // (a NaN sum is not)
+    uint64_t last = __shfl_sync(0xffffffffu, list, a.K - 1);
+#pragma unroll 4
+    for (int i = 1; i < p.parts; ++i) {
+      const uint64_t key = lane < a.K ? keys[static_cast<int64_t>(i) * a.K + lane] : 0;
+      if (!__any_sync(0xffffffffu, key > last)) continue;
+      list_insert(list, key, key > last, a.K, lane);
+      last = __shfl_sync(0xffffffffu, list, a.K - 1);
+    }
+    id = lane;
+    if (alive) {
+      const float lse = static_cast<float>(M + log(S));
+      id = static_cast<int>(0xffffffffu - static_cast<uint32_t>(list));
+      c = from_order_bits(static_cast<uint32_t>(list >> 32)) + (score - lse);
+    }
+  }
+  if (isnan(c)) c = -INFINITY;
+  if (lane < a.K) {
+    cand[w][lane] = c;
+    token[w][lane] = id;
+  }
+  __syncthreads();
+  if (w > 0) return;
+  // lane = beam, with the best candidate that is left of it
+  int at = 0;
+  const bool beam = lane < a.W;
+  uint32_t mine = beam ? order_bits(cand[lane][0]) : 0;
+  for (int k = 0; k < a.K; ++k) {
+    const uint32_t best = __reduce_max_sync(0xffffffffu, mine);
+    const int from = __ffs(__ballot_sync(0xffffffffu, beam && mine == best)) - 1;
+    if (lane == from) {
+      const int64_t o = static_cast<int64_t>(blockIdx.x) * a.K + k;
+      const int t = token[lane][at];
+      a.scores_out[o] = cand[lane][at];
+      a.parent[o] = lane;
+      a.token[o] = t;
+      if (a.finished_out) a.finished_out[o] = done[lane] || t == a.eos;
+      ++at;
+      mine = at < a.K ? order_bits(cand[lane][at]) : 0;
+    }
+  }
+}
+
+// Parts of at least 2,048 logits (a chunk for four warps), as many as give each SM two blocks.
+static BeamParts beam_parts(int S, int W, int V) {
+  BeamParts p{};
+  const int64_t rows = static_cast<int64_t>(S) * W;
+  int64_t parts = (2 * 152 + rows - 1) / rows;
+  const int64_t most = (V + 2047) / 2048;
+  parts = parts < most ? parts : most;
+  parts = parts < kBeamParts ? parts : kBeamParts;
+  const int64_t len = (V + parts - 1) / parts;
+  p.part = static_cast<int>((len + kChunk - 1) / kChunk * kChunk);
+  p.parts = (V - 1) / p.part + 1;
+  return p;
+}
+
+size_t beam_workspace(int S, int W, int V, int K) {
+  const size_t n = static_cast<size_t>(S) * W * beam_parts(S, W, V).parts;
+  return n * K * sizeof(uint64_t) + n * sizeof(float2);
 }
 
 cudaError_t launch_beam_select(const BeamArgs& a, cudaStream_t s) {
-  uint64_t* keys = static_cast<uint64_t*>(a.ws);
-  float* offset = reinterpret_cast<float*>(keys + static_cast<size_t>(a.S) * a.W * a.K);
-  const cudaError_t e = launch_pdl(beam_row_kernel, dim3(a.S * a.W), kBeamThreads, 0, s, a, keys, offset);
+  BeamParts p = beam_parts(a.S, a.W, a.V);
+  p.keys = static_cast<uint64_t*>(a.ws);
+  p.sums = reinterpret_cast<float2*>(p.keys + static_cast<size_t>(a.S) * a.W * p.parts * a.K);
+  const bool vec = (a.ld & 3) == 0 && (reinterpret_cast<uintptr_t>(a.logits) & 15) == 0;
+  const dim3 grid(a.S * a.W, p.parts);
+  const cudaError_t e = vec ? launch_pdl(beam_part_kernel<true>, grid, kBeamThreads, 0, s, a, p)
+                            : launch_pdl(beam_part_kernel<false>, grid, kBeamThreads, 0, s, a, p);
   if (e != cudaSuccess) return e;
-  return launch_pdl(beam_merge_kernel, dim3((a.S + 31) / 32), 32, 0, s, a, keys, static_cast<const float*>(offset));
+  return launch_pdl(beam_join_kernel, dim3(a.S), a.W * 32, 0, s, a, p);
 }
 
 }  // namespace svl
