@@ -16,10 +16,9 @@ namespace svl {
 //                dimensions 32 j + 4 g + 0..3, lowest nibble first
 //   scales of K  [32 rows][J] bf16
 //   scales of V  [16 row pairs][J][2] bf16
-// so that what one lane of a 16 x 8 x 16 matrix instruction needs of K (rows by
-// dimensions) and of V^T (dimensions by rows) is contiguous, and masking a word
-// with 0x000f000f leaves two operand elements side by side: n * 2^-24 in float16
-// (a subnormal number), or n * 2^-20 with 0x00f000f0.
+// so that what one lane of a 16 x 8 matrix instruction needs of K (rows by
+// dimensions) and of V^T (dimensions by rows, two rows side by side) is contiguous
+// and becomes operands by masking.
 constexpr int kKv4Tile = 32;
 __host__ __device__ constexpr int kv4_tile_bytes(int dh) { return 36 * dh; }
 __host__ __device__ constexpr int kv4_v_codes(int dh) { return 16 * dh; }

@@ -7,18 +7,18 @@
 // Bound by the cache's bytes (d_head * 9 / 8 per position and KV head) if a value
 // costs no more than about three instructions' lanes on its way from memory, which
 // is what decides the design:
-//  - The products run on mma.m16n8k16 with 16-bit operands and float32 sums:
-//    S = K q with 16 positions as rows and 8 columns, O^T = V^T P with 16
-//    dimensions as rows. A column is a query head of the KV head or one of its
-//    rows (drafted tokens); up to eight share one pass over the cache. (tcgen05 has
-//    128 rows and takes its operands from shared memory, to which every
-//    dequantised value would have to be written first.)
-//  - K's codes become float16 operands by masking alone (see kv4.cuh): n * 2^-24
-//    and n * 2^-20, both exact; q is scaled by a power of two to fill float16's
-//    range (bf16 has fewer bits, so that it is exact but for elements under 2^-29
-//    of the head's largest), times 2^-4 where it meets the second kind. The -8 of
-//    s * (n - 8) costs nothing: the accumulators start at -8 * sum q of the group.
-//    The scales multiply the 32-dimension partial sums in float32.
+//  - The products run on mma.m16n8 with float32 sums: S = K q with 16 positions as
+//    rows and 8 columns, O^T = V^T P with 16 dimensions as rows. A column is a query
+//    head of the KV head or one of its rows (drafted tokens); up to eight share one
+//    pass over the cache. (tcgen05 has 128 rows and takes its operands from shared
+//    memory, to which every dequantised value would have to be written first.)
+//  - K's codes become float16 operands by masking alone: n * 2^-24 and n * 2^-20
+//    (subnormal numbers), both exact; q is scaled by a power of two to fill
+//    float16's range (bf16 has fewer bits, so that it is exact but for elements
+//    under 2^-29 of the head's largest), times 2^-4 where it meets the second kind.
+//    The -8 of s * (n - 8) costs nothing: the accumulators start at -8 * sum q of the
+//    group. The scales multiply the 32-dimension partial sums in float32. (e4m3
+//    operands would take fewer masks, but mma.sync converts them to float16 first.)
 //  - V's codes become bf16 operands n - 8 (128 + n by masking, less 136; taken off
 //    O at the end instead, the 8 would leave the rounding of sums of 8 s in
 //    dimensions much smaller than their group). Its scales multiply the weights.
@@ -40,7 +40,7 @@
 
 namespace svl {
 
-constexpr int kAttnWarps = 16, kAttnThreads = kAttnWarps * 32;
+constexpr int kAttnWarps = 12, kAttnThreads = kAttnWarps * 32;
 constexpr int kCols = 8;
 constexpr int kMaxCtas = 256;
 constexpr int kMergeThreads = 128;
@@ -134,12 +134,12 @@ SVL_DEVINL void cp_wait() {
 }
 
 // D = A B + C, 16 x 8 x 16, float32 sums, float16 or bf16 operands.
-SVL_DEVINL void mma16816(float* d, uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1,
-                         const float* c) {
+SVL_DEVINL void mma16816_f16(float* d, uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1,
+                             float c0, float c1, float c2, float c3) {
   asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, "
       "{%10, %11, %12, %13};"
       : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
-      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(c[0]), "f"(c[1]), "f"(c[2]), "f"(c[3]));
+      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(c0), "f"(c1), "f"(c2), "f"(c3));
 }
 SVL_DEVINL void mma16816_bf16(float* d, uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
   asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, "
@@ -159,10 +159,10 @@ SVL_DEVINL uint32_t pack_f16x2(float lo, float hi) {
 }
 SVL_DEVINL float bf16_lo(uint32_t u) { return __uint_as_float(u << 16); }
 SVL_DEVINL float bf16_hi(uint32_t u) { return __uint_as_float(u & 0xffff0000u); }
-constexpr uint32_t kLow = 0x000f000fu, kHigh = 0x00f000f0u;
 SVL_DEVINL __nv_bfloat162 as_bf16x2(uint32_t u) { return *reinterpret_cast<__nv_bfloat162*>(&u); }
 SVL_DEVINL uint32_t bits_of(__nv_bfloat162 x) { return *reinterpret_cast<uint32_t*>(&x); }
-// The lowest nibble of each half, less 8, as bf16.
+constexpr uint32_t kLow = 0x000f000fu, kHigh = 0x00f000f0u;
+// The lowest nibble of each half of a word, less 8, as bf16.
 SVL_DEVINL uint32_t v_codes(uint32_t x) {
   return bits_of(__hadd2(as_bf16x2((x & kLow) | 0x43004300u), as_bf16x2(0xc308c308u)));  // 128 + n, -136
 }
@@ -173,7 +173,6 @@ SVL_DEVINL float max_quads(float x) {  // over the eight lanes that share lane %
   return x;
 }
 
-constexpr float kTwo24 = 16777216.f;
 
 template <int J>
 struct Words {
@@ -196,6 +195,47 @@ SVL_DEVINL Words<J> lds_words(const uint8_t* p) {
   return r;
 }
 
+// O^T += V^T P over 16 positions: weights hi + lo of the positions 2 t, 2 t + 1 ([0]) and those + 8 ([1]) of the operand's
+// column, V's words and scales of the same. MASK: a weight of 0 is a position that the column does not see, which
+// does not count whatever its scale.
+template <int J, bool MASK>
+SVL_DEVINL void weighted_rows(float (*o)[2][4], const uint32_t* hi, const uint32_t* lo, const Words<J>& u0,
+                              const Words<J>& u1, const Words<J>& v0, const Words<J>& v1) {
+  uint32_t keep[2];
+  if (MASK) {
+#pragma unroll
+    for (int x = 0; x < 2; ++x)
+      keep[x] = (hi[x] & 0xffffu ? 0xffffu : 0u) | (hi[x] & 0xffff0000u ? 0xffff0000u : 0u);
+  }
+#pragma unroll
+  for (int j = 0; j < J; ++j) {
+    // times the scales: the rounded product, and what it leaves
+    uint32_t ph[2], pl[2];
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+      const __nv_bfloat162 u = as_bf16x2(x ? u1.w[j] : u0.w[j]), w = as_bf16x2(hi[x]);
+      const __nv_bfloat162 prod = __hmul2(w, u);
+      ph[x] = bits_of(prod);
+      pl[x] = bits_of(__hfma2(as_bf16x2(lo[x]), u, __hfma2(w, u, __hneg2(prod))));
+      if (MASK) {
+        ph[x] &= keep[x];
+        pl[x] &= keep[x];
+      }
+    }
+    uint32_t c[4][2];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      c[k][0] = v_codes(v0.w[j] >> (4 * k));
+      c[k][1] = v_codes(v1.w[j] >> (4 * k));
+    }
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      mma16816_bf16(o[j][k], c[k][0], c[k + 2][0], c[k][1], c[k + 2][1], ph[0], ph[1]);
+      mma16816_bf16(o[j][k], c[k][0], c[k + 2][0], c[k][1], c[k + 2][1], pl[0], pl[1]);
+    }
+  }
+}
+
 // Writes four neighbouring output dimensions of column `col` of an item.
 SVL_DEVINL void store_out(const AttnParams& p, int slot, int head, int col, int d, float4 o) {
   const int grp = p.a.A / p.a.c.kv, r = col / grp, h = head * grp + col - r * grp;
@@ -216,7 +256,9 @@ SVL_DEVINL void add_scaled(float4& o, float f, float4 x) {
 // The weight 2^(m - M) l of a part beside the others' maximum M (0: it saw nothing).
 SVL_DEVINL float part_weight(float m, float l, float M) { return l == 0.f ? 0.f : l * ex2(m - M); }
 
-template <int DH, int NS>
+// NS: stages of a warp's ring. NT: 1 for items of up to four columns, 2 for up to eight. Column c is column
+// 2 (c % 4) + c / 4 of the operands, so that a lane's accumulators hold columns t (x = 0) and 4 + t (x = 1).
+template <int DH, int NS, int NT>
 __global__ void __launch_bounds__(kAttnThreads, 1) kv4_attn_kernel(AttnParams p, int slot_floats) {
   constexpr int J = DH / 32, TB = kv4_tile_bytes(DH);
   extern __shared__ __align__(128) uint8_t smem[];  // per warp: ring of NS tiles; then per warp a part
@@ -298,18 +340,11 @@ __global__ void __launch_bounds__(kAttnThreads, 1) kv4_attn_kernel(AttnParams p,
       cp_commit();
     }
     uint32_t q[J][4];
-    float qsum[J][2], factor[2], m[2], l[2], o[J][2][4];
-    int end[2], low[2];
+    float qsum[J][NT], factor[NT], m[NT], l[NT], o[J][2][4];
+    int end[NT], low[NT];
     int col0 = 0;
     bool started = false;
     for (int i = 0; i < n; ++i) {
-      cp_wait<NS - 2>();
-      __syncwarp();  // the tile is here for every lane, and the one before has been read by all
-      if (asked < n) {
-        request(asked % NS);
-        if (++asked < n) cursor_next(p, req);
-      }
-      cp_commit();
       if (i == 0 || cur.tile == 0) {
         // a new item: its columns' queries as operands
         started = cur.tile == 0;
@@ -317,59 +352,59 @@ __global__ void __launch_bounds__(kAttnThreads, 1) kv4_attn_kernel(AttnParams p,
         const int head = cur.head;
         col0 = cur.item % p.col_tiles * kCols;
         const int cols = min(kCols, a.rows * grp - col0);
+        const int col = 4 * (g & 1) + (g >> 1);  // of operand column g
         uint4 raw[J];
-        float big = 0.f;
 #pragma unroll
         for (int j = 0; j < J; ++j) raw[j] = make_uint4(0, 0, 0, 0);
-        if (g < cols) {
-          const int r = (col0 + g) / grp, h = head * grp + col0 + g - r * grp;
+        if (col < cols) {
+          const int r = (col0 + col) / grp, h = head * grp + col0 + col - r * grp;
           const uint4* src = reinterpret_cast<const uint4*>(
               a.q + (static_cast<int64_t>(cur.slot) * a.rows + r) * a.ldq + h * DH + 8 * t);
 #pragma unroll
           for (int j = 0; j < J; ++j) raw[j] = src[4 * j];
         }
+        uint32_t big = 0;  // largest magnitude's bits
 #pragma unroll
         for (int j = 0; j < J; ++j) {
           const uint32_t u[4] = {raw[j].x, raw[j].y, raw[j].z, raw[j].w};
 #pragma unroll
-          for (int k = 0; k < 4; ++k) big = fmaxf(big, fmaxf(fabsf(bf16_lo(u[k])), fabsf(bf16_hi(u[k]))));
+          for (int k = 0; k < 4; ++k) big = max(big, max(u[k] & 0x7fffu, u[k] >> 16 & 0x7fffu));
         }
-        big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, 1));
-        big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, 2));
-        // the largest to [2^14, 2^15)
-        const int eb = min(max(static_cast<int>(__float_as_uint(big) >> 23), 14), 254);
-        const float up = __uint_as_float(static_cast<uint32_t>(268 - eb) << 23);
-        const float f = a.scale * 1.4426950408889634f * 1024.f * __uint_as_float(static_cast<uint32_t>(eb) << 23);
+        big = max(big, __shfl_xor_sync(0xffffffffu, big, 1));
+        big = max(big, __shfl_xor_sync(0xffffffffu, big, 2));
+        // times a power of two that takes it to [2^14, 2^15)
+        const uint32_t eb = min(max(big >> 7, 14u), 254u);
+        const float up = __uint_as_float((268 - eb) << 23), up4 = up * 0.0625f;
+        float f = a.scale * 1.4426950408889634f * 1024.f * __uint_as_float(eb << 23);
+        if (big >= 0x7f80u) f = NAN;  // a q that is not finite
 #pragma unroll
         for (int j = 0; j < J; ++j) {
           const uint32_t u[4] = {raw[j].x, raw[j].y, raw[j].z, raw[j].w};  // dimensions 2 k, 2 k + 1 of the eight
-          q[j][0] = pack_f16x2(bf16_lo(u[0]) * up, bf16_lo(u[2]) * up);                      // 0, 4
-          q[j][1] = pack_f16x2(bf16_lo(u[1]) * up, bf16_lo(u[3]) * up);                      // 2, 6
-          q[j][2] = pack_f16x2(bf16_hi(u[0]) * up * 0.0625f, bf16_hi(u[2]) * up * 0.0625f);  // 1, 5
-          q[j][3] = pack_f16x2(bf16_hi(u[1]) * up * 0.0625f, bf16_hi(u[3]) * up * 0.0625f);  // 3, 7
-          float s = 0.f;
+          q[j][0] = pack_f16x2(bf16_lo(u[0]) * up, bf16_lo(u[2]) * up);      // 0, 4
+          q[j][1] = pack_f16x2(bf16_lo(u[1]) * up, bf16_lo(u[3]) * up);      // 2, 6
+          q[j][2] = pack_f16x2(bf16_hi(u[0]) * up4, bf16_hi(u[2]) * up4);    // 1, 5
+          q[j][3] = pack_f16x2(bf16_hi(u[1]) * up4, bf16_hi(u[3]) * up4);    // 3, 7
+          float sum = 0.f;
 #pragma unroll
           for (int k = 0; k < 4; ++k) {
-            const float2 x = __half22float2(*reinterpret_cast<const __half2*>(&q[j][k]));
-            s += k < 2 ? x.x + x.y : 16.f * (x.x + x.y);
+            const float2 y = __half22float2(*reinterpret_cast<const __half2*>(&q[j][k]));
+            sum += k < 2 ? y.x + y.y : 16.f * (y.x + y.y);
           }
-          s += __shfl_xor_sync(0xffffffffu, s, 1);
-          s += __shfl_xor_sync(0xffffffffu, s, 2);
-          s *= -8.f / kTwo24;
-          // from the operand's columns (lane / 4) to the accumulators' (2 t, 2 t + 1)
-          qsum[j][0] = __shfl_sync(0xffffffffu, s, 8 * t);
-          qsum[j][1] = __shfl_sync(0xffffffffu, s, 8 * t + 4);
-        }
-        factor[0] = __shfl_sync(0xffffffffu, f, 8 * t);
-        factor[1] = __shfl_sync(0xffffffffu, f, 8 * t + 4);
+          sum += __shfl_xor_sync(0xffffffffu, sum, 1);
+          sum += __shfl_xor_sync(0xffffffffu, sum, 2);
+          // (lane 8 t + 4 x holds operand column 2 t + x, whose accumulators are this lane's)
 #pragma unroll
-        for (int c = 0; c < 2; ++c) {
-          const int64_t pos = static_cast<int64_t>(a.start[cur.slot]) + (col0 + 2 * t + c) / grp;
+          for (int x = 0; x < NT; ++x) qsum[j][x] = __shfl_sync(0xffffffffu, sum * (-8.f / 16777216.f), 8 * t + 4 * x);
+        }
+#pragma unroll
+        for (int x = 0; x < NT; ++x) {
+          factor[x] = __shfl_sync(0xffffffffu, f, 8 * t + 4 * x);
+          const int64_t pos = static_cast<int64_t>(a.start[cur.slot]) + (col0 + 4 * x + t) / grp;
           // (-1: no such column)
-          end[c] = 2 * t + c >= cols ? -1 : (pos >= 0 && pos < a.c.max_len ? static_cast<int>(pos) + 1 : 0);
-          low[c] = a.window > 0 && end[c] > a.window ? end[c] - a.window : 0;
-          m[c] = -INFINITY;
-          l[c] = 0.f;
+          end[x] = 4 * x + t >= cols ? -1 : (pos >= 0 && pos < a.c.max_len ? static_cast<int>(pos) + 1 : 0);
+          low[x] = a.window > 0 && end[x] > a.window ? end[x] - a.window : 0;
+          m[x] = -INFINITY;
+          l[x] = 0.f;
         }
 #pragma unroll
         for (int j = 0; j < J; ++j)
@@ -377,13 +412,23 @@ __global__ void __launch_bounds__(kAttnThreads, 1) kv4_attn_kernel(AttnParams p,
           for (int k = 0; k < 8; ++k) o[j][k >> 2][k & 3] = 0.f;
       }
 
+      cp_wait<NS - 2>();
+      __syncwarp();  // the tile is here for every lane, and the one before has been read by all
+      if (asked < n) {
+        request(asked % NS);
+        if (++asked < n) cursor_next(p, req);
+      }
+      cp_commit();
       uint8_t* tile = ring + (i % NS) * TB;
       const int p0 = cursor_tile(cur) * kKv4Tile;
-      uint32_t sight[2];  // of the tile's positions
+      uint32_t sight[NT];  // of the tile's positions
+      bool all = true;
 #pragma unroll
-      for (int c = 0; c < 2; ++c)
-        sight[c] = (bits_below(end[c] - p0) & ~bits_below(low[c] - p0)) | bits_below(min(a.sinks, end[c]) - p0);
-      const bool whole = __all_sync(0xffffffffu, (end[0] < 0 || sight[0] == ~0u) && (end[1] < 0 || sight[1] == ~0u));
+      for (int x = 0; x < NT; ++x) {
+        sight[x] = (bits_below(end[x] - p0) & ~bits_below(low[x] - p0)) | bits_below(min(a.sinks, end[x]) - p0);
+        all = all && (end[x] < 0 || sight[x] == ~0u);
+      }
+      const bool whole = __all_sync(0xffffffffu, all);
 
       // whether a scale of V is not finite (a stored NaN, or what lies where nothing was written)
       bool odd = false;
@@ -394,8 +439,8 @@ __global__ void __launch_bounds__(kAttnThreads, 1) kv4_attn_kernel(AttnParams p,
       }
       odd = __any_sync(0xffffffffu, odd);
 
-      // scores of the tile's 32 positions
-      float s[2][4];
+      // scores of the tile's 32 positions: rows g and g + 8 of both halves
+      float s[2][2][NT];
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
         const Words<J> wa = lds_words<J>(tile + ((16 * h + g) * 4 + t) * J * 4);
@@ -409,121 +454,105 @@ __global__ void __launch_bounds__(kAttnThreads, 1) kv4_attn_kernel(AttnParams p,
         }
 #pragma unroll
         for (int j = 0; j < J; ++j) {
-          const float c0[4] = {qsum[j][0], qsum[j][1], qsum[j][0], qsum[j][1]};
+          const uint32_t u = wa.w[j], v = wb.w[j], u8 = u >> 8, v8 = v >> 8;
           float d[4];
-          const uint32_t x = wa.w[j], y = wb.w[j], x8 = x >> 8, y8 = y >> 8;
-          mma16816(d, x & kLow, y & kLow, x8 & kLow, y8 & kLow, q[j][0], q[j][1], c0);
-          mma16816(d, x & kHigh, y & kHigh, x8 & kHigh, y8 & kHigh, q[j][2], q[j][3], d);
+          constexpr int X = NT - 1;
+          const float c1 = NT == 2 ? qsum[j][X] : 0.f;
+          mma16816_f16(d, u & kLow, v & kLow, u8 & kLow, v8 & kLow, q[j][0], q[j][1], qsum[j][0], c1, qsum[j][0], c1);
+          mma16816_f16(d, u & kHigh, v & kHigh, u8 & kHigh, v8 & kHigh, q[j][2], q[j][3], d[0], d[1], d[2], d[3]);
           const float fa = j & 1 ? bf16_hi(ka[j / 2]) : bf16_lo(ka[j / 2]);
           const float fb = j & 1 ? bf16_hi(kb[j / 2]) : bf16_lo(kb[j / 2]);
-          s[h][0] = j ? fmaf(fa, d[0], s[h][0]) : fa * d[0];
-          s[h][1] = j ? fmaf(fa, d[1], s[h][1]) : fa * d[1];
-          s[h][2] = j ? fmaf(fb, d[2], s[h][2]) : fb * d[2];
-          s[h][3] = j ? fmaf(fb, d[3], s[h][3]) : fb * d[3];
+#pragma unroll
+          for (int x = 0; x < NT; ++x) {
+            s[h][0][x] = j ? fmaf(fa, d[x], s[h][0][x]) : fa * d[x];
+            s[h][1][x] = j ? fmaf(fb, d[x + 2], s[h][1][x]) : fb * d[x + 2];
+          }
         }
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          s[h][k] *= factor[k & 1];
-          if (!whole && !(sight[k & 1] >> (16 * h + 8 * (k >> 1) + g) & 1u)) s[h][k] = -INFINITY;
+        for (int x = 0; x < NT; ++x) {
+          s[h][0][x] *= factor[x];
+          s[h][1][x] *= factor[x];
         }
       }
+      if (!whole) {
+#pragma unroll
+        for (int x = 0; x < NT; ++x)
+#pragma unroll
+          for (int k = 0; k < 4; ++k)
+            if (!(sight[x] >> (8 * k + g) & 1u)) s[k >> 1][k & 1][x] = -INFINITY;
+      }
       // the running maximum moves when it is passed by more than a factor of two
-      float top[2];
+      float top[NT];
+      bool moves = false;
 #pragma unroll
-      for (int c = 0; c < 2; ++c) top[c] = max_quads(fmaxf(fmaxf(s[0][c], s[0][c + 2]), fmaxf(s[1][c], s[1][c + 2])));
-      if (__any_sync(0xffffffffu, top[0] > m[0] + 1.f || top[1] > m[1] + 1.f)) {
+      for (int x = 0; x < NT; ++x) {
+        top[x] = max_quads(fmaxf(fmaxf(s[0][0][x], s[0][1][x]), fmaxf(s[1][0][x], s[1][1][x])));
+        moves |= top[x] > m[x] + 1.f;
+      }
+      if (__any_sync(0xffffffffu, moves)) {
 #pragma unroll
-        for (int c = 0; c < 2; ++c) {
-          const float mn = fmaxf(m[c], top[c]);
-          const float f = mn == -INFINITY ? 1.f : ex2(m[c] - mn);
-          m[c] = mn;
-          l[c] *= f;
+        for (int x = 0; x < NT; ++x) {
+          const float mn = fmaxf(m[x], top[x]);
+          const float f = mn == -INFINITY ? 1.f : ex2(m[x] - mn);
+          m[x] = mn;
+          l[x] *= f;
 #pragma unroll
           for (int j = 0; j < J; ++j)
 #pragma unroll
             for (int k = 0; k < 2; ++k) {
-              o[j][k][c] *= f;
-              o[j][k][c + 2] *= f;
+              o[j][k][x] *= f;
+              o[j][k][x + 2] *= f;
             }
         }
       }
-      const float ref[2] = {m[0] == -INFINITY ? 0.f : m[0], m[1] == -INFINITY ? 0.f : m[1]};
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
         // weights as pairs of bf16 numbers, positions 2 t, 2 t + 1 and those + 8 of the operand's column
         uint32_t hi[2], lo[2];
 #pragma unroll
-        for (int x = 0; x < 2; ++x) {
-          const float w0 = ex2(s[h][2 * x] - ref[0]), w1 = ex2(s[h][2 * x + 1] - ref[1]);
-          l[0] += w0;
-          l[1] += w1;
-          const uint32_t u = pack_bf16x2(w0, w1);
-          hi[x] = transpose8(u);
-          lo[x] = transpose8(pack_bf16x2(w0 - bf16_lo(u), w1 - bf16_hi(u)));
+        for (int r = 0; r < 2; ++r) {
+          float w[2] = {0.f, 0.f};
+#pragma unroll
+          for (int x = 0; x < NT; ++x) {
+            w[x] = ex2(s[h][r][x] - (m[x] == -INFINITY ? 0.f : m[x]));
+            l[x] += w[x];
+          }
+          const uint32_t u = pack_bf16x2(w[0], w[1]);
+          hi[r] = transpose8(u);
+          lo[r] = transpose8(pack_bf16x2(w[0] - bf16_lo(u), w[1] - bf16_hi(u)));
         }
         const Words<J> v0 = lds_words<J>(tile + kv4_v_codes(DH) + (((h * 2) * 8 + g) * 4 + t) * J * 4);
         const Words<J> v1 = lds_words<J>(tile + kv4_v_codes(DH) + (((h * 2 + 1) * 8 + g) * 4 + t) * J * 4);
         const Words<J> u0 = lds_words<J>(tile + kv4_v_scales(DH) + (8 * h + t) * J * 4);
         const Words<J> u1 = lds_words<J>(tile + kv4_v_scales(DH) + (8 * h + 4 + t) * J * 4);
-#pragma unroll
-        for (int j = 0; j < J; ++j) {
-          // times the scales: the rounded product, and what it leaves
-          uint32_t ph[2], pl[2];
-#pragma unroll
-          for (int x = 0; x < 2; ++x) {
-            const __nv_bfloat162 u = as_bf16x2(x ? u1.w[j] : u0.w[j]), w = as_bf16x2(hi[x]);
-            const __nv_bfloat162 prod = __hmul2(w, u);
-            ph[x] = bits_of(prod);
-            pl[x] = bits_of(__hfma2(as_bf16x2(lo[x]), u, __hfma2(w, u, __hneg2(prod))));
-            if (odd) {  // what a column does not see does not count, whatever its scale
-              const uint32_t keep = (hi[x] & 0xffffu ? 0xffffu : 0u) | (hi[x] & 0xffff0000u ? 0xffff0000u : 0u);
-              ph[x] &= keep;
-              pl[x] &= keep;
-            }
-          }
-          const uint32_t x = v0.w[j], y = v1.w[j];
-          uint32_t c[4][2];
-#pragma unroll
-          for (int k = 0; k < 4; ++k) {
-            c[k][0] = v_codes(x >> (4 * k));
-            c[k][1] = v_codes(y >> (4 * k));
-          }
-#pragma unroll
-          for (int k = 0; k < 2; ++k) {
-            mma16816_bf16(o[j][k], c[k][0], c[k + 2][0], c[k][1], c[k + 2][1], ph[0], ph[1]);
-            mma16816_bf16(o[j][k], c[k][0], c[k + 2][0], c[k][1], c[k + 2][1], pl[0], pl[1]);
-          }
-        }
+        if (odd) weighted_rows<J, true>(o, hi, lo, u0, u1, v0, v1);
+        else weighted_rows<J, false>(o, hi, lo, u0, u1, v0, v1);
       }
 
       const bool ended = cur.tile + 1 == cur.span.n;
       if (ended || i + 1 == n) {
         // the item's end, or this warp's
-#pragma unroll
-        for (int c = 0; c < 2; ++c) {
-#pragma unroll
-          for (int off = 4; off <= 16; off <<= 1) l[c] += __shfl_xor_sync(0xffffffffu, l[c], off);
-        }
-        const float inv[2] = {l[0] == 0.f ? 0.f : 1.f / l[0], l[1] == 0.f ? 0.f : 1.f / l[1]};
         float* part = started ? last_part : first_part;
         if (started && !ended) {
           cp_wait<0>();
           __syncwarp();  // the ring is free
         }
 #pragma unroll
-        for (int c = 0; c < 2; ++c) {
-          const int col = 2 * t + c;
-          if (end[c] < 0) continue;
+        for (int x = 0; x < NT; ++x) {
+#pragma unroll
+          for (int off = 4; off <= 16; off <<= 1) l[x] += __shfl_xor_sync(0xffffffffu, l[x], off);
+          if (end[x] < 0) continue;
+          const float inv = l[x] == 0.f ? 0.f : 1.f / l[x];
+          const int col = 4 * x + t;
           if (!(started && ended) && g == 0) {
-            part[p.ncols * DH + 2 * col] = m[c];
-            part[p.ncols * DH + 2 * col + 1] = l[c];
+            part[p.ncols * DH + 2 * col] = m[x];
+            part[p.ncols * DH + 2 * col + 1] = l[x];
           }
 #pragma unroll
           for (int j = 0; j < J; ++j) {
-            const float4 x = make_float4(o[j][0][c] * inv[c], o[j][1][c] * inv[c], o[j][0][c + 2] * inv[c],
-                                         o[j][1][c + 2] * inv[c]);
-            if (started && ended) store_out(p, cur.slot, cur.head, col0 + col, 32 * j + 4 * g, x);
-            else *reinterpret_cast<float4*>(part + col * DH + 32 * j + 4 * g) = x;
+            const float4 y = make_float4(o[j][0][x] * inv, o[j][1][x] * inv, o[j][0][x + 2] * inv, o[j][1][x + 2] * inv);
+            if (started && ended) store_out(p, cur.slot, cur.head, col0 + col, 32 * j + 4 * g, y);
+            else *reinterpret_cast<float4*>(part + col * DH + 32 * j + 4 * g) = y;
           }
         }
         if (lane == 0 && !started) {
@@ -670,12 +699,12 @@ size_t kv4_attn_workspace(const Kv4Cache& c, int A, int rows) {
   return kMaxCtas * (2 * floats * sizeof(float) + sizeof(int4));
 }
 
-template <int DH, int NS>
+template <int DH, int NS, int NT>
 static cudaError_t launch_attn(const AttnParams& p, int slot_floats, int grid, cudaStream_t s) {
   const int smem = kAttnWarps * (NS * kv4_tile_bytes(DH) + slot_floats * 4);
-  cudaError_t e = cudaFuncSetAttribute(kv4_attn_kernel<DH, NS>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+  cudaError_t e = cudaFuncSetAttribute(kv4_attn_kernel<DH, NS, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
   if (e != cudaSuccess) return e;
-  e = launch_pdl(kv4_attn_kernel<DH, NS>, dim3(grid), kAttnThreads, smem, s, p, slot_floats);
+  e = launch_pdl(kv4_attn_kernel<DH, NS, NT>, dim3(grid), kAttnThreads, smem, s, p, slot_floats);
   if (e != cudaSuccess) return e;
   return launch_pdl(kv4_merge_kernel<DH>, dim3(grid, p.ncols), kMergeThreads, 0, s, p, slot_floats);
 }
@@ -691,8 +720,11 @@ cudaError_t launch_kv4_attention(const Kv4Attn& a, cudaStream_t s) {
   p.meta = static_cast<int4*>(a.ws);
   p.part = reinterpret_cast<float*>(p.meta + kMaxCtas);
   // as many stages as find room beside the parts
-  if (a.c.dh == 64) return launch_attn<64, 4>(p, slot_floats, grid, s);
-  return p.ncols == 1 ? launch_attn<128, 3>(p, slot_floats, grid, s) : launch_attn<128, 2>(p, slot_floats, grid, s);
+  if (a.c.dh == 64)
+    return p.ncols <= 4 ? launch_attn<64, 4, 1>(p, slot_floats, grid, s) : launch_attn<64, 4, 2>(p, slot_floats, grid, s);
+  return p.ncols == 1   ? launch_attn<128, 3, 1>(p, slot_floats, grid, s)
+         : p.ncols <= 4 ? launch_attn<128, 2, 1>(p, slot_floats, grid, s)
+                        : launch_attn<128, 2, 2>(p, slot_floats, grid, s);
 }
 
 }  // namespace svl
