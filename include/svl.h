@@ -409,7 +409,7 @@ svl_status svl_kv4_read(const svl_kv4_desc* desc, const void* cache, int64_t row
  * in the cache: both give zeros.
  * Requires 16-byte aligned q, out and cache, ld_q and ld_out multiples of 8 and
  * at least n_heads * d_head, n_heads a multiple of n_kv_heads, window and sinks
- * not negative (else SVL_ERR_INVALID_ARG). Workspace:
+ * not negative (else SVL_ERR_INVALID_ARG), n_heads at most 65,535. Workspace:
  * svl_kv4_attention_workspace_size() bytes, 256-byte aligned. */
 size_t svl_kv4_attention_workspace_size(const svl_kv4_desc* desc, int32_t n_heads, int32_t rows);
 svl_status svl_kv4_attention(const svl_kv4_desc* desc, const void* cache, int32_t n_heads, int32_t rows,

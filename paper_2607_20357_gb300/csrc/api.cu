@@ -1679,7 +1679,10 @@ svl_status svl_kv4_attention(const svl_kv4_desc* desc, const void* cache, int32_
   if (n_heads <= 0 || n_heads % a.c.kv || rows <= 0 || !q || !out || !start || !aligned16(q) || !aligned16(out) ||
       ld_q < cols || ld_out < cols || (ld_q & 7) || (ld_out & 7) || window < 0 || sinks < 0)
     return SVL_ERR_INVALID_ARG;
-  if (rows > kKv4MaxRows) return SVL_ERR_UNSUPPORTED;
+  // (tiles are counted in 32 bits, a KV head's tiles once per eight columns)
+  if (rows > kKv4MaxRows || n_heads > kKv4MaxSlots ||
+      static_cast<double>(a.c.n_slots) * a.c.kv * a.c.tiles * (rows * (n_heads / a.c.kv) / 8 + 1) > 2e9)
+    return SVL_ERR_UNSUPPORTED;
   if ((st = check_ws(ws, ws_bytes, kv4_attn_workspace(a.c, n_heads, rows))) != SVL_OK) return st;
   a.A = n_heads;
   a.rows = rows;

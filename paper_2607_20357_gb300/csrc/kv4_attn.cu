@@ -50,6 +50,7 @@ struct AttnParams {
   int ncols;      // columns of an item: min(8, rows * heads per KV head)
   int col_tiles;  // items per KV head
   int min_tiles;  // least tiles of a CTA that has any
+  float inv_grp;  // 1 / heads per KV head
   float* part;    // [CTAs][2][ncols * (d_head + 2)]: parts of items shared with other CTAs, the one from
                   // the CTA before and the one that the next goes on with
   int4* meta;     // [CTAs]: {slot (-1: none), item} of the latter; whether there is one of the former
@@ -95,33 +96,45 @@ SVL_DEVINL int slot_head(const Kv4Attn& a, int slot, int i) {
   return 0;
 }
 
-// A place in the row of all tiles.
-struct Cursor {
-  int slot, item, tile, items;  // items of the slot
-  int head;                     // KV head of the item
+// A walk over the row of all tiles: where the next tile is, how many the item has left, after how many it goes on behind
+// the sinks.
+struct Walk {
+  const uint8_t* src;
+  int p0, left, jump;
+  int slot, item, items, head, start;
   Span span;
 };
-SVL_DEVINL void cursor_slot(const AttnParams& p, Cursor& c) {
-  c.items = slot_heads(p.a, c.slot) * p.col_tiles;
-  c.span = slot_span(p.a, c.slot);
+// `tile`: of the item
+SVL_DEVINL void walk_item(const AttnParams& p, Walk& w, int tile) {
+  w.head = slot_head(p.a, w.slot, p.col_tiles == 1 ? w.item : w.item / p.col_tiles);
+  const int at = tile < w.span.sink ? tile : w.span.first + tile - w.span.sink;
+  w.left = w.span.n - tile;
+  w.jump = tile < w.span.sink ? w.span.sink - tile : 0;
+  w.p0 = at * kKv4Tile;
+  w.src = kv4_tile(p.a.c, w.slot, w.head, at);
 }
-SVL_DEVINL void cursor_head(const AttnParams& p, Cursor& c) {
-  c.head = slot_head(p.a, c.slot, p.col_tiles == 1 ? c.item : c.item / p.col_tiles);
+SVL_DEVINL void walk_slot(const AttnParams& p, Walk& w) {
+  w.items = slot_heads(p.a, w.slot) * p.col_tiles;
+  w.span = slot_span(p.a, w.slot);
+  w.start = p.a.start[w.slot];
 }
-SVL_DEVINL void cursor_next(const AttnParams& p, Cursor& c) {
-  if (++c.tile < c.span.n) return;
-  c.tile = 0;
-  if (++c.item >= c.items) {
-    c.item = 0;
-    do {
-      if (++c.slot >= p.a.c.n_slots) return;
-      cursor_slot(p, c);
-    } while (c.items == 0);
+// (only while there is a next tile)
+template <int TB>
+SVL_DEVINL void walk_next(const AttnParams& p, Walk& w) {
+  if (--w.left > 0) {
+    const int skip = --w.jump == 0 ? w.span.first - w.span.sink + 1 : 1;
+    w.p0 += skip * kKv4Tile;
+    w.src += static_cast<int64_t>(skip) * TB;
+    return;
   }
-  cursor_head(p, c);
-}
-SVL_DEVINL int cursor_tile(const Cursor& c) {
-  return c.tile < c.span.sink ? c.tile : c.span.first + c.tile - c.span.sink;
+  if (++w.item >= w.items) {
+    w.item = 0;
+    do {
+      ++w.slot;
+      walk_slot(p, w);
+    } while (w.items == 0);
+  }
+  walk_item(p, w, 0);
 }
 
 SVL_DEVINL void cp16(uint32_t smem, const void* gmem) {
@@ -195,7 +208,16 @@ SVL_DEVINL Words<J> lds_words(const uint8_t* p) {
   return r;
 }
 
-// O^T += V^T P over 16 positions: weights hi + lo of the positions 2 t, 2 t + 1 ([0]) and those + 8 ([1]) of the operand's
+// The codes of two words (of pairs of rows 8 apart) as operands, nibble by nibble.
+SVL_DEVINL void v_operands(uint32_t v0, uint32_t v1, uint32_t (*c)[2]) {
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    c[k][0] = v_codes(v0 >> (4 * k));
+    c[k][1] = v_codes(v1 >> (4 * k));
+  }
+}
+
+// O^T += V^T P over 16 positions, up to eight columns: weights hi + lo of the positions 2 t, 2 t + 1 ([0]) and those + 8 ([1]) of the operand's
 // column, V's words and scales of the same. MASK: a weight of 0 is a position that the column does not see, which
 // does not count whatever its scale.
 template <int J, bool MASK>
@@ -223,11 +245,7 @@ SVL_DEVINL void weighted_rows(float (*o)[2][4], const uint32_t* hi, const uint32
       }
     }
     uint32_t c[4][2];
-#pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      c[k][0] = v_codes(v0.w[j] >> (4 * k));
-      c[k][1] = v_codes(v1.w[j] >> (4 * k));
-    }
+    v_operands(v0.w[j], v1.w[j], c);
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
       mma16816_bf16(o[j][k], c[k][0], c[k + 2][0], c[k][1], c[k + 2][1], ph[0], ph[1]);
@@ -236,9 +254,14 @@ SVL_DEVINL void weighted_rows(float (*o)[2][4], const uint32_t* hi, const uint32
   }
 }
 
+// The row of a column, column / heads per KV head (exact: both are under 2^16, and half a column is added).
+SVL_DEVINL int column_row(const AttnParams& p, int col) {
+  return static_cast<int>((static_cast<float>(col) + 0.5f) * p.inv_grp);
+}
+
 // Writes four neighbouring output dimensions of column `col` of an item.
 SVL_DEVINL void store_out(const AttnParams& p, int slot, int head, int col, int d, float4 o) {
-  const int grp = p.a.A / p.a.c.kv, r = col / grp, h = head * grp + col - r * grp;
+  const int grp = p.a.A / p.a.c.kv, r = column_row(p, col), h = head * grp + col - r * grp;
   __nv_bfloat16* out = p.a.out + (static_cast<int64_t>(slot) * p.a.rows + r) * p.a.ldo + h * p.a.c.dh + d;
   *reinterpret_cast<uint2*>(out) = make_uint2(pack_bf16x2(o.x, o.y), pack_bf16x2(o.z, o.w));
 }
@@ -257,14 +280,16 @@ SVL_DEVINL void add_scaled(float4& o, float f, float4 x) {
 SVL_DEVINL float part_weight(float m, float l, float M) { return l == 0.f ? 0.f : l * ex2(m - M); }
 
 // NS: stages of a warp's ring. NT: 1 for items of up to four columns, 2 for up to eight. Column c is column
-// 2 (c % 4) + c / 4 of the operands, so that a lane's accumulators hold columns t (x = 0) and 4 + t (x = 1).
+// 2 (c % 4) + c / 4 of the operands, so that a lane's accumulators hold columns t (x = 0) and 4 + t (x = 1). With NT = 1
+// the other operand column of a pair holds the lower halves of the scaled weights.
 template <int DH, int NS, int NT>
 __global__ void __launch_bounds__(kAttnThreads, 1) kv4_attn_kernel(AttnParams p, int slot_floats) {
   constexpr int J = DH / 32, TB = kv4_tile_bytes(DH);
   extern __shared__ __align__(128) uint8_t smem[];  // per warp: ring of NS tiles; then per warp a part
-  __shared__ int64_t scan[kAttnWarps];
-  __shared__ Cursor at_cursor[kAttnWarps];
-  __shared__ int4 w_meta[kAttnWarps];  // {slot, item of the part in the ring (-1: none), state of the other part, -}
+  __shared__ int warp_sum[kAttnWarps], prefix[kAttnThreads];
+  __shared__ int4 tile_meta[kAttnWarps][NS];   // {first position, bit 0: first tile of its item, bit 1: last; slot, item}
+  __shared__ int2 tile_item[kAttnWarps][NS];   // {KV head, start of the slot}
+  __shared__ int4 w_meta[kAttnWarps];   // {slot, item of the part in the ring (-1: none), state of the other part, -}
   __shared__ int4 w_first[kAttnWarps];  // slot, item and KV head of that other part
   const Kv4Attn& a = p.a;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -276,90 +301,97 @@ __global__ void __launch_bounds__(kAttnThreads, 1) kv4_attn_kernel(AttnParams p,
 
   // ---- this warp's share of all tiles
   const int per = (a.c.n_slots + kAttnThreads - 1) / kAttnThreads;
-  const int s0 = min(tid * per, a.c.n_slots), s1 = min(s0 + per, a.c.n_slots);
-  int64_t mine = 0;
-  for (int s = s0; s < s1; ++s) mine += static_cast<int64_t>(slot_heads(a, s)) * p.col_tiles * slot_span(a, s).n;
-  int64_t incl = mine;
+  {
+    const int s0 = min(tid * per, a.c.n_slots), s1 = min(s0 + per, a.c.n_slots);
+    int incl = 0;
+    for (int s = s0; s < s1; ++s) incl += slot_heads(a, s) * p.col_tiles * slot_span(a, s).n;
 #pragma unroll
-  for (int off = 1; off < 32; off <<= 1) {
-    const int64_t x = __shfl_up_sync(0xffffffffu, incl, off);
-    if (lane >= off) incl += x;
-  }
-  if (lane == 31) scan[warp] = incl;
-  if (tid < kAttnWarps) w_meta[tid] = make_int4(-1, 0, 0, 0);
-  __syncthreads();
-  int64_t total = 0, before = incl - mine;
-  for (int w = 0; w < kAttnWarps; ++w) {
-    if (w < warp) before += scan[w];
-    total += scan[w];
-  }
-  int64_t cta_tiles = (total + gridDim.x - 1) / gridDim.x;
-  if (cta_tiles < p.min_tiles) cta_tiles = p.min_tiles;
-  const int64_t cta0 = min(total, cta_tiles * blockIdx.x), cta1 = min(total, cta0 + cta_tiles);
-  const int64_t share = (cta1 - cta0 + kAttnWarps - 1) / kAttnWarps;
-  // the thread that owns a warp's first tile finds its place
-  for (int w = 0; w < kAttnWarps; ++w) {
-    const int64_t x = cta0 + w * share;
-    if (x < cta1 && x >= before && x < before + mine) {
-      int64_t rest = x - before;
-      Cursor c;
-      for (c.slot = s0;; ++c.slot) {
-        cursor_slot(p, c);
-        const int64_t n = static_cast<int64_t>(c.items) * c.span.n;
-        if (rest < n) break;
-        rest -= n;
-      }
-      c.item = static_cast<int>(rest / c.span.n);
-      c.tile = static_cast<int>(rest - static_cast<int64_t>(c.item) * c.span.n);
-      cursor_head(p, c);
-      at_cursor[w] = c;
+    for (int off = 1; off < 32; off <<= 1) {
+      const int x = __shfl_up_sync(0xffffffffu, incl, off);
+      if (lane >= off) incl += x;
     }
+    prefix[tid] = incl;
+    if (lane == 31) warp_sum[warp] = incl;
+    if (tid < kAttnWarps) w_meta[tid] = make_int4(-1, 0, 0, 0);
   }
   __syncthreads();
-  const int64_t w0 = cta0 + warp * share;
-  const int n = w0 < cta1 ? static_cast<int>(min(share, cta1 - w0)) : 0;
+  int sums = lane < kAttnWarps ? warp_sum[lane] : 0;
+#pragma unroll
+  for (int off = 1; off < 16; off <<= 1) {
+    const int x = __shfl_up_sync(0xffffffffu, sums, off);
+    if (lane >= off) sums += x;
+  }
+  const int total = __shfl_sync(0xffffffffu, sums, kAttnWarps - 1);
+  const int cta_tiles = max((total + static_cast<int>(gridDim.x) - 1) / static_cast<int>(gridDim.x), p.min_tiles);
+  const int cta0 = static_cast<int>(min(static_cast<int64_t>(total), static_cast<int64_t>(cta_tiles) * blockIdx.x));
+  const int cta1 = total - cta0 < cta_tiles ? total : cta0 + cta_tiles;
+  const int share = (cta1 - cta0 + kAttnWarps - 1) / kAttnWarps;
+  const int last = share > 0 ? (cta1 - cta0 - 1) / share : -1;  // last warp with tiles
+  const int w0 = cta0 + warp * share;
+  const int n = warp <= last ? min(share, cta1 - w0) : 0;
 
   // ---- the tiles
   if (n > 0) {
-    Cursor cur = at_cursor[warp], req = cur;
+    Walk req;
+    int asked = 0;
+    {
+      // the thread's share of the slots that holds tile w0, the slot, the item
+      const int wi = __popc(__ballot_sync(0xffffffffu, lane < kAttnWarps && sums <= w0));
+      const int base = wi > 0 ? __shfl_sync(0xffffffffu, sums, wi - 1) : 0;
+      const int li = __popc(__ballot_sync(0xffffffffu, base + prefix[wi * 32 + lane] <= w0));
+      int rest = w0 - base - (li > 0 ? prefix[wi * 32 + li - 1] : 0);
+      req.slot = (wi * 32 + li) * per;
+      for (walk_slot(p, req); rest >= req.items * req.span.n; walk_slot(p, req)) {
+        rest -= req.items * req.span.n;
+        ++req.slot;
+      }
+      req.item = rest / req.span.n;
+      walk_item(p, req, rest - req.item * req.span.n);
+    }
     const uint32_t ring_s = smem_u32(ring);
-    auto request = [&](int stage) {
-      const uint8_t* src = kv4_tile(a.c, req.slot, req.head, cursor_tile(req));
+    int ask_stage = 0;
+    auto request = [&]() {
 #pragma unroll
       for (int i = 0; i < (TB / 16 + 31) / 32; ++i) {
         const int c = i * 32 + lane;
-        if (TB / 16 % 32 == 0 || c < TB / 16) cp16(ring_s + stage * TB + c * 16, src + c * 16);
+        if (TB / 16 % 32 == 0 || c < TB / 16) cp16(ring_s + ask_stage * TB + c * 16, req.src + c * 16);
       }
+      if (lane == 0) {
+        tile_meta[warp][ask_stage] =
+            make_int4(req.p0, (req.left == req.span.n ? 1 : 0) | (req.left == 1 ? 2 : 0), req.slot, req.item);
+        tile_item[warp][ask_stage] = make_int2(req.head, req.start);
+      }
+      ask_stage = ask_stage + 1 == NS ? 0 : ask_stage + 1;
+      if (++asked < n) walk_next<TB>(p, req);
     };
-    int asked = 0;
-    for (; asked < NS - 1; ++asked) {
-      if (asked < n) {
-        request(asked);
-        if (asked + 1 < n) cursor_next(p, req);
-      }
+#pragma unroll
+    for (int k = 0; k < NS - 1; ++k) {
+      if (asked < n) request();
       cp_commit();
     }
+    __syncwarp();
     uint32_t q[J][4];
     float qsum[J][NT], factor[NT], m[NT], l[NT], o[J][2][4];
     int end[NT], low[NT];
-    int col0 = 0;
+    int stage = 0, col0 = 0;
     bool started = false;
     for (int i = 0; i < n; ++i) {
-      if (i == 0 || cur.tile == 0) {
+      const int4 meta = tile_meta[warp][stage];
+      if (i == 0 || (meta.y & 1)) {
         // a new item: its columns' queries as operands
-        started = cur.tile == 0;
+        started = meta.y & 1;
         const int grp = a.A / a.c.kv;
-        const int head = cur.head;
-        col0 = cur.item % p.col_tiles * kCols;
+        const int2 at = tile_item[warp][stage];
+        col0 = p.col_tiles == 1 ? 0 : meta.w % p.col_tiles * kCols;
         const int cols = min(kCols, a.rows * grp - col0);
         const int col = 4 * (g & 1) + (g >> 1);  // of operand column g
         uint4 raw[J];
 #pragma unroll
         for (int j = 0; j < J; ++j) raw[j] = make_uint4(0, 0, 0, 0);
         if (col < cols) {
-          const int r = (col0 + col) / grp, h = head * grp + col0 + col - r * grp;
+          const int r = column_row(p, col0 + col), h = at.x * grp + col0 + col - r * grp;
           const uint4* src = reinterpret_cast<const uint4*>(
-              a.q + (static_cast<int64_t>(cur.slot) * a.rows + r) * a.ldq + h * DH + 8 * t);
+              a.q + (static_cast<int64_t>(meta.z) * a.rows + r) * a.ldq + h * DH + 8 * t);
 #pragma unroll
           for (int j = 0; j < J; ++j) raw[j] = src[4 * j];
         }
@@ -399,7 +431,7 @@ __global__ void __launch_bounds__(kAttnThreads, 1) kv4_attn_kernel(AttnParams p,
 #pragma unroll
         for (int x = 0; x < NT; ++x) {
           factor[x] = __shfl_sync(0xffffffffu, f, 8 * t + 4 * x);
-          const int64_t pos = static_cast<int64_t>(a.start[cur.slot]) + (col0 + 4 * x + t) / grp;
+          const int64_t pos = static_cast<int64_t>(at.y) + column_row(p, col0 + 4 * x + t);
           // (-1: no such column)
           end[x] = 4 * x + t >= cols ? -1 : (pos >= 0 && pos < a.c.max_len ? static_cast<int>(pos) + 1 : 0);
           low[x] = a.window > 0 && end[x] > a.window ? end[x] - a.window : 0;
@@ -414,13 +446,10 @@ __global__ void __launch_bounds__(kAttnThreads, 1) kv4_attn_kernel(AttnParams p,
 
       cp_wait<NS - 2>();
       __syncwarp();  // the tile is here for every lane, and the one before has been read by all
-      if (asked < n) {
-        request(asked % NS);
-        if (++asked < n) cursor_next(p, req);
-      }
+      if (asked < n) request();
       cp_commit();
-      uint8_t* tile = ring + (i % NS) * TB;
-      const int p0 = cursor_tile(cur) * kKv4Tile;
+      uint8_t* tile = ring + stage * TB;
+      const int p0 = meta.x;
       uint32_t sight[NT];  // of the tile's positions
       bool all = true;
 #pragma unroll
@@ -502,36 +531,71 @@ __global__ void __launch_bounds__(kAttnThreads, 1) kv4_attn_kernel(AttnParams p,
             for (int k = 0; k < 2; ++k) {
               o[j][k][x] *= f;
               o[j][k][x + 2] *= f;
+              if (NT == 1) {
+                o[j][k][1] *= f;
+                o[j][k][3] *= f;
+              }
             }
         }
       }
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        // weights as pairs of bf16 numbers, positions 2 t, 2 t + 1 and those + 8 of the operand's column
-        uint32_t hi[2], lo[2];
-#pragma unroll
-        for (int r = 0; r < 2; ++r) {
-          float w[2] = {0.f, 0.f};
-#pragma unroll
-          for (int x = 0; x < NT; ++x) {
-            w[x] = ex2(s[h][r][x] - (m[x] == -INFINITY ? 0.f : m[x]));
-            l[x] += w[x];
-          }
-          const uint32_t u = pack_bf16x2(w[0], w[1]);
-          hi[r] = transpose8(u);
-          lo[r] = transpose8(pack_bf16x2(w[0] - bf16_lo(u), w[1] - bf16_hi(u)));
-        }
         const Words<J> v0 = lds_words<J>(tile + kv4_v_codes(DH) + (((h * 2) * 8 + g) * 4 + t) * J * 4);
         const Words<J> v1 = lds_words<J>(tile + kv4_v_codes(DH) + (((h * 2 + 1) * 8 + g) * 4 + t) * J * 4);
-        const Words<J> u0 = lds_words<J>(tile + kv4_v_scales(DH) + (8 * h + t) * J * 4);
-        const Words<J> u1 = lds_words<J>(tile + kv4_v_scales(DH) + (8 * h + 4 + t) * J * 4);
-        if (odd) weighted_rows<J, true>(o, hi, lo, u0, u1, v0, v1);
-        else weighted_rows<J, false>(o, hi, lo, u0, u1, v0, v1);
+        if constexpr (NT == 1) {
+          float w[2];
+          Words<J> u[2];  // scales of this lane's rows and their neighbours
+#pragma unroll
+          for (int r = 0; r < 2; ++r) {
+            w[r] = ex2(s[h][r][0] - (m[0] == -INFINITY ? 0.f : m[0]));
+            l[0] += w[r];
+            u[r] = lds_words<J>(tile + kv4_v_scales(DH) + (8 * h + 4 * r + (g >> 1)) * J * 4);
+            if (odd && w[r] == 0.f) {  // what a column does not see does not count, whatever its scale
+#pragma unroll
+              for (int j = 0; j < J; ++j) u[r].w[j] = 0;
+            }
+          }
+#pragma unroll
+          for (int j = 0; j < J; ++j) {
+            uint32_t b[2];
+#pragma unroll
+            for (int r = 0; r < 2; ++r) {
+              const float x = w[r] * __uint_as_float(__byte_perm(u[r].w[j], 0, g & 1 ? 0x3244 : 0x1044));
+              const float hi = __uint_as_float(__float_as_uint(x) & 0xffff0000u);
+              b[r] = transpose8(pack_bf16x2(hi, x - hi));
+            }
+            uint32_t c[4][2];
+            v_operands(v0.w[j], v1.w[j], c);
+            mma16816_bf16(o[j][0], c[0][0], c[2][0], c[0][1], c[2][1], b[0], b[1]);
+            mma16816_bf16(o[j][1], c[1][0], c[3][0], c[1][1], c[3][1], b[0], b[1]);
+          }
+        } else {
+          // weights as pairs of bf16 numbers, positions 2 t, 2 t + 1 and those + 8 of the operand's column
+          uint32_t hi[2], lo[2];
+#pragma unroll
+          for (int r = 0; r < 2; ++r) {
+            float w[2];
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {
+              w[x] = ex2(s[h][r][x % NT] - (m[x % NT] == -INFINITY ? 0.f : m[x % NT]));
+              l[x % NT] += w[x];
+            }
+            const uint32_t u = pack_bf16x2(w[0], w[1]);
+            hi[r] = transpose8(u);
+            lo[r] = transpose8(pack_bf16x2(w[0] - bf16_lo(u), w[1] - bf16_hi(u)));
+          }
+          const Words<J> u0 = lds_words<J>(tile + kv4_v_scales(DH) + (8 * h + t) * J * 4);
+          const Words<J> u1 = lds_words<J>(tile + kv4_v_scales(DH) + (8 * h + 4 + t) * J * 4);
+          if (odd) weighted_rows<J, true>(o, hi, lo, u0, u1, v0, v1);
+          else weighted_rows<J, false>(o, hi, lo, u0, u1, v0, v1);
+        }
       }
 
-      const bool ended = cur.tile + 1 == cur.span.n;
+      stage = stage + 1 == NS ? 0 : stage + 1;
+      const bool ended = meta.y & 2;
       if (ended || i + 1 == n) {
         // the item's end, or this warp's
+        const int head = tile_item[warp][stage == 0 ? NS - 1 : stage - 1].x;
         float* part = started ? last_part : first_part;
         if (started && !ended) {
           cp_wait<0>();
@@ -550,71 +614,93 @@ __global__ void __launch_bounds__(kAttnThreads, 1) kv4_attn_kernel(AttnParams p,
           }
 #pragma unroll
           for (int j = 0; j < J; ++j) {
-            const float4 y = make_float4(o[j][0][x] * inv, o[j][1][x] * inv, o[j][0][x + 2] * inv, o[j][1][x + 2] * inv);
-            if (started && ended) store_out(p, cur.slot, cur.head, col0 + col, 32 * j + 4 * g, y);
+            float4 y = make_float4(o[j][0][x], o[j][1][x], o[j][0][x + 2], o[j][1][x + 2]);
+            if (NT == 1) y = make_float4(y.x + o[j][0][1], y.y + o[j][1][1], y.z + o[j][0][3], y.w + o[j][1][3]);
+            y = make_float4(y.x * inv, y.y * inv, y.z * inv, y.w * inv);
+            if (started && ended) store_out(p, meta.z, head, col0 + col, 32 * j + 4 * g, y);
             else *reinterpret_cast<float4*>(part + col * DH + 32 * j + 4 * g) = y;
           }
         }
         if (lane == 0 && !started) {
           w_meta[warp].z = ended ? 2 : 1;
-          w_first[warp] = make_int4(cur.slot, cur.item, cur.head, 0);
+          w_first[warp] = make_int4(meta.z, meta.w, head, 0);
         }
         if (lane == 0 && started && !ended) {
-          w_meta[warp].x = cur.slot;
-          w_meta[warp].y = cur.item;
+          w_meta[warp].x = meta.z;
+          w_meta[warp].y = meta.w;
         }
       }
-      if (i + 1 < n) cursor_next(p, cur);
+      __syncwarp();  // the next tile's meta
     }
     cp_wait<0>();
   }
   __syncthreads();
 
-  // ---- items that several warps share: the warp with an item's last part here puts them together
-  const int last = share > 0 ? static_cast<int>((cta1 - cta0 + share - 1) / share) - 1 : -1;
+  // ---- items that several warps share are put together, (item, column) by (item, column)
   float* out_part = p.part + static_cast<size_t>(blockIdx.x) * 2 * slot_floats;
+  const int4 wm = lane <= last ? w_meta[lane] : make_int4(-1, 0, 0, 0);
+  const uint32_t starts = __ballot_sync(0xffffffffu, wm.x >= 0);    // warps whose ring holds an item's start
+  const uint32_t goes_on = __ballot_sync(0xffffffffu, wm.z == 1);   // warps within an item
+  uint32_t ends = __ballot_sync(0xffffffffu, wm.z == 2);            // warps with an item's end
   if (tid == 0) {
-    int state = 0;
-    for (int w = 0; w <= last && w_meta[w].z; ++w) {
-      state = w_meta[w].z;
-      if (state == 2 || w_meta[w].x >= 0) break;
+    // what other CTAs have to know: the item that goes on in the next one and started here, and whether one from before
+    // ends here (warps 0, 1, ... go on with it until one ends it)
+    const bool before = (goes_on | ends) & 1u;
+    int4 mt = make_int4(-1, 0, before ? (ends && __ffs(ends) - 1 == __ffs(~goes_on) - 1 ? 2 : 1) : 0, 0);
+    if (starts && last >= 0) {
+      const int v = 31 - __clz(starts);
+      if (v == last || !(ends >> v >> 1)) {
+        mt.x = w_meta[v].x;
+        mt.y = w_meta[v].y;
+      }
     }
-    // the item that goes on in the next CTA, where it starts here
-    int from = last;
-    while (from > 0 && w_meta[from].x < 0 && w_meta[from].z == 1) --from;
-    p.meta[blockIdx.x] = last < 0 ? make_int4(-1, 0, 0, 0) : make_int4(w_meta[from].x, w_meta[from].y, state, 0);
+    p.meta[blockIdx.x] = mt;
   }
+  if (last >= 0 && (goes_on >> last & 1u)) ends |= 1u << last;
   auto part_of = [&](int w, bool first) {
     return first ? reinterpret_cast<const float*>(smem + kAttnWarps * (NS * TB)) + w * slot_floats
                  : reinterpret_cast<const float*>(smem + w * (NS * TB));
   };
-  if (warp <= last && (w_meta[warp].z == 2 || (w_meta[warp].z == 1 && warp == last))) {
-    const bool ends = w_meta[warp].z == 2;
-    int from = warp;  // first warp with a part
-    bool starts = false;
-    while (from > 0 && !starts) {
-      --from;
-      starts = w_meta[from].x >= 0;
-    }
-    const int4 it = w_first[warp];
-    const int c0 = it.y % p.col_tiles * kCols, cols = min(kCols, a.rows * (a.A / a.c.kv) - c0);
+  int turn = 0;
+  for (; ends; ends &= ends - 1) {
+    const int to = __ffs(ends) - 1;  // the warp with the item's last part here; its first is the last start before that
+    const uint32_t earlier = starts & ((1u << to) - 1u);
+    const bool here = earlier != 0;
+    const int from = here ? 31 - __clz(earlier) : 0;
+    const bool done = here && !(goes_on >> to & 1u);
+    const int4 it = w_first[to];
+    const int c0 = p.col_tiles == 1 ? 0 : it.y % p.col_tiles * kCols, cols = min(kCols, a.rows * (a.A / a.c.kv) - c0);
     for (int col = 0; col < cols; ++col) {
-      float M = -INFINITY, L = 0.f;
-      for (int w = from; w <= warp; ++w) M = fmaxf(M, part_of(w, w > from || !starts)[p.ncols * DH + 2 * col]);
+      const bool skip = turn != warp;
+      turn = turn + 1 == kAttnWarps ? 0 : turn + 1;
+      if (skip) continue;
+      float m = -INFINITY, l = 0.f;
+      if (lane <= to - from) {
+        const float* x = part_of(from + lane, lane > 0 || !here) + p.ncols * DH + 2 * col;
+        m = x[0];
+        l = x[1];
+      }
+      float M = m;
+#pragma unroll
+      for (int off = 8; off > 0; off >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, off));
+      const float f = part_weight(m, l, M);
+      float L = f;
+#pragma unroll
+      for (int off = 8; off > 0; off >>= 1) L += __shfl_xor_sync(0xffffffffu, L, off);
+      const float inv = L == 0.f ? 0.f : 1.f / L;
+      M = __shfl_sync(0xffffffffu, M, 0);
+      L = __shfl_sync(0xffffffffu, L, 0);
+      const float fi = f * __shfl_sync(0xffffffffu, inv, 0);
       float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
       const int d = 4 * lane;
-      for (int w = from; w <= warp; ++w) {
-        const float* x = part_of(w, w > from || !starts);
-        const float f = part_weight(x[p.ncols * DH + 2 * col], x[p.ncols * DH + 2 * col + 1], M);
-        L += f;
-        if (d < DH) add_scaled(o, f, *reinterpret_cast<const float4*>(x + col * DH + d));
+      for (int w = from; w <= to; ++w) {
+        const float x = __shfl_sync(0xffffffffu, fi, w - from);
+        if (d < DH) add_scaled(o, x, *reinterpret_cast<const float4*>(part_of(w, w > from || !here) + col * DH + d));
       }
-      const float inv = L == 0.f ? 0.f : 1.f / L;
-      o = make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv);
-      if (starts && ends) {
+      if (done) {
         if (d < DH) store_out(p, it.x, it.z, c0 + col, d, o);
       } else {
-        float* y = out_part + (starts ? slot_floats : 0);
+        float* y = out_part + (here ? slot_floats : 0);
         if (d < DH) *reinterpret_cast<float4*>(y + col * DH + d) = o;
         if (lane == 0) {
           y[p.ncols * DH + 2 * col] = M;
@@ -623,70 +709,75 @@ __global__ void __launch_bounds__(kAttnThreads, 1) kv4_attn_kernel(AttnParams p,
       }
     }
   }
-  if (warp == last && w_meta[warp].x >= 0) {
-    const float* x = part_of(warp, false);
-    for (int i = lane; i < slot_floats; i += 32) out_part[slot_floats + i] = x[i];
+  if (last >= 0 && (starts >> last & 1u)) {
+    const float* x = part_of(last, false);
+    for (int i = tid; i < slot_floats; i += kAttnThreads) out_part[slot_floats + i] = x[i];
   }
 }
 
-// Items shared by CTAs: block (c, column) puts together the one that starts in CTA c and goes on in others.
+// Items shared by CTAs: block (c, column) puts together the one that starts in CTA c and goes on in others. The warps take
+// its parts in turn, each with a running maximum, so that what has to be read is on its way at once.
 template <int DH>
 __global__ void __launch_bounds__(kMergeThreads) kv4_merge_kernel(AttnParams p, int slot_floats) {
   constexpr int kWarps = kMergeThreads / 32;
-  __shared__ float weight[kMaxCtas];
-  __shared__ int ends;
+  __shared__ int last;
   __shared__ float warp_m[kWarps], warp_l[kWarps];
   __shared__ float4 sum[kWarps][32];
-  pdl_begin(p.a.late);
   const int c = blockIdx.x, col = blockIdx.y, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  if (tid == 0) last = gridDim.x - 1;
+  pdl_begin(p.a.late);
   const int4 it = p.meta[c];
-  if (it.x < 0) return;
-  const int c0 = it.y % p.col_tiles * kCols;
-  if (c0 + col >= p.a.rows * (p.a.A / p.a.c.kv)) return;
-  if (tid == 0) ends = gridDim.x - 1;
-  __syncthreads();
-  for (int i = c + 1 + tid; i < static_cast<int>(gridDim.x); i += kMergeThreads)
-    if (p.meta[i].z == 2) {
-      atomicMin(&ends, i);
-      break;
-    }
-  __syncthreads();
-  const int n = ends - c + 1;
-  auto part = [&](int i) { return p.part + (static_cast<size_t>(c + i) * 2 + (i == 0)) * slot_floats; };
-  float M = -INFINITY;
-  for (int i = tid; i < n; i += kMergeThreads) M = fmaxf(M, part(i)[p.ncols * DH + 2 * col]);
+  int ends = gridDim.x;  // the first CTA from here on where an item from before ends
 #pragma unroll
-  for (int off = 16; off > 0; off >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, off));
-  if (lane == 0) warp_m[warp] = M;
-  __syncthreads();
-#pragma unroll
-  for (int w = 0; w < kWarps; ++w) M = fmaxf(M, warp_m[w]);
-  for (int i = tid; i < n; i += kMergeThreads) {
-    const float* x = part(i) + p.ncols * DH + 2 * col;
-    weight[i] = part_weight(x[0], x[1], M);
+  for (int i = 0; i < kMaxCtas / kMergeThreads; ++i) {
+    const int at = c + 1 + i * kMergeThreads + tid;
+    if (at < static_cast<int>(gridDim.x) && p.meta[at].z == 2) ends = min(ends, at);
   }
+  if (it.x < 0) return;
+  const int c0 = p.col_tiles == 1 ? 0 : it.y % p.col_tiles * kCols;
+  if (c0 + col >= p.a.rows * (p.a.A / p.a.c.kv)) return;
   __syncthreads();
-  float L = 0.f;
+  ends = __reduce_min_sync(0xffffffffu, ends);
+  if (lane == 0) atomicMin(&last, ends);
+  __syncthreads();
+  const int n = last - c + 1;
+  float m = -INFINITY, l = 0.f;
   float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
   const int d = 4 * lane;
 #pragma unroll 4
   for (int i = warp; i < n; i += kWarps) {
-    const float f = weight[i];
-    L += f;
-    if (d < DH) add_scaled(o, f, *reinterpret_cast<const float4*>(part(i) + col * DH + d));
+    const float* x = p.part + (static_cast<size_t>(c + i) * 2 + (i == 0)) * slot_floats;
+    const float xm = x[p.ncols * DH + 2 * col], xl = x[p.ncols * DH + 2 * col + 1];
+    const float4 y = d < DH ? *reinterpret_cast<const float4*>(x + col * DH + d) : o;
+    const float mn = fmaxf(m, xm), old = part_weight(m, l, mn), f = part_weight(xm, xl, mn);
+    // (o is kept with its weight l: sums of weighted outputs)
+    const float down = l == 0.f ? 0.f : ex2(m - mn);
+    o = make_float4(o.x * down, o.y * down, o.z * down, o.w * down);
+    add_scaled(o, f, y);
+    l = old + f;
+    m = mn;
   }
   sum[warp][lane] = o;
-  if (lane == 0) warp_l[warp] = L;
+  if (lane == 0) {
+    warp_m[warp] = m;
+    warp_l[warp] = l;
+  }
   __syncthreads();
-  if (warp > 0) return;
+  if (warp > 0 || d >= DH) return;
+  float M = -INFINITY, L = 0.f;
 #pragma unroll
-  for (int w = 1; w < kWarps; ++w) {
-    L += warp_l[w];
-    add_scaled(o, 1.f, sum[w][lane]);
+  for (int w = 0; w < kWarps; ++w) M = fmaxf(M, warp_m[w]);
+  o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+  for (int w = 0; w < kWarps; ++w) {
+    if (warp_l[w] == 0.f) continue;
+    const float f = ex2(warp_m[w] - M);
+    L += warp_l[w] * f;
+    add_scaled(o, f, sum[w][lane]);
   }
   const float inv = L == 0.f ? 0.f : 1.f / L;
-  const int head = slot_head(p.a, it.x, it.y / p.col_tiles);
-  if (d < DH) store_out(p, it.x, head, c0 + col, d, make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv));
+  const int head = slot_head(p.a, it.x, p.col_tiles == 1 ? it.y : it.y / p.col_tiles);
+  store_out(p, it.x, head, c0 + col, d, make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv));
 }
 
 static int attn_ncols(const Kv4Cache& c, int A, int rows) {
@@ -715,16 +806,14 @@ cudaError_t launch_kv4_attention(const Kv4Attn& a, cudaStream_t s) {
   p.ncols = attn_ncols(a.c, a.A, a.rows);
   p.col_tiles = (a.rows * (a.A / a.c.kv) + kCols - 1) / kCols;
   p.min_tiles = 4;
+  p.inv_grp = 1.f / static_cast<float>(a.A / a.c.kv);
   const int slot_floats = part_floats(p.ncols, a.c.dh);
   const int grid = a.num_sms < kMaxCtas ? a.num_sms : kMaxCtas;
   p.meta = static_cast<int4*>(a.ws);
   p.part = reinterpret_cast<float*>(p.meta + kMaxCtas);
-  // as many stages as find room beside the parts
   if (a.c.dh == 64)
     return p.ncols <= 4 ? launch_attn<64, 4, 1>(p, slot_floats, grid, s) : launch_attn<64, 4, 2>(p, slot_floats, grid, s);
-  return p.ncols == 1   ? launch_attn<128, 3, 1>(p, slot_floats, grid, s)
-         : p.ncols <= 4 ? launch_attn<128, 2, 1>(p, slot_floats, grid, s)
-                        : launch_attn<128, 2, 2>(p, slot_floats, grid, s);
+  return p.ncols <= 4 ? launch_attn<128, 3, 1>(p, slot_floats, grid, s) : launch_attn<128, 3, 2>(p, slot_floats, grid, s);
 }
 
 }  // namespace svl
