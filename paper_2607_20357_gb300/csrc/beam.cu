@@ -7,11 +7,13 @@
 //
 // Bound by the logits' bytes (4 per id). A row is cut into parts, a block each, so
 // that few rows fill the GPU; every warp keeps the K best of what it has seen as a
-// sorted list, one key per lane, and a chunk of 512 logits costs it 16 comparisons per
-// lane and a vote unless one of them passes the list's last key (K ln(n / K) times
-// for n logits in any order that is not ascending). Sums of exponentials are kept
-// per lane relative to the running maximum, in two float32 numbers. A second launch
-// joins the parts, a warp per beam, and takes the sample's best.
+// sorted list, one key per lane. Few logits ever reach a list: of the warps that a
+// block has, each holds at least K / warps logits that are no less than its bar, so
+// none under the lowest of these bars is among the K best; the bars start from the
+// lanes' maxima of the first chunk. A chunk of 512 logits then costs a warp 16
+// comparisons per lane and a vote. Sums of exponentials are kept per lane relative
+// to the running maximum, in two float32 numbers. A second launch joins the parts,
+// a warp per beam, and takes the sample's best.
 #include "kv4.cuh"
 
 namespace svl {
@@ -49,15 +51,14 @@ SVL_DEVINL void list_insert(uint64_t& list, uint64_t key, bool pass, int K, int 
   }
 }
 
-// 32 keys in descending order over the lanes (bitonic).
-SVL_DEVINL uint64_t warp_sort(uint64_t x, int lane) {
+// 32 numbers in descending order over the lanes (bitonic).
+SVL_DEVINL uint32_t warp_sort(uint32_t x, int lane) {
 #pragma unroll
   for (int size = 2; size <= 32; size <<= 1)
 #pragma unroll
     for (int step = size >> 1; step > 0; step >>= 1) {
-      const uint64_t y = __shfl_xor_sync(0xffffffffu, x, step);
-      const bool large = ((lane & step) == 0) == ((lane & size) == 0);
-      x = (x > y) == large ? x : y;
+      const uint32_t y = __shfl_xor_sync(0xffffffffu, x, step);
+      x = ((lane & step) == 0) == ((lane & size) == 0) ? max(x, y) : min(x, y);
     }
   return x;
 }
@@ -86,6 +87,7 @@ template <bool VEC>
 __global__ void __launch_bounds__(kBeamThreads) beam_part_kernel(BeamArgs a, BeamParts p) {
   __shared__ uint64_t lists[kBeamWarps][kBeamMaxTake];
   __shared__ float wm[kBeamWarps], ws[kBeamWarps];
+  __shared__ volatile uint32_t bars[kBeamWarps];  // of each warp, `each` of its logits are no less (as ordered bits)
   pdl_begin(false);
   const int row = blockIdx.x, part = blockIdx.y, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   if (a.finished && a.finished[row]) return;
@@ -93,7 +95,8 @@ __global__ void __launch_bounds__(kBeamThreads) beam_part_kernel(BeamArgs a, Bea
   const int v0 = part * p.part, v1 = min(a.V, v0 + p.part);
   float m = -INFINITY, s = 0.f, rest = 0.f;
   uint64_t list = 0, last = 0;  // last: the list's K-th key, in every lane
-  bool first = true;
+  const int active = min(kBeamWarps, (v1 - v0 + kChunk - 1) / kChunk), each = (a.K + active - 1) / active;
+  uint32_t own = 0;  // K of this warp's logits are no less
   // lane l's k-th value of the chunk at c: id c + 128 (k / 4) + 4 l + k % 4, or c + 32 k + l where rows are not aligned
   auto load = [&](int c, float* y) {
 #pragma unroll
@@ -118,7 +121,17 @@ __global__ void __launch_bounds__(kBeamThreads) beam_part_kernel(BeamArgs a, Bea
   };
   float y[16];
   int c = v0 + warp * kChunk;
-  if (c < v1) load(c, y);
+  if (c < v1) {
+    load(c, y);
+    float top = y[0];
+#pragma unroll
+    for (int k = 1; k < 16; ++k) top = fmaxf(top, y[k]);
+    const uint32_t sorted = warp_sort(order_bits(top), lane);
+    own = __shfl_sync(0xffffffffu, sorted, a.K - 1);
+    const uint32_t bar = __shfl_sync(0xffffffffu, sorted, each - 1);
+    if (lane == 0) bars[warp] = bar;
+  }
+  __syncthreads();
   for (; c < v1; c += kBeamWarps * kChunk) {
     float z[16];
     const int next = c + kBeamWarps * kChunk;
@@ -140,22 +153,24 @@ __global__ void __launch_bounds__(kBeamThreads) beam_part_kernel(BeamArgs a, Bea
     float t;
     two_sum(s, sum, s, t);
     rest += t;
-    // (the list's last key has the float `bar`; an equal logit of a higher id does not pass)
-    const float bar = from_order_bits(static_cast<uint32_t>(last >> 32));
-    if (!__any_sync(0xffffffffu, last == 0 || top >= bar)) continue;
+    const uint32_t low = max(own, __reduce_min_sync(0xffffffffu, lane < active ? bars[lane] : 0xffffffffu));
+    if (!__any_sync(0xffffffffu, top >= from_order_bits(low))) continue;
+    bool taken = false;
 #pragma unroll
     for (int k = 0; k < 16; ++k) {
+      if (!__any_sync(0xffffffffu, z[k] >= from_order_bits(low))) continue;
       const int v = VEC ? c + 128 * (k / 4) + 4 * lane + k % 4 : c + 32 * k + lane;
-      const uint64_t key = v < v1 ? beam_key(z[k], v) : 0;
-      if (first) {
-        list = warp_sort(key, lane);
-        first = false;
-      } else if (__any_sync(0xffffffffu, key > last)) {
-        list_insert(list, key, key > last, a.K, lane);
-      } else {
-        continue;
-      }
+      const uint64_t key = beam_key(z[k], v);
+      const bool pass = v < v1 && z[k] >= from_order_bits(low) && key > last;
+      if (!__any_sync(0xffffffffu, pass)) continue;
+      list_insert(list, key, pass, a.K, lane);
       last = __shfl_sync(0xffffffffu, list, a.K - 1);
+      taken = true;
+    }
+    if (taken) {
+      own = max(own, static_cast<uint32_t>(last >> 32));
+      const uint32_t bar = static_cast<uint32_t>(__shfl_sync(0xffffffffu, list, each - 1) >> 32);
+      if (lane == 0 && bar > bars[warp]) bars[warp] = bar;
     }
   }
   // ---- the warp's sums, then the block's
