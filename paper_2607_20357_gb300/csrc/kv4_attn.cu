@@ -50,11 +50,12 @@ struct AttnParams {
   int ncols;      // columns of an item: min(8, rows * heads per KV head)
   int col_tiles;  // items per KV head
   int min_tiles;  // least tiles of a CTA that has any
-  float inv_grp;  // 1 / heads per KV head
+  int grp;        // heads per KV head
+  int columns;    // rows * grp
+  float inv_grp;  // 1 / grp
   float* part;    // [CTAs][2][ncols * (d_head + 2)]: parts of items shared with other CTAs, the one from
                   // the CTA before and the one that the next goes on with
-  int4* meta;     // [CTAs]: {slot (-1: none), item} of the latter; whether there is one of the former
-                  // (0: none, 1: it goes on, 2: it ends here)
+  int4* meta;     // [CTAs]: {slot (-1: none), item, KV head} of the latter, and the CTAs that it is in
 };
 
 // The tiles of a slot that any of its rows sees: `sink` tiles from 0 on, then those from `first`.
@@ -261,7 +262,7 @@ SVL_DEVINL int column_row(const AttnParams& p, int col) {
 
 // Writes four neighbouring output dimensions of column `col` of an item.
 SVL_DEVINL void store_out(const AttnParams& p, int slot, int head, int col, int d, float4 o) {
-  const int grp = p.a.A / p.a.c.kv, r = column_row(p, col), h = head * grp + col - r * grp;
+  const int r = column_row(p, col), h = head * p.grp + col - r * p.grp;
   __nv_bfloat16* out = p.a.out + (static_cast<int64_t>(slot) * p.a.rows + r) * p.a.ldo + h * p.a.c.dh + d;
   *reinterpret_cast<uint2*>(out) = make_uint2(pack_bf16x2(o.x, o.y), pack_bf16x2(o.z, o.w));
 }
@@ -279,18 +280,22 @@ SVL_DEVINL void add_scaled(float4& o, float f, float4 x) {
 // The weight 2^(m - M) l of a part beside the others' maximum M (0: it saw nothing).
 SVL_DEVINL float part_weight(float m, float l, float M) { return l == 0.f ? 0.f : l * ex2(m - M); }
 
-// NS: stages of a warp's ring. NT: 1 for items of up to four columns, 2 for up to eight. Column c is column
-// 2 (c % 4) + c / 4 of the operands, so that a lane's accumulators hold columns t (x = 0) and 4 + t (x = 1). With NT = 1
-// the other operand column of a pair holds the lower halves of the scaled weights.
-template <int DH, int NS, int NT>
+// NS: stages of a warp's ring. MODE: 0 for items of one column, 1 for up to four, 2 for up to eight. In modes 1 and 2 column
+// c is column 2 (c % 4) + c / 4 of the operands, so that a lane's accumulators hold columns t (x = 0) and 4 + t (x = 1); in
+// mode 1 the other operand column of a pair holds the lower halves of the scaled weights. In mode 0 the operands' columns
+// 2 j and 2 j + 1 belong to group j of 32 dimensions: of q they hold that group alone, so that one chain of products gives
+// lane t the sum of group t; of the weights the halves scaled for that group, so that one operand serves all
+// dimensions, of whose sums lane t holds those of group t.
+template <int DH, int NS, int MODE>
 __global__ void __launch_bounds__(kAttnThreads, 1) kv4_attn_kernel(AttnParams p, int slot_floats) {
-  constexpr int J = DH / 32, TB = kv4_tile_bytes(DH);
+  constexpr int J = DH / 32, TB = kv4_tile_bytes(DH), NT = MODE == 2 ? 2 : 1;
   extern __shared__ __align__(128) uint8_t smem[];  // per warp: ring of NS tiles; then per warp a part
   __shared__ int warp_sum[kAttnWarps], prefix[kAttnThreads];
   __shared__ int4 tile_meta[kAttnWarps][NS];   // {first position, bit 0: first tile of its item, bit 1: last; slot, item}
-  __shared__ int2 tile_item[kAttnWarps][NS];   // {KV head, start of the slot}
-  __shared__ int4 w_meta[kAttnWarps];   // {slot, item of the part in the ring (-1: none), state of the other part, -}
-  __shared__ int4 w_first[kAttnWarps];  // slot, item and KV head of that other part
+  __shared__ int4 tile_item[kAttnWarps][NS];   // {KV head, start of the slot, tiles of the item left after it, -}
+  __shared__ int4 w_meta[kAttnWarps];   // {slot, item of the part in the ring (-1: none), state of the other part (1: goes
+                                        // on, 2: ends), tiles of the ring's item left}
+  __shared__ int4 w_first[kAttnWarps];  // slot, item and KV head of that other part; KV head of the ring's
   const Kv4Attn& a = p.a;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int g = lane >> 2, t = lane & 3;
@@ -325,10 +330,10 @@ __global__ void __launch_bounds__(kAttnThreads, 1) kv4_attn_kernel(AttnParams p,
   const int cta_tiles = max((total + static_cast<int>(gridDim.x) - 1) / static_cast<int>(gridDim.x), p.min_tiles);
   const int cta0 = static_cast<int>(min(static_cast<int64_t>(total), static_cast<int64_t>(cta_tiles) * blockIdx.x));
   const int cta1 = total - cta0 < cta_tiles ? total : cta0 + cta_tiles;
-  const int share = (cta1 - cta0 + kAttnWarps - 1) / kAttnWarps;
-  const int last = share > 0 ? (cta1 - cta0 - 1) / share : -1;  // last warp with tiles
-  const int w0 = cta0 + warp * share;
-  const int n = warp <= last ? min(share, cta1 - w0) : 0;
+  const int share = (cta1 - cta0) / kAttnWarps, more = (cta1 - cta0) % kAttnWarps;  // the first `more` warps take one more
+  const int last = min(cta1 - cta0, kAttnWarps) - 1;                                // last warp with tiles
+  auto warp_tile = [&](int w) { return cta0 + w * share + min(w, more); };
+  const int w0 = warp_tile(warp), n = share + (warp < more ? 1 : 0);
 
   // ---- the tiles
   if (n > 0) {
@@ -359,7 +364,7 @@ __global__ void __launch_bounds__(kAttnThreads, 1) kv4_attn_kernel(AttnParams p,
       if (lane == 0) {
         tile_meta[warp][ask_stage] =
             make_int4(req.p0, (req.left == req.span.n ? 1 : 0) | (req.left == 1 ? 2 : 0), req.slot, req.item);
-        tile_item[warp][ask_stage] = make_int2(req.head, req.start);
+        tile_item[warp][ask_stage] = make_int4(req.head, req.start, req.left - 1, 0);
       }
       ask_stage = ask_stage + 1 == NS ? 0 : ask_stage + 1;
       if (++asked < n) walk_next<TB>(p, req);
@@ -371,7 +376,7 @@ __global__ void __launch_bounds__(kAttnThreads, 1) kv4_attn_kernel(AttnParams p,
     }
     __syncwarp();
     uint32_t q[J][4];
-    float qsum[J][NT], factor[NT], m[NT], l[NT], o[J][2][4];
+    float qsum[MODE == 0 ? 1 : J][NT], factor[NT], m[NT], l[NT], o[J][2][4];
     int end[NT], low[NT];
     int stage = 0, col0 = 0;
     bool started = false;
@@ -380,47 +385,60 @@ __global__ void __launch_bounds__(kAttnThreads, 1) kv4_attn_kernel(AttnParams p,
       if (i == 0 || (meta.y & 1)) {
         // a new item: its columns' queries as operands
         started = meta.y & 1;
-        const int grp = a.A / a.c.kv;
-        const int2 at = tile_item[warp][stage];
+        const int4 at = tile_item[warp][stage];
         col0 = p.col_tiles == 1 ? 0 : meta.w % p.col_tiles * kCols;
-        const int cols = min(kCols, a.rows * grp - col0);
-        const int col = 4 * (g & 1) + (g >> 1);  // of operand column g
-        uint4 raw[J];
+        const int cols = min(kCols, p.columns - col0);
+        constexpr int C = MODE == 0 ? 1 : J;  // groups of q that a lane has
+        // operand column g: the column's query, in mode 0 (even g) that of group g / 2
+        const int col = MODE == 0 ? 0 : 4 * (g & 1) + (g >> 1);
+        const bool has = MODE == 0 ? !(g & 1) && g < 2 * J : col < cols;
+        uint4 raw[C];
 #pragma unroll
-        for (int j = 0; j < J; ++j) raw[j] = make_uint4(0, 0, 0, 0);
-        if (col < cols) {
-          const int r = column_row(p, col0 + col), h = at.x * grp + col0 + col - r * grp;
+        for (int j = 0; j < C; ++j) raw[j] = make_uint4(0, 0, 0, 0);
+        if (has) {
+          const int r = column_row(p, col0 + col), h = at.x * p.grp + col0 + col - r * p.grp;
           const uint4* src = reinterpret_cast<const uint4*>(
-              a.q + (static_cast<int64_t>(meta.z) * a.rows + r) * a.ldq + h * DH + 8 * t);
+              a.q + (static_cast<int64_t>(meta.z) * a.rows + r) * a.ldq + h * DH + (MODE == 0 ? 16 * g : 0) + 8 * t);
 #pragma unroll
-          for (int j = 0; j < J; ++j) raw[j] = src[4 * j];
+          for (int j = 0; j < C; ++j) raw[j] = src[4 * j];
         }
         uint32_t big = 0;  // largest magnitude's bits
 #pragma unroll
-        for (int j = 0; j < J; ++j) {
+        for (int j = 0; j < C; ++j) {
           const uint32_t u[4] = {raw[j].x, raw[j].y, raw[j].z, raw[j].w};
 #pragma unroll
           for (int k = 0; k < 4; ++k) big = max(big, max(u[k] & 0x7fffu, u[k] >> 16 & 0x7fffu));
         }
-        big = max(big, __shfl_xor_sync(0xffffffffu, big, 1));
-        big = max(big, __shfl_xor_sync(0xffffffffu, big, 2));
+        if (MODE == 0) {
+          big = __reduce_max_sync(0xffffffffu, big);
+        } else {
+          big = max(big, __shfl_xor_sync(0xffffffffu, big, 1));
+          big = max(big, __shfl_xor_sync(0xffffffffu, big, 2));
+        }
         // times a power of two that takes it to [2^14, 2^15)
         const uint32_t eb = min(max(big >> 7, 14u), 254u);
         const float up = __uint_as_float((268 - eb) << 23), up4 = up * 0.0625f;
         float f = a.scale * 1.4426950408889634f * 1024.f * __uint_as_float(eb << 23);
         if (big >= 0x7f80u) f = NAN;  // a q that is not finite
 #pragma unroll
-        for (int j = 0; j < J; ++j) {
+        for (int j = 0; j < C; ++j) {
           const uint32_t u[4] = {raw[j].x, raw[j].y, raw[j].z, raw[j].w};  // dimensions 2 k, 2 k + 1 of the eight
-          q[j][0] = pack_f16x2(bf16_lo(u[0]) * up, bf16_lo(u[2]) * up);      // 0, 4
-          q[j][1] = pack_f16x2(bf16_lo(u[1]) * up, bf16_lo(u[3]) * up);      // 2, 6
-          q[j][2] = pack_f16x2(bf16_hi(u[0]) * up4, bf16_hi(u[2]) * up4);    // 1, 5
-          q[j][3] = pack_f16x2(bf16_hi(u[1]) * up4, bf16_hi(u[3]) * up4);    // 3, 7
+          const uint32_t y[4] = {pack_f16x2(bf16_lo(u[0]) * up, bf16_lo(u[2]) * up),      // 0, 4
+                                 pack_f16x2(bf16_lo(u[1]) * up, bf16_lo(u[3]) * up),      // 2, 6
+                                 pack_f16x2(bf16_hi(u[0]) * up4, bf16_hi(u[2]) * up4),    // 1, 5
+                                 pack_f16x2(bf16_hi(u[1]) * up4, bf16_hi(u[3]) * up4)};   // 3, 7
           float sum = 0.f;
 #pragma unroll
           for (int k = 0; k < 4; ++k) {
-            const float2 y = __half22float2(*reinterpret_cast<const __half2*>(&q[j][k]));
-            sum += k < 2 ? y.x + y.y : 16.f * (y.x + y.y);
+            const float2 z = __half22float2(*reinterpret_cast<const __half2*>(&y[k]));
+            sum += k < 2 ? z.x + z.y : 16.f * (z.x + z.y);
+            if (MODE != 0) q[j][k] = y[k];
+          }
+          if (MODE == 0) {
+#pragma unroll
+            for (int i = 0; i < J; ++i)
+#pragma unroll
+              for (int k = 0; k < 4; ++k) q[i][k] = g == 2 * i ? y[k] : 0;
           }
           sum += __shfl_xor_sync(0xffffffffu, sum, 1);
           sum += __shfl_xor_sync(0xffffffffu, sum, 2);
@@ -430,10 +448,11 @@ __global__ void __launch_bounds__(kAttnThreads, 1) kv4_attn_kernel(AttnParams p,
         }
 #pragma unroll
         for (int x = 0; x < NT; ++x) {
-          factor[x] = __shfl_sync(0xffffffffu, f, 8 * t + 4 * x);
-          const int64_t pos = static_cast<int64_t>(at.y) + column_row(p, col0 + 4 * x + t);
+          factor[x] = MODE == 0 ? f : __shfl_sync(0xffffffffu, f, 8 * t + 4 * x);
+          const int c = MODE == 0 ? 0 : 4 * x + t;
+          const int64_t pos = static_cast<int64_t>(at.y) + column_row(p, col0 + c);
           // (-1: no such column)
-          end[x] = 4 * x + t >= cols ? -1 : (pos >= 0 && pos < a.c.max_len ? static_cast<int>(pos) + 1 : 0);
+          end[x] = c >= cols ? -1 : (pos >= 0 && pos < a.c.max_len ? static_cast<int>(pos) + 1 : 0);
           low[x] = a.window > 0 && end[x] > a.window ? end[x] - a.window : 0;
           m[x] = -INFINITY;
           l[x] = 0.f;
@@ -474,27 +493,47 @@ __global__ void __launch_bounds__(kAttnThreads, 1) kv4_attn_kernel(AttnParams p,
       for (int h = 0; h < 2; ++h) {
         const Words<J> wa = lds_words<J>(tile + ((16 * h + g) * 4 + t) * J * 4);
         const Words<J> wb = lds_words<J>(tile + ((16 * h + g + 8) * 4 + t) * J * 4);
+        if constexpr (MODE == 0) {
+          float d[4] = {qsum[0][0], 0.f, qsum[0][0], 0.f};
+#pragma unroll
+          for (int j = 0; j < J; ++j) {
+            const uint32_t u = wa.w[j], v = wb.w[j], u8 = u >> 8, v8 = v >> 8;
+            mma16816_f16(d, u & kLow, v & kLow, u8 & kLow, v8 & kLow, q[j][0], q[j][1], d[0], d[1], d[2], d[3]);
+            mma16816_f16(d, u & kHigh, v & kHigh, u8 & kHigh, v8 & kHigh, q[j][2], q[j][3], d[0], d[1], d[2], d[3]);
+          }
+#pragma unroll
+          for (int r = 0; r < 2; ++r) {
+            float x = 0.f;
+            if (t < J) {
+              const uint32_t u = reinterpret_cast<const uint16_t*>(tile + kv4_k_scales(DH))[(16 * h + 8 * r + g) * J + t];
+              x = bf16_lo(u) * d[2 * r];
+            }
+            x += __shfl_xor_sync(0xffffffffu, x, 1);
+            s[h][r][0] = x + __shfl_xor_sync(0xffffffffu, x, 2);
+          }
+        } else {
         const uint8_t* sk = tile + kv4_k_scales(DH) + (16 * h + g) * J * 2;
-        uint32_t ka[J / 2], kb[J / 2];
+          uint32_t ka[J / 2], kb[J / 2];
 #pragma unroll
-        for (int k = 0; k < J / 2; ++k) {
-          ka[k] = reinterpret_cast<const uint32_t*>(sk)[k];
-          kb[k] = reinterpret_cast<const uint32_t*>(sk + 8 * J * 2)[k];
-        }
+          for (int k = 0; k < J / 2; ++k) {
+            ka[k] = reinterpret_cast<const uint32_t*>(sk)[k];
+            kb[k] = reinterpret_cast<const uint32_t*>(sk + 8 * J * 2)[k];
+          }
 #pragma unroll
-        for (int j = 0; j < J; ++j) {
-          const uint32_t u = wa.w[j], v = wb.w[j], u8 = u >> 8, v8 = v >> 8;
-          float d[4];
-          constexpr int X = NT - 1;
-          const float c1 = NT == 2 ? qsum[j][X] : 0.f;
-          mma16816_f16(d, u & kLow, v & kLow, u8 & kLow, v8 & kLow, q[j][0], q[j][1], qsum[j][0], c1, qsum[j][0], c1);
-          mma16816_f16(d, u & kHigh, v & kHigh, u8 & kHigh, v8 & kHigh, q[j][2], q[j][3], d[0], d[1], d[2], d[3]);
-          const float fa = j & 1 ? bf16_hi(ka[j / 2]) : bf16_lo(ka[j / 2]);
-          const float fb = j & 1 ? bf16_hi(kb[j / 2]) : bf16_lo(kb[j / 2]);
+          for (int j = 0; j < J; ++j) {
+            const uint32_t u = wa.w[j], v = wb.w[j], u8 = u >> 8, v8 = v >> 8;
+            float d[4];
+            constexpr int X = NT - 1;
+            const float c1 = NT == 2 ? qsum[j][X] : 0.f;
+            mma16816_f16(d, u & kLow, v & kLow, u8 & kLow, v8 & kLow, q[j][0], q[j][1], qsum[j][0], c1, qsum[j][0], c1);
+            mma16816_f16(d, u & kHigh, v & kHigh, u8 & kHigh, v8 & kHigh, q[j][2], q[j][3], d[0], d[1], d[2], d[3]);
+            const float fa = j & 1 ? bf16_hi(ka[j / 2]) : bf16_lo(ka[j / 2]);
+            const float fb = j & 1 ? bf16_hi(kb[j / 2]) : bf16_lo(kb[j / 2]);
 #pragma unroll
-          for (int x = 0; x < NT; ++x) {
-            s[h][0][x] = j ? fmaf(fa, d[x], s[h][0][x]) : fa * d[x];
-            s[h][1][x] = j ? fmaf(fb, d[x + 2], s[h][1][x]) : fb * d[x + 2];
+            for (int x = 0; x < NT; ++x) {
+              s[h][0][x] = j ? fmaf(fa, d[x], s[h][0][x]) : fa * d[x];
+              s[h][1][x] = j ? fmaf(fb, d[x + 2], s[h][1][x]) : fb * d[x + 2];
+            }
           }
         }
 #pragma unroll
@@ -542,7 +581,31 @@ __global__ void __launch_bounds__(kAttnThreads, 1) kv4_attn_kernel(AttnParams p,
       for (int h = 0; h < 2; ++h) {
         const Words<J> v0 = lds_words<J>(tile + kv4_v_codes(DH) + (((h * 2) * 8 + g) * 4 + t) * J * 4);
         const Words<J> v1 = lds_words<J>(tile + kv4_v_codes(DH) + (((h * 2 + 1) * 8 + g) * 4 + t) * J * 4);
-        if constexpr (NT == 1) {
+        if constexpr (MODE == 0) {
+          uint32_t b[2];
+#pragma unroll
+          for (int r = 0; r < 2; ++r) {
+            const float w = ex2(s[h][r][0] - (m[0] == -INFINITY ? 0.f : m[0]));
+            l[0] += w;
+            float x = 0.f;
+            if (t < J) {
+              // the lane's row and group
+              const int at = ((8 * h + 4 * r + (g >> 1)) * J + t) * 2 + (g & 1);
+              const uint32_t u = reinterpret_cast<const uint16_t*>(tile + kv4_v_scales(DH))[at];
+              x = w * bf16_lo(u);
+            }
+            if (odd && w == 0.f) x = 0.f;  // what the column does not see does not count, whatever its scale
+            const float hi = __uint_as_float(__float_as_uint(x) & 0xffff0000u);
+            b[r] = transpose8(pack_bf16x2(hi, x - hi));
+          }
+#pragma unroll
+          for (int j = 0; j < J; ++j) {
+            uint32_t c[4][2];
+            v_operands(v0.w[j], v1.w[j], c);
+            mma16816_bf16(o[j][0], c[0][0], c[2][0], c[0][1], c[2][1], b[0], b[1]);
+            mma16816_bf16(o[j][1], c[1][0], c[3][0], c[1][1], c[3][1], b[0], b[1]);
+          }
+        } else if constexpr (MODE == 1) {
           float w[2];
           Words<J> u[2];  // scales of this lane's rows and their neighbours
 #pragma unroll
@@ -595,7 +658,7 @@ __global__ void __launch_bounds__(kAttnThreads, 1) kv4_attn_kernel(AttnParams p,
       const bool ended = meta.y & 2;
       if (ended || i + 1 == n) {
         // the item's end, or this warp's
-        const int head = tile_item[warp][stage == 0 ? NS - 1 : stage - 1].x;
+        const int4 at = tile_item[warp][stage == 0 ? NS - 1 : stage - 1];
         float* part = started ? last_part : first_part;
         if (started && !ended) {
           cp_wait<0>();
@@ -606,28 +669,45 @@ __global__ void __launch_bounds__(kAttnThreads, 1) kv4_attn_kernel(AttnParams p,
 #pragma unroll
           for (int off = 4; off <= 16; off <<= 1) l[x] += __shfl_xor_sync(0xffffffffu, l[x], off);
           if (end[x] < 0) continue;
-          const float inv = l[x] == 0.f ? 0.f : 1.f / l[x];
-          const int col = 4 * x + t;
-          if (!(started && ended) && g == 0) {
+          const float inv = l[x] == 0.f ? 0.f : __fdividef(1.f, l[x]);
+          const int col = MODE == 0 ? 0 : 4 * x + t;
+          if (!(started && ended) && lane < (MODE == 0 ? 1 : 4)) {
             part[p.ncols * DH + 2 * col] = m[x];
             part[p.ncols * DH + 2 * col + 1] = l[x];
           }
+          if constexpr (MODE == 0) {
+            float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
-          for (int j = 0; j < J; ++j) {
-            float4 y = make_float4(o[j][0][x], o[j][1][x], o[j][0][x + 2], o[j][1][x + 2]);
-            if (NT == 1) y = make_float4(y.x + o[j][0][1], y.y + o[j][1][1], y.z + o[j][0][3], y.w + o[j][1][3]);
+            for (int j = 0; j < J; ++j)
+              if (t == j)
+                y = make_float4(o[j][0][0] + o[j][0][1], o[j][1][0] + o[j][1][1], o[j][0][2] + o[j][0][3],
+                                o[j][1][2] + o[j][1][3]);
+            if (t >= J) continue;
             y = make_float4(y.x * inv, y.y * inv, y.z * inv, y.w * inv);
-            if (started && ended) store_out(p, meta.z, head, col0 + col, 32 * j + 4 * g, y);
-            else *reinterpret_cast<float4*>(part + col * DH + 32 * j + 4 * g) = y;
+            if (started && ended) store_out(p, meta.z, at.x, 0, 32 * t + 4 * g, y);
+            else *reinterpret_cast<float4*>(part + 32 * t + 4 * g) = y;
+          } else {
+#pragma unroll
+            for (int j = 0; j < J; ++j) {
+              float4 y = make_float4(o[j][0][x], o[j][1][x], o[j][0][x + 2], o[j][1][x + 2]);
+              if (MODE == 1) y = make_float4(y.x + o[j][0][1], y.y + o[j][1][1], y.z + o[j][0][3], y.w + o[j][1][3]);
+              y = make_float4(y.x * inv, y.y * inv, y.z * inv, y.w * inv);
+              if (started && ended) store_out(p, meta.z, at.x, col0 + col, 32 * j + 4 * g, y);
+              else *reinterpret_cast<float4*>(part + col * DH + 32 * j + 4 * g) = y;
+            }
           }
         }
         if (lane == 0 && !started) {
           w_meta[warp].z = ended ? 2 : 1;
-          w_first[warp] = make_int4(meta.z, meta.w, head, 0);
+          w_first[warp].x = meta.z;
+          w_first[warp].y = meta.w;
+          w_first[warp].z = at.x;
         }
         if (lane == 0 && started && !ended) {
           w_meta[warp].x = meta.z;
           w_meta[warp].y = meta.w;
+          w_meta[warp].w = at.z;
+          w_first[warp].w = at.x;
         }
       }
       __syncwarp();  // the next tile's meta
@@ -643,16 +723,13 @@ __global__ void __launch_bounds__(kAttnThreads, 1) kv4_attn_kernel(AttnParams p,
   const uint32_t goes_on = __ballot_sync(0xffffffffu, wm.z == 1);   // warps within an item
   uint32_t ends = __ballot_sync(0xffffffffu, wm.z == 2);            // warps with an item's end
   if (tid == 0) {
-    // what other CTAs have to know: the item that goes on in the next one and started here, and whether one from before
-    // ends here (warps 0, 1, ... go on with it until one ends it)
-    const bool before = (goes_on | ends) & 1u;
-    int4 mt = make_int4(-1, 0, before ? (ends && __ffs(ends) - 1 == __ffs(~goes_on) - 1 ? 2 : 1) : 0, 0);
-    if (starts && last >= 0) {
-      const int v = 31 - __clz(starts);
-      if (v == last || !(ends >> v >> 1)) {
-        mt.x = w_meta[v].x;
-        mt.y = w_meta[v].y;
-      }
+    // the item that started here and goes on in the next CTA, and how many CTAs it is in
+    int4 mt = make_int4(-1, 0, 0, 0);
+    const int v = 31 - __clz(starts);
+    if (starts && !(ends >> v >> 1)) {
+      // (the rest of the start's part is in the warps after it)
+      const int left = w_meta[v].w - (cta1 - warp_tile(v + 1));
+      if (left > 0) mt = make_int4(w_meta[v].x, w_meta[v].y, w_first[v].w, 1 + (left + cta_tiles - 1) / cta_tiles);
     }
     p.meta[blockIdx.x] = mt;
   }
@@ -669,7 +746,7 @@ __global__ void __launch_bounds__(kAttnThreads, 1) kv4_attn_kernel(AttnParams p,
     const int from = here ? 31 - __clz(earlier) : 0;
     const bool done = here && !(goes_on >> to & 1u);
     const int4 it = w_first[to];
-    const int c0 = p.col_tiles == 1 ? 0 : it.y % p.col_tiles * kCols, cols = min(kCols, a.rows * (a.A / a.c.kv) - c0);
+    const int c0 = p.col_tiles == 1 ? 0 : it.y % p.col_tiles * kCols, cols = min(kCols, p.columns - c0);
     for (int col = 0; col < cols; ++col) {
       const bool skip = turn != warp;
       turn = turn + 1 == kAttnWarps ? 0 : turn + 1;
@@ -687,7 +764,7 @@ __global__ void __launch_bounds__(kAttnThreads, 1) kv4_attn_kernel(AttnParams p,
       float L = f;
 #pragma unroll
       for (int off = 8; off > 0; off >>= 1) L += __shfl_xor_sync(0xffffffffu, L, off);
-      const float inv = L == 0.f ? 0.f : 1.f / L;
+      const float inv = L == 0.f ? 0.f : __fdividef(1.f, L);
       M = __shfl_sync(0xffffffffu, M, 0);
       L = __shfl_sync(0xffffffffu, L, 0);
       const float fi = f * __shfl_sync(0xffffffffu, inv, 0);
@@ -720,27 +797,13 @@ __global__ void __launch_bounds__(kAttnThreads, 1) kv4_attn_kernel(AttnParams p,
 template <int DH>
 __global__ void __launch_bounds__(kMergeThreads) kv4_merge_kernel(AttnParams p, int slot_floats) {
   constexpr int kWarps = kMergeThreads / 32;
-  __shared__ int last;
   __shared__ float warp_m[kWarps], warp_l[kWarps];
   __shared__ float4 sum[kWarps][32];
-  const int c = blockIdx.x, col = blockIdx.y, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  if (tid == 0) last = gridDim.x - 1;
+  const int c = blockIdx.x, col = blockIdx.y, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   pdl_begin(p.a.late);
   const int4 it = p.meta[c];
-  int ends = gridDim.x;  // the first CTA from here on where an item from before ends
-#pragma unroll
-  for (int i = 0; i < kMaxCtas / kMergeThreads; ++i) {
-    const int at = c + 1 + i * kMergeThreads + tid;
-    if (at < static_cast<int>(gridDim.x) && p.meta[at].z == 2) ends = min(ends, at);
-  }
-  if (it.x < 0) return;
-  const int c0 = p.col_tiles == 1 ? 0 : it.y % p.col_tiles * kCols;
-  if (c0 + col >= p.a.rows * (p.a.A / p.a.c.kv)) return;
-  __syncthreads();
-  ends = __reduce_min_sync(0xffffffffu, ends);
-  if (lane == 0) atomicMin(&last, ends);
-  __syncthreads();
-  const int n = last - c + 1;
+  const int c0 = p.col_tiles == 1 ? 0 : it.y % p.col_tiles * kCols, n = it.w;
+  if (it.x < 0 || c0 + col >= p.columns) return;
   float m = -INFINITY, l = 0.f;
   float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
   const int d = 4 * lane;
@@ -776,8 +839,7 @@ __global__ void __launch_bounds__(kMergeThreads) kv4_merge_kernel(AttnParams p, 
     add_scaled(o, f, sum[w][lane]);
   }
   const float inv = L == 0.f ? 0.f : 1.f / L;
-  const int head = slot_head(p.a, it.x, p.col_tiles == 1 ? it.y : it.y / p.col_tiles);
-  store_out(p, it.x, head, c0 + col, d, make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv));
+  store_out(p, it.x, it.z, c0 + col, d, make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv));
 }
 
 static int attn_ncols(const Kv4Cache& c, int A, int rows) {
@@ -790,12 +852,12 @@ size_t kv4_attn_workspace(const Kv4Cache& c, int A, int rows) {
   return kMaxCtas * (2 * floats * sizeof(float) + sizeof(int4));
 }
 
-template <int DH, int NS, int NT>
+template <int DH, int NS, int MODE>
 static cudaError_t launch_attn(const AttnParams& p, int slot_floats, int grid, cudaStream_t s) {
   const int smem = kAttnWarps * (NS * kv4_tile_bytes(DH) + slot_floats * 4);
-  cudaError_t e = cudaFuncSetAttribute(kv4_attn_kernel<DH, NS, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+  cudaError_t e = cudaFuncSetAttribute(kv4_attn_kernel<DH, NS, MODE>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
   if (e != cudaSuccess) return e;
-  e = launch_pdl(kv4_attn_kernel<DH, NS, NT>, dim3(grid), kAttnThreads, smem, s, p, slot_floats);
+  e = launch_pdl(kv4_attn_kernel<DH, NS, MODE>, dim3(grid), kAttnThreads, smem, s, p, slot_floats);
   if (e != cudaSuccess) return e;
   return launch_pdl(kv4_merge_kernel<DH>, dim3(grid, p.ncols), kMergeThreads, 0, s, p, slot_floats);
 }
@@ -805,15 +867,22 @@ cudaError_t launch_kv4_attention(const Kv4Attn& a, cudaStream_t s) {
   p.a = a;
   p.ncols = attn_ncols(a.c, a.A, a.rows);
   p.col_tiles = (a.rows * (a.A / a.c.kv) + kCols - 1) / kCols;
-  p.min_tiles = 4;
-  p.inv_grp = 1.f / static_cast<float>(a.A / a.c.kv);
+  p.min_tiles = 6;  // (1,900 rows of four KV heads: 2 10.5 us, 4 9.1, 6 9.0, 12 9.8)
+  p.grp = a.A / a.c.kv;
+  p.columns = a.rows * p.grp;
+  p.inv_grp = 1.f / static_cast<float>(p.grp);
   const int slot_floats = part_floats(p.ncols, a.c.dh);
   const int grid = a.num_sms < kMaxCtas ? a.num_sms : kMaxCtas;
   p.meta = static_cast<int4*>(a.ws);
   p.part = reinterpret_cast<float*>(p.meta + kMaxCtas);
+  // (one column: a head per KV head and one row, the decode step of a model without grouped heads)
   if (a.c.dh == 64)
-    return p.ncols <= 4 ? launch_attn<64, 4, 1>(p, slot_floats, grid, s) : launch_attn<64, 4, 2>(p, slot_floats, grid, s);
-  return p.ncols <= 4 ? launch_attn<128, 3, 1>(p, slot_floats, grid, s) : launch_attn<128, 3, 2>(p, slot_floats, grid, s);
+    return p.ncols == 1   ? launch_attn<64, 4, 0>(p, slot_floats, grid, s)
+           : p.ncols <= 4 ? launch_attn<64, 4, 1>(p, slot_floats, grid, s)
+                          : launch_attn<64, 4, 2>(p, slot_floats, grid, s);
+  return p.ncols == 1   ? launch_attn<128, 3, 0>(p, slot_floats, grid, s)
+         : p.ncols <= 4 ? launch_attn<128, 3, 1>(p, slot_floats, grid, s)
+                        : launch_attn<128, 3, 2>(p, slot_floats, grid, s);
 }
 
 }  // namespace svl
