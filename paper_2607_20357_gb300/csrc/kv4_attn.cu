@@ -40,7 +40,6 @@
 
 namespace svl {
 
-constexpr int kAttnWarps = 12, kAttnThreads = kAttnWarps * 32;
 constexpr int kCols = 8;
 constexpr int kMaxCtas = 256;
 constexpr int kMergeThreads = 128;
@@ -280,15 +279,17 @@ SVL_DEVINL void add_scaled(float4& o, float f, float4 x) {
 // The weight 2^(m - M) l of a part beside the others' maximum M (0: it saw nothing).
 SVL_DEVINL float part_weight(float m, float l, float M) { return l == 0.f ? 0.f : l * ex2(m - M); }
 
-// NS: stages of a warp's ring. MODE: 0 for items of one column, 1 for up to four, 2 for up to eight. In modes 1 and 2 column
+// NW: warps, NS: stages of a warp's ring. MODE: 0 for items of one column, 1 for up to four, 2 for up to eight. In modes 1 and 2 column
 // c is column 2 (c % 4) + c / 4 of the operands, so that a lane's accumulators hold columns t (x = 0) and 4 + t (x = 1); in
 // mode 1 the other operand column of a pair holds the lower halves of the scaled weights. In mode 0 the operands' columns
 // 2 j and 2 j + 1 belong to group j of 32 dimensions: of q they hold that group alone, so that one chain of products gives
 // lane t the sum of group t; of the weights the halves scaled for that group, so that one operand serves all
 // dimensions, of whose sums lane t holds those of group t.
-template <int DH, int NS, int MODE>
-__global__ void __launch_bounds__(kAttnThreads, 1) kv4_attn_kernel(AttnParams p, int slot_floats) {
+template <int DH, int NS, int NW, int MODE>
+__global__ void __launch_bounds__(NW * 32, 1) kv4_attn_kernel(AttnParams p, int slot_floats) {
   constexpr int J = DH / 32, TB = kv4_tile_bytes(DH), NT = MODE == 2 ? 2 : 1;
+  constexpr int kAttnWarps = NW, kAttnThreads = NW * 32;
+  static_assert(NW <= 16, "sums over the warps take 16 lanes");
   extern __shared__ __align__(128) uint8_t smem[];  // per warp: ring of NS tiles; then per warp a part
   __shared__ int warp_sum[kAttnWarps], prefix[kAttnThreads];
   __shared__ int4 tile_meta[kAttnWarps][NS];   // {first position, bit 0: first tile of its item, bit 1: last; slot, item}
@@ -378,7 +379,7 @@ __global__ void __launch_bounds__(kAttnThreads, 1) kv4_attn_kernel(AttnParams p,
     uint32_t q[J][4];
     float qsum[MODE == 0 ? 1 : J][NT], factor[NT], m[NT], l[NT], o[J][2][4];
     int end[NT], low[NT];
-    int stage = 0, col0 = 0;
+    int stage = 0, col0 = 0, whole_lo = 0, whole_hi = 0;
     bool started = false;
     for (int i = 0; i < n; ++i) {
       const int4 meta = tile_meta[warp][stage];
@@ -457,6 +458,16 @@ __global__ void __launch_bounds__(kAttnThreads, 1) kv4_attn_kernel(AttnParams p,
           m[x] = -INFINITY;
           l[x] = 0.f;
         }
+        // what every column sees: [whole_lo, whole_hi), and below whole_hi the sinks
+        {
+          int lo = low[0], hi = end[0] < 0 ? 0x7fffffff : end[0];
+          if (NT == 2) {
+            lo = max(lo, low[NT - 1]);
+            hi = min(hi, end[NT - 1] < 0 ? 0x7fffffff : end[NT - 1]);
+          }
+          whole_lo = MODE == 0 ? lo : __reduce_max_sync(0xffffffffu, lo);
+          whole_hi = MODE == 0 ? hi : __reduce_min_sync(0xffffffffu, hi);
+        }
 #pragma unroll
         for (int j = 0; j < J; ++j)
 #pragma unroll
@@ -469,30 +480,14 @@ __global__ void __launch_bounds__(kAttnThreads, 1) kv4_attn_kernel(AttnParams p,
       cp_commit();
       uint8_t* tile = ring + stage * TB;
       const int p0 = meta.x;
-      uint32_t sight[NT];  // of the tile's positions
-      bool all = true;
-#pragma unroll
-      for (int x = 0; x < NT; ++x) {
-        sight[x] = (bits_below(end[x] - p0) & ~bits_below(low[x] - p0)) | bits_below(min(a.sinks, end[x]) - p0);
-        all = all && (end[x] < 0 || sight[x] == ~0u);
-      }
-      const bool whole = __all_sync(0xffffffffu, all);
-
-      // whether a scale of V is not finite (a stored NaN, or what lies where nothing was written)
-      bool odd = false;
-#pragma unroll
-      for (int k = 0; k < J / 2; ++k) {
-        const uint32_t x = reinterpret_cast<const uint32_t*>(tile + kv4_v_scales(DH))[lane * (J / 2) + k];
-        odd |= (x & 0x7f80u) == 0x7f80u || (x & 0x7f800000u) == 0x7f800000u;
-      }
-      odd = __any_sync(0xffffffffu, odd);
+      const bool whole = p0 + kKv4Tile <= whole_hi && (p0 >= whole_lo || p0 + kKv4Tile <= a.sinks);
 
       // scores of the tile's 32 positions: rows g and g + 8 of both halves
       float s[2][2][NT];
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        const Words<J> wa = lds_words<J>(tile + ((16 * h + g) * 4 + t) * J * 4);
-        const Words<J> wb = lds_words<J>(tile + ((16 * h + g + 8) * 4 + t) * J * 4);
+        const Words<J> wa = lds_words<J>(tile + (64 * h + lane) * J * 4);
+        const Words<J> wb = lds_words<J>(tile + (64 * h + 32 + lane) * J * 4);
         if constexpr (MODE == 0) {
           float d[4] = {qsum[0][0], 0.f, qsum[0][0], 0.f};
 #pragma unroll
@@ -544,10 +539,13 @@ __global__ void __launch_bounds__(kAttnThreads, 1) kv4_attn_kernel(AttnParams p,
       }
       if (!whole) {
 #pragma unroll
-        for (int x = 0; x < NT; ++x)
+        for (int x = 0; x < NT; ++x) {
+          const uint32_t sight =
+              (bits_below(end[x] - p0) & ~bits_below(low[x] - p0)) | bits_below(min(a.sinks, end[x]) - p0);
 #pragma unroll
           for (int k = 0; k < 4; ++k)
-            if (!(sight[x] >> (8 * k + g) & 1u)) s[k >> 1][k & 1][x] = -INFINITY;
+            if (!(sight >> (8 * k + g) & 1u)) s[k >> 1][k & 1][x] = -INFINITY;
+        }
       }
       // the running maximum moves when it is passed by more than a factor of two
       float top[NT];
@@ -579,8 +577,8 @@ __global__ void __launch_bounds__(kAttnThreads, 1) kv4_attn_kernel(AttnParams p,
       }
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        const Words<J> v0 = lds_words<J>(tile + kv4_v_codes(DH) + (((h * 2) * 8 + g) * 4 + t) * J * 4);
-        const Words<J> v1 = lds_words<J>(tile + kv4_v_codes(DH) + (((h * 2 + 1) * 8 + g) * 4 + t) * J * 4);
+        const Words<J> v0 = lds_words<J>(tile + kv4_v_codes(DH) + (64 * h + lane) * J * 4);
+        const Words<J> v1 = lds_words<J>(tile + kv4_v_codes(DH) + (64 * h + 32 + lane) * J * 4);
         if constexpr (MODE == 0) {
           uint32_t b[2];
 #pragma unroll
@@ -594,7 +592,7 @@ __global__ void __launch_bounds__(kAttnThreads, 1) kv4_attn_kernel(AttnParams p,
               const uint32_t u = reinterpret_cast<const uint16_t*>(tile + kv4_v_scales(DH))[at];
               x = w * bf16_lo(u);
             }
-            if (odd && w == 0.f) x = 0.f;  // what the column does not see does not count, whatever its scale
+            if (!whole && w == 0.f) x = 0.f;  // what the column does not see does not count, whatever its scale
             const float hi = __uint_as_float(__float_as_uint(x) & 0xffff0000u);
             b[r] = transpose8(pack_bf16x2(hi, x - hi));
           }
@@ -613,7 +611,7 @@ __global__ void __launch_bounds__(kAttnThreads, 1) kv4_attn_kernel(AttnParams p,
             w[r] = ex2(s[h][r][0] - (m[0] == -INFINITY ? 0.f : m[0]));
             l[0] += w[r];
             u[r] = lds_words<J>(tile + kv4_v_scales(DH) + (8 * h + 4 * r + (g >> 1)) * J * 4);
-            if (odd && w[r] == 0.f) {  // what a column does not see does not count, whatever its scale
+            if (!whole && w[r] == 0.f) {  // what a column does not see does not count, whatever its scale
 #pragma unroll
               for (int j = 0; j < J; ++j) u[r].w[j] = 0;
             }
@@ -649,8 +647,8 @@ __global__ void __launch_bounds__(kAttnThreads, 1) kv4_attn_kernel(AttnParams p,
           }
           const Words<J> u0 = lds_words<J>(tile + kv4_v_scales(DH) + (8 * h + t) * J * 4);
           const Words<J> u1 = lds_words<J>(tile + kv4_v_scales(DH) + (8 * h + 4 + t) * J * 4);
-          if (odd) weighted_rows<J, true>(o, hi, lo, u0, u1, v0, v1);
-          else weighted_rows<J, false>(o, hi, lo, u0, u1, v0, v1);
+          if (whole) weighted_rows<J, false>(o, hi, lo, u0, u1, v0, v1);
+          else weighted_rows<J, true>(o, hi, lo, u0, u1, v0, v1);
         }
       }
 
@@ -852,12 +850,12 @@ size_t kv4_attn_workspace(const Kv4Cache& c, int A, int rows) {
   return kMaxCtas * (2 * floats * sizeof(float) + sizeof(int4));
 }
 
-template <int DH, int NS, int MODE>
+template <int DH, int NS, int NW, int MODE>
 static cudaError_t launch_attn(const AttnParams& p, int slot_floats, int grid, cudaStream_t s) {
-  const int smem = kAttnWarps * (NS * kv4_tile_bytes(DH) + slot_floats * 4);
-  cudaError_t e = cudaFuncSetAttribute(kv4_attn_kernel<DH, NS, MODE>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+  const int smem = NW * (NS * kv4_tile_bytes(DH) + slot_floats * 4);
+  cudaError_t e = cudaFuncSetAttribute(kv4_attn_kernel<DH, NS, NW, MODE>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
   if (e != cudaSuccess) return e;
-  e = launch_pdl(kv4_attn_kernel<DH, NS, MODE>, dim3(grid), kAttnThreads, smem, s, p, slot_floats);
+  e = launch_pdl(kv4_attn_kernel<DH, NS, NW, MODE>, dim3(grid), NW * 32, smem, s, p, slot_floats);
   if (e != cudaSuccess) return e;
   return launch_pdl(kv4_merge_kernel<DH>, dim3(grid, p.ncols), kMergeThreads, 0, s, p, slot_floats);
 }
@@ -877,12 +875,12 @@ cudaError_t launch_kv4_attention(const Kv4Attn& a, cudaStream_t s) {
   p.part = reinterpret_cast<float*>(p.meta + kMaxCtas);
   // (one column: a head per KV head and one row, the decode step of a model without grouped heads)
   if (a.c.dh == 64)
-    return p.ncols == 1   ? launch_attn<64, 4, 0>(p, slot_floats, grid, s)
-           : p.ncols <= 4 ? launch_attn<64, 4, 1>(p, slot_floats, grid, s)
-                          : launch_attn<64, 4, 2>(p, slot_floats, grid, s);
-  return p.ncols == 1   ? launch_attn<128, 3, 0>(p, slot_floats, grid, s)
-         : p.ncols <= 4 ? launch_attn<128, 3, 1>(p, slot_floats, grid, s)
-                        : launch_attn<128, 3, 2>(p, slot_floats, grid, s);
+    return p.ncols == 1   ? launch_attn<64, 4, 16, 0>(p, slot_floats, grid, s)
+           : p.ncols <= 4 ? launch_attn<64, 4, 12, 1>(p, slot_floats, grid, s)
+                          : launch_attn<64, 4, 12, 2>(p, slot_floats, grid, s);
+  return p.ncols == 1   ? launch_attn<128, 2, 16, 0>(p, slot_floats, grid, s)
+         : p.ncols <= 4 ? launch_attn<128, 3, 12, 1>(p, slot_floats, grid, s)
+                        : launch_attn<128, 3, 12, 2>(p, slot_floats, grid, s);
 }
 
 }  // namespace svl
