@@ -64,64 +64,68 @@ SVL_DEVINL bool find_unit(const Kv4Rows& a, int64_t u, int lane, Unit& q) {
   return first >= 0 && q.i1 > q.i0;
 }
 
-// x / s rounded to the nearest integer, of two the even one, exactly, at most 7. inv is 1 / s in float32, so t = x * inv
-// is off by less than 2^-20 for |x / s| <= 8. x and s are bf16 numbers: where x / s is not half an integer it is at
-// least 2^-9 from one, so t rounded to a multiple of 2^-15 (by 384 = 1.5 * 2^8, whose last place that is) is half an
-// integer exactly where x / s is.
-SVL_DEVINL float kv4_code(float x, float inv) {
-  const float t = __fadd_rn(__fadd_rn(__fmul_rn(x, inv), 384.f), -384.f);
-  return __fadd_rn(__fadd_rn(fminf(t, 7.f), 12582912.f), -12582912.f);  // 1.5 * 2^23: to an integer
+// The code of x, rint(x / s) + 8 (of two nearest the even one) and at most 15, in the low four bits. inv is 1 / s to within
+// 2^-23 of it, so x * inv is off by less than 2^-19 for |x / s| <= 8. x and s are bf16 numbers: where x / s is not half an
+// integer it is at least 2^-9 from one. Rounded to a multiple of 2^-15 (the last place of 384 = 1.5 * 2^8), x * inv is
+// thus half an integer exactly where x / s is, and on its side of it elsewhere; the second sum (1.5 * 2^23 + 8) rounds it to
+// an integer.
+SVL_DEVINL uint32_t kv4_code(float x, float inv) {
+  const float t = fminf(__fmaf_rn(x, inv, 384.f), 391.f);
+  return __float_as_uint(__fadd_rn(t, 12582920.f - 384.f));
 }
-
-// The scale (bf16 bits) of a group whose largest and smallest values are in hi and lo, of which `finite` says whether
-// all were, and its reciprocal for kv4_code (0: every code is 8).
-SVL_DEVINL uint16_t kv4_scale(float hi, float lo, bool finite, float& inv) {
-  const float s = (hi >= -lo ? hi : lo) * -0.125f;
-  inv = 0.f;
-  if (!finite) return 0x7fc0;
-  if (fabsf(s) < 1.17549435e-38f) return 0;
-  inv = __frcp_rn(s);
-  return __bfloat16_as_ushort(__float2bfloat16_rn(s));
+// Eight codes as a word, lowest first (kv4_code's upper bits, 0x4b400000 each, are taken off together).
+SVL_DEVINL uint32_t eight_codes(const uint32_t* n) {
+  uint32_t w = n[7];
+#pragma unroll
+  for (int i = 6; i >= 0; --i) w = w * 16u + n[i];
+  return w - 0x4b400000u * 0x11111111u;
 }
 
 SVL_DEVINL __nv_bfloat162 b2(uint32_t u) { return *reinterpret_cast<__nv_bfloat162*>(&u); }
 SVL_DEVINL uint32_t u2(__nv_bfloat162 x) { return *reinterpret_cast<uint32_t*>(&x); }
 SVL_DEVINL bool finite2(uint32_t u) { return (u & 0x7f80u) != 0x7f80u && (u & 0x7f800000u) != 0x7f800000u; }
+SVL_DEVINL float rcp_approx(float x) {
+  float y;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
 
-// Largest and smallest value of a group and whether it is finite, from a lane's N pairs and the lanes that differ from
-// it in the bits FROM .. TO of their number.
+// The scale (bf16 bits) of a group, and its reciprocal for kv4_code (0: every code is 8), from a lane's N pairs of values
+// and those of the lanes that differ from it in the bits FROM .. TO of their number.
 template <int N, int FROM, int TO>
-SVL_DEVINL uint16_t group_scale(const uint32_t* u, float& inv) {
+SVL_DEVINL uint32_t group_scale(const uint32_t* u, float& inv) {
   __nv_bfloat162 hi = b2(u[0]), lo = hi;
-  bool fine = finite2(u[0]);
 #pragma unroll
   for (int i = 1; i < N; ++i) {
-    hi = __hmax2(hi, b2(u[i]));
-    lo = __hmin2(lo, b2(u[i]));
-    fine = fine && finite2(u[i]);
+    hi = __hmax2_nan(hi, b2(u[i]));
+    lo = __hmin2_nan(lo, b2(u[i]));
   }
-  // both in one word: the largest value and the negative of the smallest
-  uint32_t x = u2(__halves2bfloat162(__hmax(__low2bfloat16(hi), __high2bfloat16(hi)),
-                                     __hneg(__hmin(__low2bfloat16(lo), __high2bfloat16(lo)))));
-  if (!fine) x = 0x7f807f80u;  // +inf beats every value (a NaN would not)
+  // the largest value and the negative of the smallest in one word (a NaN stays one)
+  const uint32_t h = u2(hi), l = u2(lo) ^ 0x80008000u;
+  uint32_t x = u2(__hmax2_nan(b2(__byte_perm(h, l, 0x5410)), b2(__byte_perm(h, l, 0x7632))));
 #pragma unroll
-  for (int off = FROM; off <= TO; off <<= 1) x = u2(__hmax2(b2(x), b2(__shfl_xor_sync(0xffffffffu, x, off))));
-  const float2 f = __bfloat1622float2(b2(x));
-  return kv4_scale(f.x, -f.y, (x & 0x7f80u) != 0x7f80u, inv);
+  for (int off = FROM; off <= TO; off <<= 1) x = u2(__hmax2_nan(b2(x), b2(__shfl_xor_sync(0xffffffffu, x, off))));
+  const float2 f = unpack_bf16x2(x);
+  const float s = f.x >= f.y ? f.x * -0.125f : f.y * 0.125f;
+  const bool zero = !(fabsf(s) >= 1.17549435e-38f);
+  inv = zero ? 0.f : rcp_approx(s);
+  if (!finite2(x)) {
+    inv = 0.f;
+    return 0x7fc0;
+  }
+  return zero ? 0u : __float_as_uint(s) >> 16;
 }
 
-// Four codes as 16 bits, lowest first.
-SVL_DEVINL uint32_t four_codes(float x0, float x1, float x2, float x3, float inv) {
-  float n = kv4_code(x3, inv);
-  n = fmaf(n, 16.f, kv4_code(x2, inv));
-  n = fmaf(n, 16.f, kv4_code(x1, inv));
-  n = fmaf(n, 16.f, kv4_code(x0, inv));
-  // (each n is 8 less than its code: 8 * (1 + 16 + 256 + 4096))
-  return __float_as_uint(n + (8388608.f + 34952.f)) & 0xffffu;
-}
-SVL_DEVINL uint32_t four_codes2(uint32_t a, uint32_t b, float inv) {
-  const float2 x = unpack_bf16x2(a), y = unpack_bf16x2(b);
-  return four_codes(x.x, x.y, y.x, y.y, inv);
+// Codes of four pairs of values.
+SVL_DEVINL uint32_t word_codes(uint32_t a, uint32_t b, uint32_t c, uint32_t d, float inv_lo, float inv_hi) {
+  const float2 x[4] = {unpack_bf16x2(a), unpack_bf16x2(b), unpack_bf16x2(c), unpack_bf16x2(d)};
+  uint32_t n[8];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    n[2 * i] = kv4_code(x[i].x, i < 2 ? inv_lo : inv_hi);
+    n[2 * i + 1] = kv4_code(x[i].y, i < 2 ? inv_lo : inv_hi);
+  }
+  return eight_codes(n);
 }
 
 template <int J>
@@ -166,58 +170,54 @@ __global__ void __launch_bounds__(kRowThreads) kv4_write_kernel(Kv4Rows a) {
   const bool row_in = g >= q.i0 && g < q.i1, even = 2 * t >= q.i0 && 2 * t < q.i1, odd = 2 * t + 1 >= q.i0 && 2 * t + 1 < q.i1;
   uint4 k[J];
   uint2 v[2][J];
+  const __nv_bfloat16* kp = a.k + (q.row + g) * a.k_row + h * DH + 8 * t;
 #pragma unroll
   for (int j = 0; j < J; ++j) {
     k[j] = make_uint4(0, 0, 0, 0);
-    if (row_in) k[j] = *reinterpret_cast<const uint4*>(a.k + (q.row + g) * a.k_row + h * DH + 32 * j + 8 * t);
+    if (row_in) k[j] = *reinterpret_cast<const uint4*>(kp + 32 * j);
   }
+  const __nv_bfloat16* vp = a.v + (q.row + 2 * t) * a.v_row + (h * DH + 4 * g) * a.v_col;
 #pragma unroll
   for (int x = 0; x < 2; ++x)
 #pragma unroll
     for (int j = 0; j < J; ++j) {
       v[x][j] = make_uint2(0, 0);
       if (!(x ? odd : even)) continue;
-      const int64_t c = h * DH + 32 * j + 4 * g;
       if (VT) {
         uint16_t y[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-          y[i] = reinterpret_cast<const uint16_t*>(a.v)[(c + i) * a.v_col + q.row + 2 * t + x];
+        for (int i = 0; i < 4; ++i) y[i] = reinterpret_cast<const uint16_t*>(vp)[(32 * j + i) * a.v_col + x];
         v[x][j] = make_uint2(y[0] | static_cast<uint32_t>(y[1]) << 16, y[2] | static_cast<uint32_t>(y[3]) << 16);
       } else {
-        v[x][j] = *reinterpret_cast<const uint2*>(a.v + (q.row + 2 * t + x) * a.v_row + c);
+        v[x][j] = *reinterpret_cast<const uint2*>(vp + x * a.v_row + 32 * j);
       }
     }
   {
-    uint32_t w4[J];
-    uint16_t s[J];
+    uint32_t w4[J], s[J];
 #pragma unroll
     for (int j = 0; j < J; ++j) {
       const uint32_t u4[4] = {k[j].x, k[j].y, k[j].z, k[j].w};
       float inv;
       s[j] = group_scale<4, 1, 2>(u4, inv);
-      w4[j] = four_codes2(u4[0], u4[1], inv) | four_codes2(u4[2], u4[3], inv) << 16;
+      w4[j] = word_codes(u4[0], u4[1], u4[2], u4[3], inv, inv);
     }
     if (row_in) {
-      store_words<J>(tile + ((quad * 8 + g) * 4 + t) * J * 4, w4);
+      store_words<J>(tile + (quad * 32 + lane) * J * 4, w4);
       if (t == 0) {
         uint32_t* at = reinterpret_cast<uint32_t*>(tile + kv4_k_scales(DH) + (quad * 8 + g) * J * 2);
 #pragma unroll
-        for (int j = 0; j < J; j += 2) at[j / 2] = s[j] | static_cast<uint32_t>(s[j + 1]) << 16;
+        for (int j = 0; j < J; j += 2) at[j / 2] = s[j] | s[j + 1] << 16;
       }
     }
   }
   uint32_t w4[J], s2[J];
 #pragma unroll
   for (int j = 0; j < J; ++j) {
-    w4[j] = s2[j] = 0;
-#pragma unroll
-    for (int x = 0; x < 2; ++x) {
-      const uint32_t u4[2] = {v[x][j].x, v[x][j].y};
-      float inv;
-      s2[j] |= static_cast<uint32_t>(group_scale<2, 4, 16>(u4, inv)) << (16 * x);
-      w4[j] |= four_codes2(u4[0], u4[1], inv) << (16 * x);
-    }
+    const uint32_t e[2] = {v[0][j].x, v[0][j].y}, o[2] = {v[1][j].x, v[1][j].y};
+    float inv_e, inv_o;
+    s2[j] = group_scale<2, 4, 16>(e, inv_e);
+    s2[j] |= group_scale<2, 4, 16>(o, inv_o) << 16;
+    w4[j] = word_codes(e[0], e[1], o[0], o[1], inv_e, inv_o);
   }
   uint8_t* codes = tile + kv4_v_codes(DH) + (quad * 32 + lane) * J * 4;
   uint8_t* scales = tile + kv4_v_scales(DH) + (quad * 4 + t) * J * 4;
@@ -261,36 +261,35 @@ __global__ void __launch_bounds__(kRowThreads) kv4_read_kernel(Kv4Rows a) {
       sk[j] = reinterpret_cast<const uint32_t*>(tile + kv4_k_scales(DH) + (quad * 8 + g) * J * 2)[j];
     load_words<J>(tile + kv4_v_scales(DH) + (quad * 4 + t) * J * 4, sv);
   }
-  auto wanted = [&](int i) { return i >= q.i0 && i < q.i1; };
-  auto in = [&](int i) { return held && q.p + i < a.c.max_len; };  // else zeros
-  if (wanted(g)) {
+  // rows that are wanted, and of them those that the cache has (the others read as 0)
+  const int in = held ? static_cast<int>(q.p + 8 <= a.c.max_len ? 8 : a.c.max_len - q.p) : 0;
+  if (g >= q.i0 && g < q.i1) {
     __nv_bfloat16* out = a.k_out + (q.row + g) * a.k_row + h * DH + 8 * t;
+    const uint32_t keep = g < in ? 0xffffffffu : 0u;
 #pragma unroll
     for (int j = 0; j < J; ++j) {
       const uint32_t s = __byte_perm(sk[j / 2], 0, j & 1 ? 0x3232 : 0x1010);
       uint32_t y[4];  // dimensions i and i + 4
 #pragma unroll
-      for (int i = 0; i < 4; ++i) y[i] = two_values(k[j] >> (4 * i), s);
-      uint4 o = make_uint4(__byte_perm(y[0], y[1], 0x5410), __byte_perm(y[2], y[3], 0x5410),
-                           __byte_perm(y[0], y[1], 0x7632), __byte_perm(y[2], y[3], 0x7632));
-      if (!in(g)) o = make_uint4(0, 0, 0, 0);
-      *reinterpret_cast<uint4*>(out + 32 * j) = o;
+      for (int i = 0; i < 4; ++i) y[i] = two_values(k[j] >> (4 * i), s) & keep;
+      *reinterpret_cast<uint4*>(out + 32 * j) =
+          make_uint4(__byte_perm(y[0], y[1], 0x5410), __byte_perm(y[2], y[3], 0x5410), __byte_perm(y[0], y[1], 0x7632),
+                     __byte_perm(y[2], y[3], 0x7632));
     }
   }
+  const bool even = 2 * t >= q.i0 && 2 * t < q.i1, odd = 2 * t + 1 >= q.i0 && 2 * t + 1 < q.i1;
+  const uint32_t keep = (2 * t < in ? 0xffffu : 0u) | (2 * t + 1 < in ? 0xffff0000u : 0u);
+  __nv_bfloat16* out = a.v_out + (q.row + 2 * t) * a.v_row + h * DH + 4 * g;
 #pragma unroll
   for (int j = 0; j < J; ++j) {
     uint32_t y[4];  // dimension i of rows 2 t and 2 t + 1
 #pragma unroll
-    for (int i = 0; i < 4; ++i) y[i] = two_values(v[j] >> (4 * i), sv[j]);
-#pragma unroll
-    for (int x = 0; x < 2; ++x) {
-      const int i = 2 * t + x;
-      if (!wanted(i)) continue;
-      const uint32_t pick = x ? 0x7632 : 0x5410;
-      uint2 o = make_uint2(__byte_perm(y[0], y[1], pick), __byte_perm(y[2], y[3], pick));
-      if (!in(i)) o = make_uint2(0, 0);
-      *reinterpret_cast<uint2*>(a.v_out + (q.row + i) * a.v_row + h * DH + 32 * j + 4 * g) = o;
-    }
+    for (int i = 0; i < 4; ++i) y[i] = two_values(v[j] >> (4 * i), sv[j]) & keep;
+    if (even)
+      *reinterpret_cast<uint2*>(out + 32 * j) = make_uint2(__byte_perm(y[0], y[1], 0x5410), __byte_perm(y[2], y[3], 0x5410));
+    if (odd)
+      *reinterpret_cast<uint2*>(out + a.v_row + 32 * j) =
+          make_uint2(__byte_perm(y[0], y[1], 0x7632), __byte_perm(y[2], y[3], 0x7632));
   }
 }
 
