@@ -233,14 +233,14 @@ __global__ void __launch_bounds__(kKv4MaxBeams * 32) beam_join_kernel(BeamArgs a
     for (int i = lane; i < p.parts; i += 32) M = fmaxf(M, sums[i].x);
 #pragma unroll
     for (int off = 16; off > 0; off >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, off));
-    double S = 0;
+    float S = 0.f;
     for (int i = lane; i < p.parts; i += 32) {
       const float2 x = sums[i];
-      S += static_cast<double>(x.y) * exp_less(x.x, M);
+      S += x.y * exp_less(x.x, M);
     }
 #pragma unroll
     for (int off = 16; off > 0; off >>= 1) S += __shfl_xor_sync(0xffffffffu, S, off);
-    const bool alive = S > 0 && M < INFINITY;  // (a NaN sum is not)
+    const bool alive = S > 0.f && M < INFINITY;  // (a NaN sum is not)
     uint64_t last = __shfl_sync(0xffffffffu, list, a.K - 1);
 #pragma unroll 4
     for (int i = 1; i < p.parts; ++i) {
@@ -251,7 +251,7 @@ __global__ void __launch_bounds__(kKv4MaxBeams * 32) beam_join_kernel(BeamArgs a
     }
     id = lane;
     if (alive) {
-      const float lse = static_cast<float>(M + log(S));
+      const float lse = M + logf(S);
       id = static_cast<int>(0xffffffffu - static_cast<uint32_t>(list));
       c = from_order_bits(static_cast<uint32_t>(list >> 32)) + (score - lse);
     }
@@ -283,16 +283,19 @@ __global__ void __launch_bounds__(kKv4MaxBeams * 32) beam_join_kernel(BeamArgs a
   }
 }
 
-// Parts of at least 2,048 logits (a chunk for four warps), as many as give each SM two blocks.
+// Parts of a row. 608 blocks (four on each SM) run at once, and a part costs a block as much as some 16,000 logits more:
+// the fewest waves times that, with parts of at least 4,096 logits (a chunk for each warp).
 static BeamParts beam_parts(int S, int W, int V) {
   BeamParts p{};
   const int64_t rows = static_cast<int64_t>(S) * W;
-  int64_t parts = (2 * 152 + rows - 1) / rows;
-  const int64_t most = (V + 2047) / 2048;
-  parts = parts < most ? parts : most;
-  parts = parts < kBeamParts ? parts : kBeamParts;
-  const int64_t len = (V + parts - 1) / parts;
-  p.part = static_cast<int>((len + kChunk - 1) / kChunk * kChunk);
+  const int most = (V + 4095) / 4096 < kBeamParts ? (V + 4095) / 4096 : kBeamParts;
+  int64_t best = 0;
+  for (int n = 1; n <= most; ++n) {
+    const int64_t cost = (rows * n + 607) / 608 * ((V + n - 1) / n + 16000);
+    if (n > 1 && cost >= best) continue;
+    best = cost;
+    p.part = ((V + n - 1) / n + kChunk - 1) / kChunk * kChunk;
+  }
   p.parts = (V - 1) / p.part + 1;
   return p;
 }
