@@ -64,21 +64,24 @@ SVL_DEVINL bool find_unit(const Kv4Rows& a, int64_t u, int lane, Unit& q) {
   return first >= 0 && q.i1 > q.i0;
 }
 
-// The code of x, rint(x / s) + 8 (of two nearest the even one) and at most 15, in the low four bits. inv is 1 / s to within
+// The code of x, rint(x / s) + 8 (of two nearest the even one) and at most 15. inv is 1 / s to within
 // 2^-23 of it, so x * inv is off by less than 2^-19 for |x / s| <= 8. x and s are bf16 numbers: where x / s is not half an
 // integer it is at least 2^-9 from one. Rounded to a multiple of 2^-15 (the last place of 384 = 1.5 * 2^8), x * inv is
-// thus half an integer exactly where x / s is, and on its side of it elsewhere; the second sum (1.5 * 2^23 + 8) rounds it to
+// thus half an integer exactly where x / s is, and on its side of it elsewhere; the second sum (1.5 * 2^23) rounds it to
 // an integer.
-SVL_DEVINL uint32_t kv4_code(float x, float inv) {
+SVL_DEVINL float kv4_code(float x, float inv) {  // less 8, as a float
   const float t = fminf(__fmaf_rn(x, inv, 384.f), 391.f);
-  return __float_as_uint(__fadd_rn(t, 12582920.f - 384.f));
+  return __fadd_rn(__fadd_rn(t, 12582912.f - 384.f), -12582912.f);
 }
-// Eight codes as a word, lowest first (kv4_code's upper bits, 0x4b400000 each, are taken off together).
-SVL_DEVINL uint32_t eight_codes(const uint32_t* n) {
-  uint32_t w = n[7];
-#pragma unroll
-  for (int i = 6; i >= 0; --i) w = w * 16u + n[i];
-  return w - 0x4b400000u * 0x11111111u;
+// Four codes as 16 bits, lowest first. (The sums of products run beside the maxima, masks and shifts, of which there are
+// enough: the kernel is bound by those.)
+SVL_DEVINL uint32_t four_codes(float x0, float x1, float x2, float x3, float inv) {
+  float n = kv4_code(x3, inv);
+  n = __fmaf_rn(n, 16.f, kv4_code(x2, inv));
+  n = __fmaf_rn(n, 16.f, kv4_code(x1, inv));
+  n = __fmaf_rn(n, 16.f, kv4_code(x0, inv));
+  // (8 * (1 + 16 + 256 + 4096) more, above 2^23: an integer's bits)
+  return __float_as_uint(__fadd_rn(n, 8388608.f + 34952.f));
 }
 
 SVL_DEVINL __nv_bfloat162 b2(uint32_t u) { return *reinterpret_cast<__nv_bfloat162*>(&u); }
@@ -90,26 +93,52 @@ SVL_DEVINL float rcp_approx(float x) {
   return y;
 }
 
-// The scale (bf16 bits) of a group, and its reciprocal for kv4_code (0: every code is 8), from a lane's N pairs of values
-// and those of the lanes that differ from it in the bits FROM .. TO of their number.
-template <int N, int FROM, int TO>
-SVL_DEVINL uint32_t group_scale(const uint32_t* u, float& inv) {
+// Largest value and negative of the smallest (halves of a word; a NaN stays one) of a lane's N pairs of values.
+template <int N>
+SVL_DEVINL uint32_t pair_range(const uint32_t* u) {
   __nv_bfloat162 hi = b2(u[0]), lo = hi;
 #pragma unroll
   for (int i = 1; i < N; ++i) {
     hi = __hmax2_nan(hi, b2(u[i]));
     lo = __hmin2_nan(lo, b2(u[i]));
   }
-  // the largest value and the negative of the smallest in one word (a NaN stays one)
   const uint32_t h = u2(hi), l = u2(lo) ^ 0x80008000u;
-  uint32_t x = u2(__hmax2_nan(b2(__byte_perm(h, l, 0x5410)), b2(__byte_perm(h, l, 0x7632))));
+  return u2(__hmax2_nan(b2(__byte_perm(h, l, 0x5410)), b2(__byte_perm(h, l, 0x7632))));
+}
+SVL_DEVINL uint32_t wider(uint32_t x, uint32_t y) { return u2(__hmax2_nan(b2(x), b2(y))); }
+
+// The ranges of N groups (a power of two), of which each of the lanes that differ in the bits LOW .. HIGH of their number
+// has a part: a lane ends up with the whole of one, that whose number the lowest of these bits are. The lanes hand each
+// other the half of the groups that they do not keep.
+template <int N, int LOW, int HIGH>
+SVL_DEVINL uint32_t group_range(uint32_t* r, int lane) {
+  int n = N;
 #pragma unroll
-  for (int off = FROM; off <= TO; off <<= 1) x = u2(__hmax2_nan(b2(x), b2(__shfl_xor_sync(0xffffffffu, x, off))));
-  const float2 f = unpack_bf16x2(x);
+  for (int off = HIGH; off >= LOW; off >>= 1) {
+    if (N <= off / LOW) {
+#pragma unroll
+      for (int i = 0; i < N; ++i) r[i] = wider(r[i], __shfl_xor_sync(0xffffffffu, r[i], off));
+      continue;
+    }
+    n /= 2;
+    const bool upper = lane & off;
+#pragma unroll
+    for (int i = 0; i < N / 2; ++i) {
+      if (i >= n) break;
+      const uint32_t keep = upper ? r[i + n] : r[i], give = upper ? r[i] : r[i + n];
+      r[i] = wider(keep, __shfl_xor_sync(0xffffffffu, give, off));
+    }
+  }
+  return r[0];
+}
+
+// The scale (bf16 bits) of a group of that range, and its reciprocal for kv4_code (0: every code is 8).
+SVL_DEVINL uint32_t group_scale(uint32_t range, float& inv) {
+  const float2 f = unpack_bf16x2(range);
   const float s = f.x >= f.y ? f.x * -0.125f : f.y * 0.125f;
   const bool zero = !(fabsf(s) >= 1.17549435e-38f);
   inv = zero ? 0.f : rcp_approx(s);
-  if (!finite2(x)) {
+  if (!finite2(range)) {
     inv = 0.f;
     return 0x7fc0;
   }
@@ -118,14 +147,8 @@ SVL_DEVINL uint32_t group_scale(const uint32_t* u, float& inv) {
 
 // Codes of four pairs of values.
 SVL_DEVINL uint32_t word_codes(uint32_t a, uint32_t b, uint32_t c, uint32_t d, float inv_lo, float inv_hi) {
-  const float2 x[4] = {unpack_bf16x2(a), unpack_bf16x2(b), unpack_bf16x2(c), unpack_bf16x2(d)};
-  uint32_t n[8];
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    n[2 * i] = kv4_code(x[i].x, i < 2 ? inv_lo : inv_hi);
-    n[2 * i + 1] = kv4_code(x[i].y, i < 2 ? inv_lo : inv_hi);
-  }
-  return eight_codes(n);
+  const float2 x = unpack_bf16x2(a), y = unpack_bf16x2(b), z = unpack_bf16x2(c), w = unpack_bf16x2(d);
+  return __byte_perm(four_codes(x.x, x.y, y.x, y.y, inv_lo), four_codes(z.x, z.y, w.x, w.y, inv_hi), 0x5410);
 }
 
 template <int J>
@@ -193,44 +216,53 @@ __global__ void __launch_bounds__(kRowThreads) kv4_write_kernel(Kv4Rows a) {
       }
     }
   {
-    uint32_t w4[J], s[J];
+    // groups j of row g: lane t ends up with the scale of the group t % J
+    uint32_t r[J];
 #pragma unroll
     for (int j = 0; j < J; ++j) {
       const uint32_t u4[4] = {k[j].x, k[j].y, k[j].z, k[j].w};
-      float inv;
-      s[j] = group_scale<4, 1, 2>(u4, inv);
-      w4[j] = word_codes(u4[0], u4[1], u4[2], u4[3], inv, inv);
+      r[j] = pair_range<4>(u4);
+    }
+    float inv;
+    const uint32_t s = group_scale(group_range<J, 1, 2>(r, lane), inv);
+    uint32_t w4[J];
+#pragma unroll
+    for (int j = 0; j < J; ++j) {
+      const float i = __shfl_sync(0xffffffffu, inv, (lane & ~3) | j);
+      w4[j] = word_codes(k[j].x, k[j].y, k[j].z, k[j].w, i, i);
     }
     if (row_in) {
       store_words<J>(tile + (quad * 32 + lane) * J * 4, w4);
-      if (t == 0) {
-        uint32_t* at = reinterpret_cast<uint32_t*>(tile + kv4_k_scales(DH) + (quad * 8 + g) * J * 2);
-#pragma unroll
-        for (int j = 0; j < J; j += 2) at[j / 2] = s[j] | s[j + 1] << 16;
-      }
+      if (t < J) reinterpret_cast<uint16_t*>(tile + kv4_k_scales(DH))[(quad * 8 + g) * J + t] = static_cast<uint16_t>(s);
     }
   }
-  uint32_t w4[J], s2[J];
+  // groups j of rows 2 t (number 2 j) and 2 t + 1 (2 j + 1): lane g ends up with the scale of number g % (2 J)
+  uint32_t r[2 * J];
+#pragma unroll
+  for (int j = 0; j < J; ++j)
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+      const uint32_t u4[2] = {v[x][j].x, v[x][j].y};
+      r[2 * j + x] = pair_range<2>(u4);
+    }
+  float inv;
+  const uint32_t s = group_scale(group_range<2 * J, 4, 16>(r, lane), inv);
+  uint32_t w4[J];
 #pragma unroll
   for (int j = 0; j < J; ++j) {
-    const uint32_t e[2] = {v[0][j].x, v[0][j].y}, o[2] = {v[1][j].x, v[1][j].y};
-    float inv_e, inv_o;
-    s2[j] = group_scale<2, 4, 16>(e, inv_e);
-    s2[j] |= group_scale<2, 4, 16>(o, inv_o) << 16;
-    w4[j] = word_codes(e[0], e[1], o[0], o[1], inv_e, inv_o);
+    const float e = __shfl_sync(0xffffffffu, inv, 8 * j + t), o = __shfl_sync(0xffffffffu, inv, 8 * j + 4 + t);
+    w4[j] = word_codes(v[0][j].x, v[0][j].y, v[1][j].x, v[1][j].y, e, o);
   }
   uint8_t* codes = tile + kv4_v_codes(DH) + (quad * 32 + lane) * J * 4;
-  uint8_t* scales = tile + kv4_v_scales(DH) + (quad * 4 + t) * J * 4;
   if (even && odd) {
     store_words<J>(codes, w4);
-    if (g == 0) store_words<J>(scales, s2);
   } else if (even || odd) {  // the other row of the pair stays
 #pragma unroll
-    for (int j = 0; j < J; ++j) {
+    for (int j = 0; j < J; ++j)
       reinterpret_cast<uint16_t*>(codes)[2 * j + odd] = static_cast<uint16_t>(w4[j] >> (16 * odd));
-      if (g == 0) reinterpret_cast<uint16_t*>(scales)[2 * j + odd] = static_cast<uint16_t>(s2[j] >> (16 * odd));
-    }
   }
+  if (g < 2 * J && (g & 1 ? odd : even))
+    reinterpret_cast<uint16_t*>(tile + kv4_v_scales(DH))[(quad * 4 + t) * 2 * J + g] = static_cast<uint16_t>(s);
 }
 
 // The lowest nibble of each half, less 8, times the halves of s, as bf16 (the product rounded once).
@@ -261,30 +293,40 @@ __global__ void __launch_bounds__(kRowThreads) kv4_read_kernel(Kv4Rows a) {
       sk[j] = reinterpret_cast<const uint32_t*>(tile + kv4_k_scales(DH) + (quad * 8 + g) * J * 2)[j];
     load_words<J>(tile + kv4_v_scales(DH) + (quad * 4 + t) * J * 4, sv);
   }
-  // rows that are wanted, and of them those that the cache has (the others read as 0)
+  // rows that the cache does not have read as 0
   const int in = held ? static_cast<int>(q.p + 8 <= a.c.max_len ? 8 : a.c.max_len - q.p) : 0;
+  if (in < 8) {
+    const uint32_t keep = (2 * t < in ? 0xffffu : 0u) | (2 * t + 1 < in ? 0xffff0000u : 0u);
+#pragma unroll
+    for (int j = 0; j < J; ++j) {
+      if (g >= in) {
+        k[j] = 0x88888888u;
+        sk[j / 2] = 0;
+      }
+      v[j] = (v[j] & keep) | (0x88888888u & ~keep);
+      sv[j] &= keep;
+    }
+  }
   if (g >= q.i0 && g < q.i1) {
     __nv_bfloat16* out = a.k_out + (q.row + g) * a.k_row + h * DH + 8 * t;
-    const uint32_t keep = g < in ? 0xffffffffu : 0u;
 #pragma unroll
     for (int j = 0; j < J; ++j) {
       const uint32_t s = __byte_perm(sk[j / 2], 0, j & 1 ? 0x3232 : 0x1010);
       uint32_t y[4];  // dimensions i and i + 4
 #pragma unroll
-      for (int i = 0; i < 4; ++i) y[i] = two_values(k[j] >> (4 * i), s) & keep;
+      for (int i = 0; i < 4; ++i) y[i] = two_values(k[j] >> (4 * i), s);
       *reinterpret_cast<uint4*>(out + 32 * j) =
           make_uint4(__byte_perm(y[0], y[1], 0x5410), __byte_perm(y[2], y[3], 0x5410), __byte_perm(y[0], y[1], 0x7632),
                      __byte_perm(y[2], y[3], 0x7632));
     }
   }
   const bool even = 2 * t >= q.i0 && 2 * t < q.i1, odd = 2 * t + 1 >= q.i0 && 2 * t + 1 < q.i1;
-  const uint32_t keep = (2 * t < in ? 0xffffu : 0u) | (2 * t + 1 < in ? 0xffff0000u : 0u);
   __nv_bfloat16* out = a.v_out + (q.row + 2 * t) * a.v_row + h * DH + 4 * g;
 #pragma unroll
   for (int j = 0; j < J; ++j) {
     uint32_t y[4];  // dimension i of rows 2 t and 2 t + 1
 #pragma unroll
-    for (int i = 0; i < 4; ++i) y[i] = two_values(v[j] >> (4 * i), sv[j]) & keep;
+    for (int i = 0; i < 4; ++i) y[i] = two_values(v[j] >> (4 * i), sv[j]);
     if (even)
       *reinterpret_cast<uint2*>(out + 32 * j) = make_uint2(__byte_perm(y[0], y[1], 0x5410), __byte_perm(y[2], y[3], 0x5410));
     if (odd)
