@@ -175,9 +175,12 @@ SVL_DEVINL float bf16_hi(uint32_t u) { return __uint_as_float(u & 0xffff0000u); 
 SVL_DEVINL __nv_bfloat162 as_bf16x2(uint32_t u) { return *reinterpret_cast<__nv_bfloat162*>(&u); }
 SVL_DEVINL uint32_t bits_of(__nv_bfloat162 x) { return *reinterpret_cast<uint32_t*>(&x); }
 constexpr uint32_t kLow = 0x000f000fu, kHigh = 0x00f000f0u;
-// The lowest nibble of each half of a word, less 8, as bf16.
-SVL_DEVINL uint32_t v_codes(uint32_t x) {
-  return bits_of(__hadd2(as_bf16x2((x & kLow) | 0x43004300u), as_bf16x2(0xc308c308u)));  // 128 + n, -136
+// The lowest nibble of each half of a word, less 8, as bf16. `k128`: 128 in both halves, in a register (with a second
+// constant, mask and sum would take an instruction each).
+SVL_DEVINL uint32_t v_codes(uint32_t x, uint32_t k128) {
+  uint32_t y;
+  asm("lop3.b32 %0, %1, 0x000f000f, %2, 0xea;" : "=r"(y) : "r"(x), "r"(k128));  // 128 + n
+  return bits_of(__hadd2(as_bf16x2(y), as_bf16x2(0xc308c308u)));                // -136
 }
 SVL_DEVINL uint32_t bits_below(int n) { return n <= 0 ? 0u : (n >= 32 ? ~0u : (1u << n) - 1u); }
 SVL_DEVINL float max_quads(float x) {  // over the eight lanes that share lane % 4
@@ -209,11 +212,11 @@ SVL_DEVINL Words<J> lds_words(const uint8_t* p) {
 }
 
 // The codes of two words (of pairs of rows 8 apart) as operands, nibble by nibble.
-SVL_DEVINL void v_operands(uint32_t v0, uint32_t v1, uint32_t (*c)[2]) {
+SVL_DEVINL void v_operands(uint32_t v0, uint32_t v1, uint32_t k128, uint32_t (*c)[2]) {
 #pragma unroll
   for (int k = 0; k < 4; ++k) {
-    c[k][0] = v_codes(v0 >> (4 * k));
-    c[k][1] = v_codes(v1 >> (4 * k));
+    c[k][0] = v_codes(v0 >> (4 * k), k128);
+    c[k][1] = v_codes(v1 >> (4 * k), k128);
   }
 }
 
@@ -222,7 +225,7 @@ SVL_DEVINL void v_operands(uint32_t v0, uint32_t v1, uint32_t (*c)[2]) {
 // does not count whatever its scale.
 template <int J, bool MASK>
 SVL_DEVINL void weighted_rows(float (*o)[2][4], const uint32_t* hi, const uint32_t* lo, const Words<J>& u0,
-                              const Words<J>& u1, const Words<J>& v0, const Words<J>& v1) {
+                              const Words<J>& u1, const Words<J>& v0, const Words<J>& v1, uint32_t k128) {
   uint32_t keep[2];
   if (MASK) {
 #pragma unroll
@@ -245,7 +248,7 @@ SVL_DEVINL void weighted_rows(float (*o)[2][4], const uint32_t* hi, const uint32
       }
     }
     uint32_t c[4][2];
-    v_operands(v0.w[j], v1.w[j], c);
+    v_operands(v0.w[j], v1.w[j], k128, c);
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
       mma16816_bf16(o[j][k], c[k][0], c[k + 2][0], c[k][1], c[k + 2][1], ph[0], ph[1]);
@@ -380,6 +383,8 @@ __global__ void __launch_bounds__(NW * 32, 1) kv4_attn_kernel(AttnParams p, int 
     float qsum[MODE == 0 ? 1 : J][NT], factor[NT], m[NT], l[NT], o[J][2][4];
     int end[NT], low[NT];
     int stage = 0, col0 = 0, whole_lo = 0, whole_hi = 0;
+    uint32_t k128;
+    asm volatile("mov.b32 %0, 0x43004300;" : "=r"(k128));
     bool started = false;
     for (int i = 0; i < n; ++i) {
       const int4 meta = tile_meta[warp][stage];
@@ -599,7 +604,7 @@ __global__ void __launch_bounds__(NW * 32, 1) kv4_attn_kernel(AttnParams p, int 
 #pragma unroll
           for (int j = 0; j < J; ++j) {
             uint32_t c[4][2];
-            v_operands(v0.w[j], v1.w[j], c);
+            v_operands(v0.w[j], v1.w[j], k128, c);
             mma16816_bf16(o[j][0], c[0][0], c[2][0], c[0][1], c[2][1], b[0], b[1]);
             mma16816_bf16(o[j][1], c[1][0], c[3][0], c[1][1], c[3][1], b[0], b[1]);
           }
@@ -626,7 +631,7 @@ __global__ void __launch_bounds__(NW * 32, 1) kv4_attn_kernel(AttnParams p, int 
               b[r] = transpose8(pack_bf16x2(hi, x - hi));
             }
             uint32_t c[4][2];
-            v_operands(v0.w[j], v1.w[j], c);
+            v_operands(v0.w[j], v1.w[j], k128, c);
             mma16816_bf16(o[j][0], c[0][0], c[2][0], c[0][1], c[2][1], b[0], b[1]);
             mma16816_bf16(o[j][1], c[1][0], c[3][0], c[1][1], c[3][1], b[0], b[1]);
           }
@@ -647,8 +652,8 @@ __global__ void __launch_bounds__(NW * 32, 1) kv4_attn_kernel(AttnParams p, int 
           }
           const Words<J> u0 = lds_words<J>(tile + kv4_v_scales(DH) + (8 * h + t) * J * 4);
           const Words<J> u1 = lds_words<J>(tile + kv4_v_scales(DH) + (8 * h + 4 + t) * J * 4);
-          if (whole) weighted_rows<J, false>(o, hi, lo, u0, u1, v0, v1);
-          else weighted_rows<J, true>(o, hi, lo, u0, u1, v0, v1);
+          if (whole) weighted_rows<J, false>(o, hi, lo, u0, u1, v0, v1, k128);
+          else weighted_rows<J, true>(o, hi, lo, u0, u1, v0, v1, k128);
         }
       }
 
