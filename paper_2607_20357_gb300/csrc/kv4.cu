@@ -266,8 +266,10 @@ __global__ void __launch_bounds__(kRowThreads) kv4_write_kernel(Kv4Rows a) {
 }
 
 // The lowest nibble of each half, less 8, times the halves of s, as bf16 (the product rounded once).
-SVL_DEVINL uint32_t two_values(uint32_t x, uint32_t s) {
-  return u2(__hmul2(__hadd2(b2((x & 0x000f000fu) | 0x43004300u), b2(0xc308c308u)), b2(s)));
+SVL_DEVINL uint32_t two_values(uint32_t x, uint32_t s, uint32_t k128) {
+  uint32_t y;  // 128 + n (k128: 128 in both halves, in a register), less 136
+  asm("lop3.b32 %0, %1, 0x000f000f, %2, 0xea;" : "=r"(y) : "r"(x), "r"(k128));
+  return u2(__hmul2(__hadd2(b2(y), b2(0xc308c308u)), b2(s)));
 }
 
 // A warp per (unit, KV head), as for writing; positions that the cache does not have read as 0.
@@ -280,6 +282,8 @@ __global__ void __launch_bounds__(kRowThreads) kv4_read_kernel(Kv4Rows a) {
   if (h >= a.c.kv || !find_unit(a, blockIdx.x, lane, q)) return;
   const int g = lane >> 2, t = lane & 3;
   const bool held = q.p >= 0 && q.p < a.c.max_len;
+  uint32_t k128;
+  asm volatile("mov.b32 %0, 0x43004300;" : "=r"(k128));
   uint32_t k[J], v[J], sk[J / 2], sv[J];
 #pragma unroll
   for (int j = 0; j < J; ++j) k[j] = v[j] = sk[j / 2] = sv[j] = 0;
@@ -314,7 +318,7 @@ __global__ void __launch_bounds__(kRowThreads) kv4_read_kernel(Kv4Rows a) {
       const uint32_t s = __byte_perm(sk[j / 2], 0, j & 1 ? 0x3232 : 0x1010);
       uint32_t y[4];  // dimensions i and i + 4
 #pragma unroll
-      for (int i = 0; i < 4; ++i) y[i] = two_values(k[j] >> (4 * i), s);
+      for (int i = 0; i < 4; ++i) y[i] = two_values(k[j] >> (4 * i), s, k128);
       *reinterpret_cast<uint4*>(out + 32 * j) =
           make_uint4(__byte_perm(y[0], y[1], 0x5410), __byte_perm(y[2], y[3], 0x5410), __byte_perm(y[0], y[1], 0x7632),
                      __byte_perm(y[2], y[3], 0x7632));
@@ -326,7 +330,7 @@ __global__ void __launch_bounds__(kRowThreads) kv4_read_kernel(Kv4Rows a) {
   for (int j = 0; j < J; ++j) {
     uint32_t y[4];  // dimension i of rows 2 t and 2 t + 1
 #pragma unroll
-    for (int i = 0; i < 4; ++i) y[i] = two_values(v[j] >> (4 * i), sv[j]);
+    for (int i = 0; i < 4; ++i) y[i] = two_values(v[j] >> (4 * i), sv[j], k128);
     if (even)
       *reinterpret_cast<uint2*>(out + 32 * j) = make_uint2(__byte_perm(y[0], y[1], 0x5410), __byte_perm(y[2], y[3], 0x5410));
     if (odd)
