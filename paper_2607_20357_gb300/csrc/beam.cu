@@ -63,6 +63,18 @@ SVL_DEVINL uint32_t warp_sort(uint32_t x, int lane) {
   return x;
 }
 
+// The 32 largest of two lists (descending over the lanes), descending.
+SVL_DEVINL uint64_t list_merge(uint64_t a, uint64_t b, int lane) {
+  const uint64_t r = __shfl_xor_sync(0xffffffffu, b, 31);
+  uint64_t x = a > r ? a : r;
+#pragma unroll
+  for (int step = 16; step > 0; step >>= 1) {
+    const uint64_t y = __shfl_xor_sync(0xffffffffu, x, step);
+    x = ((lane & step) == 0) == (x > y) ? x : y;
+  }
+  return x;
+}
+
 // s + t = a + b exactly
 SVL_DEVINL void two_sum(float a, float b, float& s, float& t) {
   s = __fadd_rn(a, b);
@@ -187,17 +199,14 @@ __global__ void __launch_bounds__(kBeamThreads) beam_part_kernel(BeamArgs a, Bea
       ws[warp] = s;
     }
   }
-  if (lane < a.K) lists[warp][lane] = list;
-  __syncthreads();
-  if (warp > 0) return;
-  if (lane >= a.K) list = 0;
-  last = __shfl_sync(0xffffffffu, list, a.K - 1);
-  for (int w = 1; w < kBeamWarps; ++w) {
-    const uint64_t key = lane < a.K ? lists[w][lane] : 0;
-    if (!__any_sync(0xffffffffu, key > last)) continue;
-    list_insert(list, key, key > last, a.K, lane);
-    last = __shfl_sync(0xffffffffu, list, a.K - 1);
+  if (lane >= a.K) list = 0;  // (of what fell out, nothing is among the best)
+#pragma unroll
+  for (int n = kBeamWarps / 2; n > 0; n >>= 1) {
+    if (warp >= n && warp < 2 * n) lists[warp][lane] = list;
+    __syncthreads();
+    if (warp < n) list = list_merge(list, lists[warp + n][lane], lane);
   }
+  if (warp > 0) return;
   const int64_t at = static_cast<int64_t>(row) * p.parts + part;
   if (lane < a.K) p.keys[at * a.K + lane] = list;
   if (lane == 0) {
@@ -246,7 +255,7 @@ __global__ void __launch_bounds__(kKv4MaxBeams * 32) beam_join_kernel(BeamArgs a
     for (int i = 1; i < p.parts; ++i) {
       const uint64_t key = lane < a.K ? keys[static_cast<int64_t>(i) * a.K + lane] : 0;
       if (!__any_sync(0xffffffffu, key > last)) continue;
-      list_insert(list, key, key > last, a.K, lane);
+      list = list_merge(list, key, lane);
       last = __shfl_sync(0xffffffffu, list, a.K - 1);
     }
     id = lane;
@@ -283,7 +292,7 @@ __global__ void __launch_bounds__(kKv4MaxBeams * 32) beam_join_kernel(BeamArgs a
   }
 }
 
-// Parts of a row. 608 blocks (four on each SM) run at once, and a part costs a block as much as some 16,000 logits more:
+// Parts of a row. 608 blocks (four on each SM) run at once, and a part costs a block as much as some 8,000 logits more:
 // the fewest waves times that, with parts of at least 4,096 logits (a chunk for each warp).
 static BeamParts beam_parts(int S, int W, int V) {
   BeamParts p{};
@@ -291,7 +300,7 @@ static BeamParts beam_parts(int S, int W, int V) {
   const int most = (V + 4095) / 4096 < kBeamParts ? (V + 4095) / 4096 : kBeamParts;
   int64_t best = 0;
   for (int n = 1; n <= most; ++n) {
-    const int64_t cost = (rows * n + 607) / 608 * ((V + n - 1) / n + 16000);
+    const int64_t cost = (rows * n + 607) / 608 * ((V + n - 1) / n + 8000);
     if (n > 1 && cost >= best) continue;
     best = cost;
     p.part = ((V + n - 1) / n + kChunk - 1) / kChunk * kChunk;
