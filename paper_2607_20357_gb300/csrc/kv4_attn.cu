@@ -189,7 +189,6 @@ SVL_DEVINL float max_quads(float x) {  // over the eight lanes that share lane %
   return x;
 }
 
-
 template <int J>
 struct Words {
   uint32_t w[J];
@@ -220,18 +219,13 @@ SVL_DEVINL void v_operands(uint32_t v0, uint32_t v1, uint32_t k128, uint32_t (*c
   }
 }
 
-// O^T += V^T P over 16 positions, up to eight columns: weights hi + lo of the positions 2 t, 2 t + 1 ([0]) and those + 8 ([1]) of the operand's
-// column, V's words and scales of the same. MASK: a weight of 0 is a position that the column does not see, which
-// does not count whatever its scale.
+// O^T += V^T P over 16 positions, up to eight columns: weights hi + lo of the positions 2 t, 2 t + 1 ([0]) and those
+// + 8 ([1]) of the operand's column, V's words and scales of the same. MASK: `keep` is 0 at the positions that the column
+// does not see, which do not count whatever their scales.
 template <int J, bool MASK>
-SVL_DEVINL void weighted_rows(float (*o)[2][4], const uint32_t* hi, const uint32_t* lo, const Words<J>& u0,
-                              const Words<J>& u1, const Words<J>& v0, const Words<J>& v1, uint32_t k128) {
-  uint32_t keep[2];
-  if (MASK) {
-#pragma unroll
-    for (int x = 0; x < 2; ++x)
-      keep[x] = (hi[x] & 0xffffu ? 0xffffu : 0u) | (hi[x] & 0xffff0000u ? 0xffff0000u : 0u);
-  }
+SVL_DEVINL void weighted_rows(float (*o)[2][4], const uint32_t* hi, const uint32_t* lo, const uint32_t* keep,
+                              const Words<J>& u0, const Words<J>& u1, const Words<J>& v0, const Words<J>& v1,
+                              uint32_t k128) {
 #pragma unroll
   for (int j = 0; j < J; ++j) {
     // times the scales: the rounded product, and what it leaves
@@ -282,12 +276,12 @@ SVL_DEVINL void add_scaled(float4& o, float f, float4 x) {
 // The weight 2^(m - M) l of a part beside the others' maximum M (0: it saw nothing).
 SVL_DEVINL float part_weight(float m, float l, float M) { return l == 0.f ? 0.f : l * ex2(m - M); }
 
-// NW: warps, NS: stages of a warp's ring. MODE: 0 for items of one column, 1 for up to four, 2 for up to eight. In modes 1 and 2 column
-// c is column 2 (c % 4) + c / 4 of the operands, so that a lane's accumulators hold columns t (x = 0) and 4 + t (x = 1); in
-// mode 1 the other operand column of a pair holds the lower halves of the scaled weights. In mode 0 the operands' columns
-// 2 j and 2 j + 1 belong to group j of 32 dimensions: of q they hold that group alone, so that one chain of products gives
-// lane t the sum of group t; of the weights the halves scaled for that group, so that one operand serves all
-// dimensions, of whose sums lane t holds those of group t.
+// NW: warps, NS: stages of a warp's ring. MODE: 0 for items of one column, 1 for up to four, 2 for up to eight.
+// In modes 1 and 2 column c is column 2 (c % 4) + c / 4 of the operands, so that a lane's accumulators hold columns t
+// (x = 0) and 4 + t (x = 1); in mode 1 the other operand column of a pair holds the lower halves of the scaled weights.
+// In mode 0 the operands' columns 2 j and 2 j + 1 belong to group j of 32 dimensions: of q they hold that group alone, so
+// that one chain of products gives lane t the sum of group t; of the weights the halves scaled for that group, so that
+// one operand serves all dimensions, of whose sums lane t holds those of group t.
 template <int DH, int NS, int NW, int MODE>
 __global__ void __launch_bounds__(NW * 32, 1) kv4_attn_kernel(AttnParams p, int slot_floats) {
   constexpr int J = DH / 32, TB = kv4_tile_bytes(DH), NT = MODE == 2 ? 2 : 1;
@@ -512,7 +506,7 @@ __global__ void __launch_bounds__(NW * 32, 1) kv4_attn_kernel(AttnParams p, int 
             s[h][r][0] = x + __shfl_xor_sync(0xffffffffu, x, 2);
           }
         } else {
-        const uint8_t* sk = tile + kv4_k_scales(DH) + (16 * h + g) * J * 2;
+          const uint8_t* sk = tile + kv4_k_scales(DH) + (16 * h + g) * J * 2;
           uint32_t ka[J / 2], kb[J / 2];
 #pragma unroll
           for (int k = 0; k < J / 2; ++k) {
@@ -542,14 +536,17 @@ __global__ void __launch_bounds__(NW * 32, 1) kv4_attn_kernel(AttnParams p, int 
           s[h][1][x] *= factor[x];
         }
       }
+      uint32_t sight[NT];  // bit: the column sees the position of this lane's row 8 k + g, at 8 k
+#pragma unroll
+      for (int x = 0; x < NT; ++x) sight[x] = ~0u;
       if (!whole) {
 #pragma unroll
         for (int x = 0; x < NT; ++x) {
-          const uint32_t sight =
-              (bits_below(end[x] - p0) & ~bits_below(low[x] - p0)) | bits_below(min(a.sinks, end[x]) - p0);
+          sight[x] = (bits_below(end[x] - p0) & ~bits_below(low[x] - p0)) | bits_below(min(a.sinks, end[x]) - p0);
+          sight[x] >>= g;
 #pragma unroll
           for (int k = 0; k < 4; ++k)
-            if (!(sight >> (8 * k + g) & 1u)) s[k >> 1][k & 1][x] = -INFINITY;
+            if (!(sight[x] >> (8 * k) & 1u)) s[k >> 1][k & 1][x] = -INFINITY;
         }
       }
       // the running maximum moves when it is passed by more than a factor of two
@@ -597,7 +594,7 @@ __global__ void __launch_bounds__(NW * 32, 1) kv4_attn_kernel(AttnParams p, int 
               const uint32_t u = reinterpret_cast<const uint16_t*>(tile + kv4_v_scales(DH))[at];
               x = w * bf16_lo(u);
             }
-            if (!whole && w == 0.f) x = 0.f;  // what the column does not see does not count, whatever its scale
+            if (!whole && !(sight[0] >> (16 * h + 8 * r) & 1u)) x = 0.f;  // not in sight: its scale does not matter
             const float hi = __uint_as_float(__float_as_uint(x) & 0xffff0000u);
             b[r] = transpose8(pack_bf16x2(hi, x - hi));
           }
@@ -616,7 +613,7 @@ __global__ void __launch_bounds__(NW * 32, 1) kv4_attn_kernel(AttnParams p, int 
             w[r] = ex2(s[h][r][0] - (m[0] == -INFINITY ? 0.f : m[0]));
             l[0] += w[r];
             u[r] = lds_words<J>(tile + kv4_v_scales(DH) + (8 * h + 4 * r + (g >> 1)) * J * 4);
-            if (!whole && w[r] == 0.f) {  // what a column does not see does not count, whatever its scale
+            if (!whole && !(sight[0] >> (16 * h + 8 * r) & 1u)) {  // not in sight: as above
 #pragma unroll
               for (int j = 0; j < J; ++j) u[r].w[j] = 0;
             }
@@ -637,7 +634,7 @@ __global__ void __launch_bounds__(NW * 32, 1) kv4_attn_kernel(AttnParams p, int 
           }
         } else {
           // weights as pairs of bf16 numbers, positions 2 t, 2 t + 1 and those + 8 of the operand's column
-          uint32_t hi[2], lo[2];
+          uint32_t hi[2], lo[2], keep[2];
 #pragma unroll
           for (int r = 0; r < 2; ++r) {
             float w[2];
@@ -649,11 +646,15 @@ __global__ void __launch_bounds__(NW * 32, 1) kv4_attn_kernel(AttnParams p, int 
             const uint32_t u = pack_bf16x2(w[0], w[1]);
             hi[r] = transpose8(u);
             lo[r] = transpose8(pack_bf16x2(w[0] - bf16_lo(u), w[1] - bf16_hi(u)));
+            if (!whole) {
+              const int k = 16 * h + 8 * r;
+              keep[r] = transpose8((sight[0] >> k & 1u ? 0xffffu : 0u) | (sight[NT - 1] >> k & 1u ? 0xffff0000u : 0u));
+            }
           }
           const Words<J> u0 = lds_words<J>(tile + kv4_v_scales(DH) + (8 * h + t) * J * 4);
           const Words<J> u1 = lds_words<J>(tile + kv4_v_scales(DH) + (8 * h + 4 + t) * J * 4);
-          if (whole) weighted_rows<J, false>(o, hi, lo, u0, u1, v0, v1, k128);
-          else weighted_rows<J, true>(o, hi, lo, u0, u1, v0, v1, k128);
+          if (whole) weighted_rows<J, false>(o, hi, lo, keep, u0, u1, v0, v1, k128);
+          else weighted_rows<J, true>(o, hi, lo, keep, u0, u1, v0, v1, k128);
         }
       }
 
