@@ -102,7 +102,7 @@ __global__ void __launch_bounds__(kBeamThreads) beam_part_kernel(BeamArgs a, Bea
   __shared__ volatile uint32_t bars[kBeamWarps];  // of each warp, `each` of its logits are no less (as ordered bits)
   pdl_begin(false);
   const int row = blockIdx.x, part = blockIdx.y, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  if (a.finished && a.finished[row]) return;
+  const bool fin = a.finished && a.finished[row];
   const float* x = a.logits + row * a.ld;
   const int v0 = part * p.part, v1 = min(a.V, v0 + p.part);
   float m = -INFINITY, s = 0.f, rest = 0.f;
@@ -133,8 +133,9 @@ __global__ void __launch_bounds__(kBeamThreads) beam_part_kernel(BeamArgs a, Bea
   };
   float y[16];
   int c = v0 + warp * kChunk;
+  if (c < v1) load(c, y);  // (on its way before it is known whether the beam is finished)
+  if (fin) return;
   if (c < v1) {
-    load(c, y);
     float top = y[0];
 #pragma unroll
     for (int k = 1; k < 16; ++k) top = fmaxf(top, y[k]);
@@ -227,21 +228,26 @@ __global__ void __launch_bounds__(kKv4MaxBeams * 32) beam_join_kernel(BeamArgs a
   pdl_begin(false);
   const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
   const int row = blockIdx.x * a.W + w;
+  // all that has to be read is on its way at once (a finished beam's parts hold whatever, and do not count)
+  const float2* sums = p.sums + static_cast<int64_t>(row) * p.parts;
+  const uint64_t* keys = p.keys + static_cast<int64_t>(row) * p.parts * a.K;
+  constexpr int kEarly = 8;
+  uint64_t early[kEarly];
+#pragma unroll
+  for (int i = 0; i < kEarly; ++i) early[i] = i < p.parts && lane < a.K ? keys[i * a.K + lane] : 0;
   const float score = a.scores[row];
   const bool fin = a.finished && a.finished[row];
+  float M = -INFINITY;
+  for (int i = lane; i < p.parts; i += 32) M = fmaxf(M, sums[i].x);
+#pragma unroll
+  for (int off = 16; off > 0; off >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, off));
   if (lane == 0) done[w] = fin;
   float c = -INFINITY;
-  int id = a.eos;
+  int id = lane;
   if (fin) {
     if (lane == 0) c = score;
+    id = a.eos;
   } else {
-    const float2* sums = p.sums + static_cast<int64_t>(row) * p.parts;
-    const uint64_t* keys = p.keys + static_cast<int64_t>(row) * p.parts * a.K;
-    uint64_t list = lane < a.K ? keys[lane] : 0;
-    float M = -INFINITY;
-    for (int i = lane; i < p.parts; i += 32) M = fmaxf(M, sums[i].x);
-#pragma unroll
-    for (int off = 16; off > 0; off >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, off));
     float S = 0.f;
     for (int i = lane; i < p.parts; i += 32) {
       const float2 x = sums[i];
@@ -249,17 +255,17 @@ __global__ void __launch_bounds__(kKv4MaxBeams * 32) beam_join_kernel(BeamArgs a
     }
 #pragma unroll
     for (int off = 16; off > 0; off >>= 1) S += __shfl_xor_sync(0xffffffffu, S, off);
-    const bool alive = S > 0.f && M < INFINITY;  // (a NaN sum is not)
-    uint64_t last = __shfl_sync(0xffffffffu, list, a.K - 1);
-#pragma unroll 4
-    for (int i = 1; i < p.parts; ++i) {
-      const uint64_t key = lane < a.K ? keys[static_cast<int64_t>(i) * a.K + lane] : 0;
-      if (!__any_sync(0xffffffffu, key > last)) continue;
+    uint64_t list = early[0], last = __shfl_sync(0xffffffffu, list, a.K - 1);
+    auto join = [&](uint64_t key) {
+      if (!__any_sync(0xffffffffu, key > last)) return;
       list = list_merge(list, key, lane);
       last = __shfl_sync(0xffffffffu, list, a.K - 1);
-    }
-    id = lane;
-    if (alive) {
+    };
+#pragma unroll
+    for (int i = 1; i < kEarly; ++i) join(early[i]);
+#pragma unroll 4
+    for (int i = kEarly; i < p.parts; ++i) join(lane < a.K ? keys[static_cast<int64_t>(i) * a.K + lane] : 0);
+    if (S > 0.f && M < INFINITY) {  // (a NaN sum is not)
       const float lse = M + logf(S);
       id = static_cast<int>(0xffffffffu - static_cast<uint32_t>(list));
       c = from_order_bits(static_cast<uint32_t>(list >> 32)) + (score - lse);
