@@ -804,20 +804,30 @@ __global__ void __launch_bounds__(kMergeThreads) kv4_merge_kernel(AttnParams p, 
   __shared__ float warp_m[kWarps], warp_l[kWarps];
   __shared__ float4 sum[kWarps][32];
   const int c = blockIdx.x, col = blockIdx.y, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int d = 4 * lane;
   pdl_begin(p.a.late);
+  // each warp's first part is read beside the meta that says whether it belongs to the item
+  const float* first =
+      p.part + (static_cast<size_t>(min(c + warp, static_cast<int>(gridDim.x) - 1)) * 2 + (warp == 0)) * slot_floats;
+  float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+  if (d < DH) o = *reinterpret_cast<const float4*>(first + col * DH + d);
+  float m = first[p.ncols * DH + 2 * col], l = first[p.ncols * DH + 2 * col + 1];
   const int4 it = p.meta[c];
   const int c0 = p.col_tiles == 1 ? 0 : it.y % p.col_tiles * kCols, n = it.w;
   if (it.x < 0 || c0 + col >= p.columns) return;
-  float m = -INFINITY, l = 0.f;
-  float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-  const int d = 4 * lane;
+  // (o is kept with its weight l: sums of weighted outputs)
+  o = make_float4(o.x * l, o.y * l, o.z * l, o.w * l);
+  if (warp >= n) {
+    m = -INFINITY;
+    l = 0.f;
+    o = make_float4(0.f, 0.f, 0.f, 0.f);
+  }
 #pragma unroll 4
-  for (int i = warp; i < n; i += kWarps) {
-    const float* x = p.part + (static_cast<size_t>(c + i) * 2 + (i == 0)) * slot_floats;
+  for (int i = warp + kWarps; i < n; i += kWarps) {
+    const float* x = p.part + static_cast<size_t>(c + i) * 2 * slot_floats;
     const float xm = x[p.ncols * DH + 2 * col], xl = x[p.ncols * DH + 2 * col + 1];
     const float4 y = d < DH ? *reinterpret_cast<const float4*>(x + col * DH + d) : o;
     const float mn = fmaxf(m, xm), old = part_weight(m, l, mn), f = part_weight(xm, xl, mn);
-    // (o is kept with its weight l: sums of weighted outputs)
     const float down = l == 0.f ? 0.f : ex2(m - mn);
     o = make_float4(o.x * down, o.y * down, o.z * down, o.w * down);
     add_scaled(o, f, y);
