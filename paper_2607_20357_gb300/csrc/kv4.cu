@@ -65,16 +65,16 @@ SVL_DEVINL bool find_unit(const Kv4Rows& a, int64_t u, int lane, Unit& q) {
 }
 
 // The code of x, rint(x / s) + 8 (of two nearest the even one) and at most 15. inv is 1 / s to within
-// 2^-23 of it, so x * inv is off by less than 2^-19 for |x / s| <= 8. x and s are bf16 numbers: where x / s is not half an
-// integer it is at least 2^-9 from one. Rounded to a multiple of 2^-15 (the last place of 384 = 1.5 * 2^8), x * inv is
-// thus half an integer exactly where x / s is, and on its side of it elsewhere; the second sum (1.5 * 2^23) rounds it to
-// an integer.
+// 2^-23 of it, so x * inv is off by less than 2^-19 for |x / s| <= 8. x and s are bf16 numbers: where x / s is not
+// half an integer it is at least 2^-9 from one. Rounded to a multiple of 2^-15 (the last place of 384 = 1.5 * 2^8),
+// x * inv is thus half an integer exactly where x / s is, and on its side of it elsewhere; the second sum (1.5 * 2^23)
+// rounds it to an integer.
 SVL_DEVINL float kv4_code(float x, float inv) {  // less 8, as a float
   const float t = fminf(__fmaf_rn(x, inv, 384.f), 391.f);
   return __fadd_rn(__fadd_rn(t, 12582912.f - 384.f), -12582912.f);
 }
-// Four codes as 16 bits, lowest first. (The sums of products run beside the maxima, masks and shifts, of which there are
-// enough: the kernel is bound by those.)
+// Four codes as 16 bits, lowest first. (The sums of products run beside the maxima, masks and shifts, of which there
+// are enough: the kernel is bound by those.)
 SVL_DEVINL uint32_t four_codes(float x0, float x1, float x2, float x3, float inv) {
   float n = kv4_code(x3, inv);
   n = __fmaf_rn(n, 16.f, kv4_code(x2, inv));
@@ -107,9 +107,9 @@ SVL_DEVINL uint32_t pair_range(const uint32_t* u) {
 }
 SVL_DEVINL uint32_t wider(uint32_t x, uint32_t y) { return u2(__hmax2_nan(b2(x), b2(y))); }
 
-// The ranges of N groups (a power of two), of which each of the lanes that differ in the bits LOW .. HIGH of their number
-// has a part: a lane ends up with the whole of one, that whose number the lowest of these bits are. The lanes hand each
-// other the half of the groups that they do not keep.
+// The ranges of N groups (a power of two), of which each of the lanes that differ in the bits LOW .. HIGH of their
+// number has a part: a lane ends up with the whole of one, that whose number the lowest of these bits are. The lanes
+// hand each other the half of the groups that they do not keep.
 template <int N, int LOW, int HIGH>
 SVL_DEVINL uint32_t group_range(uint32_t* r, int lane) {
   int n = N;
@@ -171,8 +171,8 @@ SVL_DEVINL void load_words(const void* p, uint32_t* w) {
   }
 }
 
-// A warp per (unit, KV head): block (unit, heads). VT: V is given transposed (row r of dimension c at v[c * v_col + r]),
-// as the QKV projection leaves it.
+// A warp per (unit, KV head): block (unit, heads). VT: V is given transposed (row r of dimension c at
+// v[c * v_col + r]), as the QKV projection leaves it.
 template <int DH, bool VT>
 __global__ void __launch_bounds__(kRowThreads) kv4_write_kernel(Kv4Rows a) {
   constexpr int J = DH / 32;
@@ -188,9 +188,11 @@ __global__ void __launch_bounds__(kRowThreads) kv4_write_kernel(Kv4Rows a) {
   }
   uint8_t* tile = kv4_tile(a.c, q.sample * a.slot_step, h, static_cast<int>(q.p / kKv4Tile));
   const int quad = static_cast<int>(q.p % kKv4Tile) / 8;
-  // what the lane converts: of K row lane / 4, dimensions 32 j + 8 t + 0..7; of V rows 2 t and 2 t + 1, 32 j + 4 g + 0..3
+  // what the lane converts: of K row lane / 4, dimensions 32 j + 8 t + 0..7; of V rows 2 t and 2 t + 1,
+  // 32 j + 4 g + 0..3
   const int g = lane >> 2, t = lane & 3;
-  const bool row_in = g >= q.i0 && g < q.i1, even = 2 * t >= q.i0 && 2 * t < q.i1, odd = 2 * t + 1 >= q.i0 && 2 * t + 1 < q.i1;
+  const bool row_in = g >= q.i0 && g < q.i1;
+  const bool even = 2 * t >= q.i0 && 2 * t < q.i1, odd = 2 * t + 1 >= q.i0 && 2 * t + 1 < q.i1;
   uint4 k[J];
   uint2 v[2][J];
   const __nv_bfloat16* kp = a.k + (q.row + g) * a.k_row + h * DH + 8 * t;
@@ -332,7 +334,8 @@ __global__ void __launch_bounds__(kRowThreads) kv4_read_kernel(Kv4Rows a) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) y[i] = two_values(v[j] >> (4 * i), sv[j], k128);
     if (even)
-      *reinterpret_cast<uint2*>(out + 32 * j) = make_uint2(__byte_perm(y[0], y[1], 0x5410), __byte_perm(y[2], y[3], 0x5410));
+      *reinterpret_cast<uint2*>(out + 32 * j) =
+          make_uint2(__byte_perm(y[0], y[1], 0x5410), __byte_perm(y[2], y[3], 0x5410));
     if (odd)
       *reinterpret_cast<uint2*>(out + a.v_row + 32 * j) =
           make_uint2(__byte_perm(y[0], y[1], 0x7632), __byte_perm(y[2], y[3], 0x7632));
@@ -410,7 +413,8 @@ __global__ void __launch_bounds__(kMoveThreads) kv4_reorder_kernel(Kv4Reorder a)
 // Parts of at least 4 KB (a step of a block), as many as give each SM eight blocks.
 cudaError_t launch_kv4_reorder(const Kv4Reorder& a, cudaStream_t s) {
   const int64_t heads = static_cast<int64_t>(a.c.kv) * a.layers * (a.c.n_slots / a.W);
-  const int64_t steps = (static_cast<int64_t>(a.c.tiles) * kv4_tile_bytes(a.c.dh) / 16 + kMoveThreads - 1) / kMoveThreads;
+  const int64_t words = static_cast<int64_t>(a.c.tiles) * kv4_tile_bytes(a.c.dh) / 16;
+  const int64_t steps = (words + kMoveThreads - 1) / kMoveThreads;
   int64_t parts = (8 * 152 + heads - 1) / heads;
   parts = parts < steps ? parts : steps;
   const dim3 grid(static_cast<unsigned>(parts), a.c.kv, a.c.n_slots / a.W * a.layers);

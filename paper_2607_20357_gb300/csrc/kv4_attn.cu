@@ -96,8 +96,8 @@ SVL_DEVINL int slot_head(const Kv4Attn& a, int slot, int i) {
   return 0;
 }
 
-// A walk over the row of all tiles: where the next tile is, how many the item has left, after how many it goes on behind
-// the sinks.
+// A walk over the row of all tiles: where the next tile is, how many the item has left, after how many it goes on
+// behind the sinks.
 struct Walk {
   const uint8_t* src;
   int p0, left, jump;
@@ -220,8 +220,8 @@ SVL_DEVINL void v_operands(uint32_t v0, uint32_t v1, uint32_t k128, uint32_t (*c
 }
 
 // O^T += V^T P over 16 positions, up to eight columns: weights hi + lo of the positions 2 t, 2 t + 1 ([0]) and those
-// + 8 ([1]) of the operand's column, V's words and scales of the same. MASK: `keep` is 0 at the positions that the column
-// does not see, which do not count whatever their scales.
+// + 8 ([1]) of the operand's column, V's words and scales of the same. MASK: `keep` is 0 at the positions that the
+// column does not see, which do not count whatever their scales.
 template <int J, bool MASK>
 SVL_DEVINL void weighted_rows(float (*o)[2][4], const uint32_t* hi, const uint32_t* lo, const uint32_t* keep,
                               const Words<J>& u0, const Words<J>& u1, const Words<J>& v0, const Words<J>& v1,
@@ -244,10 +244,9 @@ SVL_DEVINL void weighted_rows(float (*o)[2][4], const uint32_t* hi, const uint32
     uint32_t c[4][2];
     v_operands(v0.w[j], v1.w[j], k128, c);
 #pragma unroll
-    for (int k = 0; k < 2; ++k) {
-      mma16816_bf16(o[j][k], c[k][0], c[k + 2][0], c[k][1], c[k + 2][1], ph[0], ph[1]);
-      mma16816_bf16(o[j][k], c[k][0], c[k + 2][0], c[k][1], c[k + 2][1], pl[0], pl[1]);
-    }
+    for (int k = 0; k < 2; ++k) mma16816_bf16(o[j][k], c[k][0], c[k + 2][0], c[k][1], c[k + 2][1], ph[0], ph[1]);
+#pragma unroll
+    for (int k = 0; k < 2; ++k) mma16816_bf16(o[j][k], c[k][0], c[k + 2][0], c[k][1], c[k + 2][1], pl[0], pl[1]);
   }
 }
 
@@ -279,9 +278,9 @@ SVL_DEVINL float part_weight(float m, float l, float M) { return l == 0.f ? 0.f 
 // NW: warps, NS: stages of a warp's ring. MODE: 0 for items of one column, 1 for up to four, 2 for up to eight.
 // In modes 1 and 2 column c is column 2 (c % 4) + c / 4 of the operands, so that a lane's accumulators hold columns t
 // (x = 0) and 4 + t (x = 1); in mode 1 the other operand column of a pair holds the lower halves of the scaled weights.
-// In mode 0 the operands' columns 2 j and 2 j + 1 belong to group j of 32 dimensions: of q they hold that group alone, so
-// that one chain of products gives lane t the sum of group t; of the weights the halves scaled for that group, so that
-// one operand serves all dimensions, of whose sums lane t holds those of group t.
+// In mode 0 the operands' columns 2 j and 2 j + 1 belong to group j of 32 dimensions: of q they hold that group alone,
+// so that one chain of products gives lane t the sum of group t; of the weights the halves scaled for that group, so
+// that one operand serves all dimensions, of whose sums lane t holds those of group t.
 template <int DH, int NS, int NW, int MODE>
 __global__ void __launch_bounds__(NW * 32, 1) kv4_attn_kernel(AttnParams p, int slot_floats) {
   constexpr int J = DH / 32, TB = kv4_tile_bytes(DH), NT = MODE == 2 ? 2 : 1;
@@ -289,10 +288,11 @@ __global__ void __launch_bounds__(NW * 32, 1) kv4_attn_kernel(AttnParams p, int 
   static_assert(NW <= 16, "sums over the warps take 16 lanes");
   extern __shared__ __align__(128) uint8_t smem[];  // per warp: ring of NS tiles; then per warp a part
   __shared__ int warp_sum[kAttnWarps], prefix[kAttnThreads];
-  __shared__ int4 tile_meta[kAttnWarps][NS];   // {first position, bit 0: first tile of its item, bit 1: last; slot, item}
-  __shared__ int4 tile_item[kAttnWarps][NS];   // {KV head, start of the slot, tiles of the item left after it, -}
-  __shared__ int4 w_meta[kAttnWarps];   // {slot, item of the part in the ring (-1: none), state of the other part (1: goes
-                                        // on, 2: ends), tiles of the ring's item left}
+  __shared__ int4 tile_meta[kAttnWarps][NS];  // {first position, bit 0: first tile of its item, bit 1: last; slot,
+                                              // item}
+  __shared__ int4 tile_item[kAttnWarps][NS];  // {KV head, start of the slot, tiles of the item left after it, -}
+  __shared__ int4 w_meta[kAttnWarps];   // {slot, item of the part in the ring (-1: none), state of the other part
+                                        // (1: goes on, 2: ends), tiles of the ring's item left}
   __shared__ int4 w_first[kAttnWarps];  // slot, item and KV head of that other part; KV head of the ring's
   const Kv4Attn& a = p.a;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -328,7 +328,7 @@ __global__ void __launch_bounds__(NW * 32, 1) kv4_attn_kernel(AttnParams p, int 
   const int cta_tiles = max((total + static_cast<int>(gridDim.x) - 1) / static_cast<int>(gridDim.x), p.min_tiles);
   const int cta0 = static_cast<int>(min(static_cast<int64_t>(total), static_cast<int64_t>(cta_tiles) * blockIdx.x));
   const int cta1 = total - cta0 < cta_tiles ? total : cta0 + cta_tiles;
-  const int share = (cta1 - cta0) / kAttnWarps, more = (cta1 - cta0) % kAttnWarps;  // the first `more` warps take one more
+  const int share = (cta1 - cta0) / kAttnWarps, more = (cta1 - cta0) % kAttnWarps;  // (the first `more`: one more)
   const int last = min(cta1 - cta0, kAttnWarps) - 1;                                // last warp with tiles
   auto warp_tile = [&](int w) { return cta0 + w * share + min(w, more); };
   const int w0 = warp_tile(warp), n = share + (warp < more ? 1 : 0);
@@ -499,7 +499,8 @@ __global__ void __launch_bounds__(NW * 32, 1) kv4_attn_kernel(AttnParams p, int 
           for (int r = 0; r < 2; ++r) {
             float x = 0.f;
             if (t < J) {
-              const uint32_t u = reinterpret_cast<const uint16_t*>(tile + kv4_k_scales(DH))[(16 * h + 8 * r + g) * J + t];
+              const int at = (16 * h + 8 * r + g) * J + t;
+              const uint32_t u = reinterpret_cast<const uint16_t*>(tile + kv4_k_scales(DH))[at];
               x = bf16_lo(u) * d[2 * r];
             }
             x += __shfl_xor_sync(0xffffffffu, x, 1);
@@ -869,9 +870,10 @@ size_t kv4_attn_workspace(const Kv4Cache& c, int A, int rows) {
 template <int DH, int NS, int NW, int MODE>
 static cudaError_t launch_attn(const AttnParams& p, int slot_floats, int grid, cudaStream_t s) {
   const int smem = NW * (NS * kv4_tile_bytes(DH) + slot_floats * 4);
-  cudaError_t e = cudaFuncSetAttribute(kv4_attn_kernel<DH, NS, NW, MODE>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+  const auto kernel = kv4_attn_kernel<DH, NS, NW, MODE>;
+  cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
   if (e != cudaSuccess) return e;
-  e = launch_pdl(kv4_attn_kernel<DH, NS, NW, MODE>, dim3(grid), NW * 32, smem, s, p, slot_floats);
+  e = launch_pdl(kernel, dim3(grid), NW * 32, smem, s, p, slot_floats);
   if (e != cudaSuccess) return e;
   return launch_pdl(kv4_merge_kernel<DH>, dim3(grid, p.ncols), kMergeThreads, 0, s, p, slot_floats);
 }
