@@ -37,11 +37,12 @@
 //
 // Measured, d_head 128 (times of the call in a graph, rates of the cache's bytes; a
 // copy runs at 6.8 TB/s):
-//  - 32 heads of their own, 8 slots of 4,000 to 16,000 positions: 55.9 us, 5.7 TB/s.
-//    Some 620 instructions a tile, of which 337 are the ALU's, keep it busy 62 % of
-//    the time. 16 slots of 250 to 450 positions: 12.3 us, two or three tiles a warp.
+//  - 32 heads of their own, 8 slots of 4,000 to 16,000 positions: 55.9 us, 5.7 TB/s
+//    (52.5 us without any arithmetic, some 6 of them launching and joining). Some 620
+//    instructions a tile, of which 337 are the ALU's, keep it busy 62 % of the time.
+//    16 slots of 250 to 450 positions: 12.3 us (8.6), two or three tiles a warp.
 //  - 28 heads on 4 KV heads (seven columns), 8 slots of 20,000 to 40,000 positions:
-//    37.5 us, 3.5 TB/s; with four rows (28 columns, four passes) 112 us. Three warps
+//    37.5 us (26.7), 3.5 TB/s; four rows (28 columns, four passes) 112 us (45). Three warps
 //    per scheduler are all that the registers allow, each a chain of products,
 //    shuffles and exponentials: instructions issue in 62 % of the cycles, and no
 //    single kind of arithmetic left out saves more than 8 %.
