@@ -1256,7 +1256,7 @@ svl_status prefill_impl(svl_model* m, int32_t B, int32_t t_cap, void* X, const i
       Launch L1(m, SVL_TAG_ATTENTION, s);
       ka.late = !f8;
       next_launch(ka.late);
-      g_launches++;  // (a second kernel puts split heads together)
+      g_launches += kv4_attn_launches(ka) - 1;  // (a second kernel may put split heads together)
       if (launch_kv4_attention(ka, s) != cudaSuccess) return SVL_ERR_CUDA;
     } else if (decode) {
       DecAttnArgs da;
@@ -1696,7 +1696,7 @@ svl_status svl_kv4_attention(const svl_kv4_desc* desc, const void* cache, int32_
   a.scale = scale;
   a.ws = ws;
   if ((a.num_sms = device_sms()) <= 0) return SVL_ERR_CUDA;
-  g_launches += 2;
+  g_launches += kv4_attn_launches(a);
   if (launch_kv4_attention(a, static_cast<cudaStream_t>(stream)) != cudaSuccess) return SVL_ERR_CUDA;
   return last_error();
 }

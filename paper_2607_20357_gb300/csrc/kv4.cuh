@@ -86,6 +86,7 @@ struct Kv4Attn {
 };
 size_t kv4_attn_workspace(const Kv4Cache& c, int A, int rows);
 cudaError_t launch_kv4_attention(const Kv4Attn& a, cudaStream_t s);
+int kv4_attn_launches(const Kv4Attn& a);
 constexpr int kKv4MaxRows = 16;  // query rows per slot
 
 struct Kv4Reorder {

@@ -33,7 +33,8 @@
 // with an online softmax, its next tiles on their way into a ring of its own in
 // shared memory (cp.async). Items that end up in several warps are put together
 // from their parts in order: in shared memory within a CTA, by a second launch
-// across CTAs.
+// across CTAs. Few and short items instead have a cluster of one to eight CTAs each,
+// whose parts meet in its shared memory: one launch (attn_run has the rule).
 //
 // Measured, d_head 128 (times of the call in a graph, rates of the cache's bytes; a
 // copy runs at 6.8 TB/s):
@@ -46,9 +47,9 @@
 //    per scheduler are all that the registers allow, each a chain of products,
 //    shuffles and exponentials: instructions issue in 62 % of the cycles, and no
 //    single kind of arithmetic left out saves more than 8 %.
-//  - one slot of 1,900 positions, 28 heads on 4 KV heads: 8.4 us of latencies: starts
-//    and places 0.8, queries and first tile 1.3, a tile 1.1, its end 0.5, the warps'
-//    parts 1.0, the second launch 2.1, the rest launching.
+//  - one slot of 1,900 positions, 28 heads on 4 KV heads: 7.4 us of latencies (8.4 with
+//    the second launch): launching 0.8, queries and first tile 1.3, a tile 1.1, its end
+//    0.5, the warps' parts 1.0, the cluster's some 1.
 #include <cuda_fp16.h>
 
 #include "kv4.cuh"
@@ -58,11 +59,13 @@ namespace svl {
 constexpr int kCols = 8;
 constexpr int kMaxCtas = 256;
 constexpr int kMergeThreads = 128;
+constexpr int kClusterCtas = 8;  // most CTAs of a cluster
 
 struct AttnParams {
   Kv4Attn a;
   int ncols;      // columns of an item: min(8, rows * heads per KV head)
   int col_tiles;  // items per KV head
+  int run;        // CTAs of an item's cluster (0: tiles are dealt to all CTAs)
   int min_tiles;  // least tiles of a CTA that has any
   int grp;        // heads per KV head
   int columns;    // rows * grp
@@ -297,7 +300,7 @@ SVL_DEVINL float part_weight(float m, float l, float M) { return l == 0.f ? 0.f 
 // In mode 0 the operands' columns 2 j and 2 j + 1 belong to group j of 32 dimensions: of q they hold that group alone,
 // so that one chain of products gives lane t the sum of group t; of the weights the halves scaled for that group, so
 // that one operand serves all dimensions, of whose sums lane t holds those of group t.
-template <int DH, int NS, int NW, int MODE>
+template <int DH, int NS, int NW, int MODE, bool CLUSTER>
 __global__ void __launch_bounds__(NW * 32, 1) kv4_attn_kernel(AttnParams p, int slot_floats) {
   constexpr int J = DH / 32, TB = kv4_tile_bytes(DH), NT = MODE == 2 ? 2 : 1;
   constexpr int kAttnWarps = NW, kAttnThreads = NW * 32;
@@ -316,33 +319,50 @@ __global__ void __launch_bounds__(NW * 32, 1) kv4_attn_kernel(AttnParams p, int 
   uint8_t* ring = smem + warp * (NS * TB);
   float* first_part = reinterpret_cast<float*>(smem + kAttnWarps * (NS * TB)) + warp * slot_floats;
   float* last_part = reinterpret_cast<float*>(ring);
-  pdl_begin(false);
+  pdl_begin(CLUSTER && a.late);
 
-  // ---- this warp's share of all tiles
-  const int per = (a.c.n_slots + kAttnThreads - 1) / kAttnThreads;
-  {
-    const int s0 = min(tid * per, a.c.n_slots), s1 = min(s0 + per, a.c.n_slots);
-    int incl = 0;
-    for (int s = s0; s < s1; ++s) incl += slot_heads(a, s) * p.col_tiles * slot_span(a, s).n;
+  // ---- this warp's share of all tiles; in a cluster, of those of its item
+  int total, cta_tiles, index, sums = 0, per = 0;
+  const int own = CLUSTER ? blockIdx.x / p.run : 0, own_slot = own / (a.c.kv * p.col_tiles);
+  const int own_item = own % (a.c.kv * p.col_tiles);
+  Walk req;
+  if constexpr (CLUSTER) {
+    req.slot = own_slot;
+    req.item = own_item;
+    walk_slot(p, req);
+    if (req.item >= req.items) return;  // (the whole cluster)
+    total = req.span.n;
+    cta_tiles = max((total + p.run - 1) / p.run, 4);  // (10 tiles: 4 6.5 us, 6 6.7, 12 6.9)
+    index = static_cast<int>(cluster_rank());
+    if (lane == 0) w_meta[warp] = make_int4(-1, 0, 0, 0);
+    __syncwarp();
+  } else {
+    per = (a.c.n_slots + kAttnThreads - 1) / kAttnThreads;
+    {
+      const int s0 = min(tid * per, a.c.n_slots), s1 = min(s0 + per, a.c.n_slots);
+      int incl = 0;
+      for (int s = s0; s < s1; ++s) incl += slot_heads(a, s) * p.col_tiles * slot_span(a, s).n;
 #pragma unroll
-    for (int off = 1; off < 32; off <<= 1) {
-      const int x = __shfl_up_sync(0xffffffffu, incl, off);
-      if (lane >= off) incl += x;
+      for (int off = 1; off < 32; off <<= 1) {
+        const int x = __shfl_up_sync(0xffffffffu, incl, off);
+        if (lane >= off) incl += x;
+      }
+      prefix[tid] = incl;
+      if (lane == 31) warp_sum[warp] = incl;
+      if (tid < kAttnWarps) w_meta[tid] = make_int4(-1, 0, 0, 0);
     }
-    prefix[tid] = incl;
-    if (lane == 31) warp_sum[warp] = incl;
-    if (tid < kAttnWarps) w_meta[tid] = make_int4(-1, 0, 0, 0);
-  }
-  __syncthreads();
-  int sums = lane < kAttnWarps ? warp_sum[lane] : 0;
+    __syncthreads();
+    sums = lane < kAttnWarps ? warp_sum[lane] : 0;
 #pragma unroll
-  for (int off = 1; off < 16; off <<= 1) {
-    const int x = __shfl_up_sync(0xffffffffu, sums, off);
-    if (lane >= off) sums += x;
+    for (int off = 1; off < 16; off <<= 1) {
+      const int x = __shfl_up_sync(0xffffffffu, sums, off);
+      if (lane >= off) sums += x;
+    }
+    total = __shfl_sync(0xffffffffu, sums, kAttnWarps - 1);
+    cta_tiles = max((total + static_cast<int>(gridDim.x) - 1) / static_cast<int>(gridDim.x), p.min_tiles);
+    index = blockIdx.x;
   }
-  const int total = __shfl_sync(0xffffffffu, sums, kAttnWarps - 1);
-  const int cta_tiles = max((total + static_cast<int>(gridDim.x) - 1) / static_cast<int>(gridDim.x), p.min_tiles);
-  const int cta0 = static_cast<int>(min(static_cast<int64_t>(total), static_cast<int64_t>(cta_tiles) * blockIdx.x));
+  const int cta0 = static_cast<int>(min(static_cast<int64_t>(total), static_cast<int64_t>(cta_tiles) * index));
   const int cta1 = total - cta0 < cta_tiles ? total : cta0 + cta_tiles;
   const int share = (cta1 - cta0) / kAttnWarps, more = (cta1 - cta0) % kAttnWarps;  // (the first `more`: one more)
   const int last = min(cta1 - cta0, kAttnWarps) - 1;                                // last warp with tiles
@@ -351,9 +371,10 @@ __global__ void __launch_bounds__(NW * 32, 1) kv4_attn_kernel(AttnParams p, int 
 
   // ---- the tiles
   if (n > 0) {
-    Walk req;
     int asked = 0;
-    {
+    if constexpr (CLUSTER) {
+      walk_item(p, req, w0);
+    } else {
       // the thread's share of the slots that holds tile w0, the slot, the item
       const int wi = __popc(__ballot_sync(0xffffffffu, lane < kAttnWarps && sums <= w0));
       const int base = wi > 0 ? __shfl_sync(0xffffffffu, sums, wi - 1) : 0;
@@ -738,12 +759,15 @@ __global__ void __launch_bounds__(NW * 32, 1) kv4_attn_kernel(AttnParams p, int 
   __syncthreads();
 
   // ---- items that several warps share are put together, (item, column) by (item, column)
-  float* out_part = p.part + static_cast<size_t>(blockIdx.x) * 2 * slot_floats;
+  // (a cluster's CTAs have a part of one item, kept in shared memory for the others to read)
+  float* out_part = CLUSTER ? reinterpret_cast<float*>(smem + kAttnWarps * (NS * TB + slot_floats * 4))
+                            : p.part + static_cast<size_t>(blockIdx.x) * 2 * slot_floats;
+  const int next_part = CLUSTER ? 0 : slot_floats;  // where the part that the next CTA goes on with is
   const int4 wm = lane <= last ? w_meta[lane] : make_int4(-1, 0, 0, 0);
   const uint32_t starts = __ballot_sync(0xffffffffu, wm.x >= 0);    // warps whose ring holds an item's start
   const uint32_t goes_on = __ballot_sync(0xffffffffu, wm.z == 1);   // warps within an item
   uint32_t ends = __ballot_sync(0xffffffffu, wm.z == 2);            // warps with an item's end
-  if (tid == 0) {
+  if (!CLUSTER && tid == 0) {
     // the item that started here and goes on in the next CTA, and how many CTAs it is in
     int4 mt = make_int4(-1, 0, 0, 0);
     const int v = 31 - __clz(starts);
@@ -798,7 +822,7 @@ __global__ void __launch_bounds__(NW * 32, 1) kv4_attn_kernel(AttnParams p, int 
       if (done) {
         if (d < DH) store_out(p, it.x, it.z, c0 + col, d, o);
       } else {
-        float* y = out_part + (here ? slot_floats : 0);
+        float* y = out_part + (here ? next_part : 0);
         if (d < DH) *reinterpret_cast<float4*>(y + col * DH + d) = o;
         if (lane == 0) {
           y[p.ncols * DH + 2 * col] = M;
@@ -809,7 +833,38 @@ __global__ void __launch_bounds__(NW * 32, 1) kv4_attn_kernel(AttnParams p, int 
   }
   if (last >= 0 && (starts >> last & 1u)) {
     const float* x = part_of(last, false);
-    for (int i = tid; i < slot_floats; i += kAttnThreads) out_part[slot_floats + i] = x[i];
+    for (int i = tid; i < slot_floats; i += kAttnThreads) out_part[next_part + i] = x[i];
+  }
+  if constexpr (CLUSTER) {
+    // ---- the item's parts: column c by warp c / run of CTA c % run
+    const int parts = (total - 1) / cta_tiles + 1, c0 = own_item % p.col_tiles * kCols, col = index + p.run * warp;
+    if (parts == 1) return;  // (the whole cluster: the item is done)
+    cluster_sync();
+    if (col < min(kCols, p.columns - c0)) {
+      float m = -INFINITY, l = 0.f;
+      if (lane < parts) {
+        const float* x = out_part + p.ncols * DH + 2 * col;
+        m = ld_cluster(mapa_shared(x, lane));
+        l = ld_cluster(mapa_shared(x + 1, lane));
+      }
+      float M = m;
+#pragma unroll
+      for (int off = kClusterCtas / 2; off > 0; off >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, off));
+      const float f = part_weight(m, l, M);
+      float L = f;
+#pragma unroll
+      for (int off = kClusterCtas / 2; off > 0; off >>= 1) L += __shfl_xor_sync(0xffffffffu, L, off);
+      const float inv = __shfl_sync(0xffffffffu, L == 0.f ? 0.f : __fdividef(1.f, L), 0);
+      float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+      const int d = 4 * lane;
+#pragma unroll
+      for (int i = 0; i < kClusterCtas; ++i) {
+        const float x = __shfl_sync(0xffffffffu, f, i) * inv;
+        if (d < DH && i < parts) add_scaled(o, x, ld_cluster4(mapa_shared(out_part + col * DH + d, i)));
+      }
+      if (d < DH) store_out(p, own_slot, slot_head(a, own_slot, own_item / p.col_tiles), c0 + col, d, o);
+    }
+    cluster_sync();  // the others have read this CTA's part
   }
 }
 
@@ -884,10 +939,40 @@ size_t kv4_attn_workspace(const Kv4Cache& c, int A, int rows) {
   return kMaxCtas * (2 * floats * sizeof(float) + sizeof(int4));
 }
 
+// CTAs of an item's cluster (0: none, the tiles are dealt to all CTAs and a second launch joins them). Clusters need a
+// single wave of CTAs: 14 clusters of eight fit the GPU and 16 do not (16 items of 60 tiles: 9.6 us dealt, 13.9 in
+// clusters of eight, 9.4 of four), 32 of four and not 38, 76 of two. They save the second launch and lose where a CTA
+// has many more tiles than its share of all, or where items differ much in length, which max_len alone bounds here: up
+// to three tiles a warp and 14 tiles more. Dealt and in clusters, 28 heads on 4 KV heads: one slot of 1,100 positions
+// 9.1 and 7.0 us, of 4,000 9.6 and 9.4; 8 heads on one, 6,000 positions 9.4 and 10.0; seven heads on each of 96 KV
+// heads, 1,088 positions 12.1 and 10.9 (a CTA each), of 48, 4,000 positions 15.8 and 16.7 (two each).
+static int attn_run(const Kv4Attn& a) {
+  const int columns = a.rows * (a.A / a.c.kv), warps = columns == 1 ? 16 : 12;
+  const int64_t items = static_cast<int64_t>(a.c.n_slots) * a.c.kv * ((columns + kCols - 1) / kCols);
+  int64_t tiles = a.c.tiles;
+  if (a.window > 0) {
+    const int64_t near = (static_cast<int64_t>(a.window) + a.rows - 2) / kKv4Tile + 2;
+    const int64_t seen = near + (a.sinks + static_cast<int64_t>(kKv4Tile) - 1) / kKv4Tile;
+    tiles = seen < tiles ? seen : tiles;
+  }
+  const int run = items * 8 <= 96 ? 8 : items * 4 <= 128 ? 4 : items * 2 <= a.num_sms ? 2 : 1;
+  if (items * run > a.num_sms || tiles > 3 * warps * run) return 0;
+  return tiles / run <= items * tiles / a.num_sms + 14 ? run : 0;
+}
+int kv4_attn_launches(const Kv4Attn& a) { return attn_run(a) ? 1 : 2; }
+
 template <int DH, int NS, int NW, int MODE>
 static cudaError_t launch_attn(const AttnParams& p, int slot_floats, int grid, cudaStream_t s) {
-  const int smem = NW * (NS * kv4_tile_bytes(DH) + slot_floats * 4);
-  const auto kernel = kv4_attn_kernel<DH, NS, NW, MODE>;
+  int smem = NW * (NS * kv4_tile_bytes(DH) + slot_floats * 4);
+  if (p.run) {
+    smem += slot_floats * 4;
+    const auto kernel = kv4_attn_kernel<DH, NS, NW, MODE, true>;
+    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+    if (e != cudaSuccess) return e;
+    const unsigned items = static_cast<unsigned>(p.a.c.n_slots * p.a.c.kv * p.col_tiles);
+    return launch_pdl_cluster(kernel, dim3(items * p.run), NW * 32, smem, p.run, s, p, slot_floats);
+  }
+  const auto kernel = kv4_attn_kernel<DH, NS, NW, MODE, false>;
   cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
   if (e != cudaSuccess) return e;
   e = launch_pdl(kernel, dim3(grid), NW * 32, smem, s, p, slot_floats);
@@ -900,6 +985,7 @@ cudaError_t launch_kv4_attention(const Kv4Attn& a, cudaStream_t s) {
   p.a = a;
   p.ncols = attn_ncols(a.c, a.A, a.rows);
   p.col_tiles = (a.rows * (a.A / a.c.kv) + kCols - 1) / kCols;
+  p.run = attn_run(a);
   p.min_tiles = 6;  // (1,900 rows of four KV heads: 2 10.5 us, 4 9.1, 6 9.0, 12 9.8)
   p.grp = a.A / a.c.kv;
   p.columns = a.rows * p.grp;

@@ -1,5 +1,5 @@
 """The 4-bit cache's attention and the model calls over it at their edges: values that are not finite in sight and in
-queries, eight heads per KV head under gates, prompts that the cache has no room for."""
+queries, eight heads per KV head under gates, prompts that the cache has no room for, both ways to cut a call's work."""
 import numpy as np
 import pytest
 import torch
@@ -34,7 +34,8 @@ def test_a_nan_in_sight_shows_though_its_weight_is_zero(heads, kv, dh, n, at):
     kv4_tests.write(desc, cache, k.to(BF16).view(n, -1).cuda(), v.view(n, -1).cuda(), [n], None)
     q = torch.zeros(1, heads, dh)
     q[:, :, 0] = 400.0  # scores of 3,200 and 0: weights of 1 and e^-3200
-    got = kv4_tests._attend(desc, cache, q.to(BF16).view(1, -1), [n - 1], 1, heads, 0, 0, 1.0).reshape(heads, dh // 32, 32)
+    got = kv4_tests._attend(desc, cache, q.to(BF16).view(1, -1), [n - 1], 1, heads, 0, 0, 1.0)
+    got = got.reshape(heads, dh // 32, 32)
     nan = np.isnan(got)
     assert nan[:, 1].all() and nan.sum() == heads * 32
     want = R.as_bf16(R.quantised(clean[5])).double().numpy().reshape(kv, dh // 32, 32)
@@ -107,3 +108,42 @@ def test_a_prompt_that_the_cache_has_no_room_for():
     assert cache_len2.tolist() == [lens[0], lens[1] + 1]
     assert int(nxt[0]) == -1 and int(nxt[1]) >= 0
     case.close()
+
+
+# The same sizes as the other file's, in a cache with room for far more positions and with many slots: how a call's work
+# is cut depends on both.
+@pytest.mark.parametrize("heads,kv,dh,rows,starts,window,sinks", kv4_tests.test_attention.pytestmark[0].args[1])
+def test_attention_in_a_cache_with_room_for_more(heads, kv, dh, rows, starts, window, sinks):
+    desc = svl.Kv4Desc(len(starts), kv, dh, 13_000)
+    cache, look = kv4_tests._filled(71, desc, [max(0, s + rows) for s in starts])
+    q = kv4_tests.rows_of(72, len(starts) * rows, heads * dh + 8)
+    kv4_tests._check_attention(desc, cache, q, starts, rows, heads, window, sinks, look)
+
+
+@pytest.mark.parametrize("slots,heads,kv,dh,rows,window,sinks", [
+    (40, 8, 4, 64, 3, 70, 5), (40, 4, 4, 128, 1, 40, 37), (13, 7, 1, 64, 1, 0, 0), (3, 12, 4, 128, 1, 0, 0),
+    (8, 4, 4, 64, 1, 0, 0), (19, 8, 2, 128, 2, 0, 0), (38, 4, 2, 64, 1, 64, 1), (75, 2, 2, 128, 1, 0, 0),
+    (152, 1, 1, 64, 1, 0, 0), (153, 1, 1, 64, 2, 0, 0), (7, 40, 2, 64, 16, 100, 0),
+])
+def test_attention_of_many_and_few_items(slots, heads, kv, dh, rows, window, sinks):
+    rng = np.random.default_rng(slots)
+    starts = rng.integers(-2, 300, slots).tolist()
+    starts[0] = 400
+    desc = svl.Kv4Desc(slots, kv, dh, 420)
+    cache, look = kv4_tests._filled(73, desc, [max(0, s + rows) for s in starts])
+    q = kv4_tests.rows_of(74, slots * rows, heads * dh)
+    kv4_tests._check_attention(desc, cache, q, starts, rows, heads, window, sinks, look)
+
+
+def test_beam_search_over_many_items_under_gates():
+    dims = synth.reduced(model_tests.TINY.dims, n_layers=2, d_model=512, n_heads=8, n_kv_heads=8, n_groups=8, c_vis=512)
+    model_tests.test_beam_search_scores_are_its_tokens_log_probabilities(dims, 16, 0)
+
+
+def test_one_item_per_cluster_gives_the_same_bits_every_time():
+    desc = svl.Kv4Desc(2, 4, 128, 4000)
+    cache, _ = kv4_tests._filled(75, desc, [4000, 77])
+    q = kv4_tests.rows_of(76, 2, 28 * 128)
+    first = kv4_tests._attend(desc, cache, q, [3999, 76], 1, 28, 0, 0, 0.088)
+    for _ in range(5):
+        np.testing.assert_array_equal(first, kv4_tests._attend(desc, cache, q, [3999, 76], 1, 28, 0, 0, 0.088))
