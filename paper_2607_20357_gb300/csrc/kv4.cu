@@ -187,12 +187,12 @@ __global__ void __launch_bounds__(kRowThreads) kv4_write_kernel(Kv4Rows a) {
   const int lane = threadIdx.x & 31, h = blockIdx.y * (blockDim.x / 32) + (threadIdx.x >> 5);
   Unit q;
   if (h >= a.c.kv || !find_unit(a, blockIdx.x, lane, q) || q.p < 0) return;
-  if (!gate_on(a.gate, q.sample, a.gate.G ? h / (a.c.kv / a.gate.G) : 0)) return;
   if (q.p + q.i1 > a.c.max_len) {
     if (h == 0 && lane == 0) report(a.status, SVL_DEV_BAD_INDEX);
     if (q.p + q.i0 >= a.c.max_len) return;
     q.i1 = static_cast<int>(a.c.max_len - q.p);
   }
+  if (!gate_on(a.gate, q.sample, a.gate.G ? h / (a.c.kv / a.gate.G) : 0)) return;
   uint8_t* tile = kv4_tile(a.c, q.sample * a.slot_step, h, static_cast<int>(q.p / kKv4Tile));
   const int quad = static_cast<int>(q.p % kKv4Tile) / 8;
   // what the lane converts: of K row lane / 4, dimensions 32 j + 8 t + 0..7; of V rows 2 t and 2 t + 1,

@@ -147,3 +147,14 @@ def test_one_item_per_cluster_gives_the_same_bits_every_time():
     first = kv4_tests._attend(desc, cache, q, [3999, 76], 1, 28, 0, 0, 0.088)
     for _ in range(5):
         np.testing.assert_array_equal(first, kv4_tests._attend(desc, cache, q, [3999, 76], 1, 28, 0, 0, 0.088))
+
+
+def test_rows_without_a_place_are_reported_under_gates():
+    """The first group is off in every layer; a prompt longer than the cache still shows."""
+    dims = model_tests.GQA
+    case = model_tests._case(dims, 81, [64], [16], gates=False)
+    case.b["group_gate"][:, :, 0] = 0
+    _, _, cache_len, _, _ = model_tests._prefill(case, 45, 1)
+    assert cache_len.tolist()[0] > 45
+    assert svl.svl_get_device_status(case.model.handle) == svl.SVL_DEV_BAD_INDEX
+    case.close()
