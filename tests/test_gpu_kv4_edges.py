@@ -149,6 +149,37 @@ def test_one_item_per_cluster_gives_the_same_bits_every_time():
         np.testing.assert_array_equal(first, kv4_tests._attend(desc, cache, q, [3999, 76], 1, 28, 0, 0, 0.088))
 
 
+@pytest.mark.parametrize("kv,dh", [(1, 64), (3, 64), (1, 128), (5, 128)])
+def test_one_row_per_slot_equals_rows_by_offsets(kv, dh):
+    """Values of every kind, written both ways into caches that hold the same before: the same bytes."""
+    n, cols = 60, kv * dh
+    desc = svl.Kv4Desc(n, kv, dh, 70)
+    x = kv4_tests.rows_of(77, n, 2 * cols + 16).float()
+    x[1] = 0.0
+    x[2], x[3] = 3.0, -3.0
+    x[4, ::2], x[4, 1::2] = 5.0, -5.0
+    x[5] = torch.arange(2 * cols + 16) % 33 - 16.0
+    x[6, ::7] = float("nan")
+    x[7, ::40], x[8, 3::50] = float("inf"), -float("inf")
+    x[9], x[10] = x[9] * 2.0 ** -126, x[10] * 2.0 ** -122
+    x[11] = 3e38
+    x[12:20] = torch.randint(-255, 256, x[12:20].shape, generator=torch.Generator().manual_seed(78)).float()
+    xd = x.to(BF16).cuda()
+    k, v = xd[:, 8:8 + cols], xd[:, 16 + cols:]
+    starts = [(7 * i) % 70 for i in range(n)]
+    starts[20:24] = [-1, -70, 70, 2 ** 31 - 1]
+    caches, status = [], []
+    for row_off in (None, "ragged"):
+        g = torch.Generator(device="cuda").manual_seed(79)
+        cache = torch.randint(0, 256, (svl.svl_kv4_cache_size(desc),), dtype=torch.uint8, device="cuda", generator=g)
+        st = torch.zeros(1, dtype=torch.int32, device="cuda")
+        kv4_tests.write(desc, cache, k, v, [1] * n, starts, st, row_off)
+        caches.append(cache)
+        status.append(int(st))
+    assert torch.equal(*caches)
+    assert status == [svl.SVL_DEV_BAD_INDEX] * 2
+
+
 def test_rows_without_a_place_are_reported_under_gates():
     """The first group is off in every layer; a prompt longer than the cache still shows."""
     dims = model_tests.GQA
