@@ -456,6 +456,15 @@ __global__ void __launch_bounds__(NW * 32, 1) kv4_attn_kernel(AttnParams p, int 
         const uint32_t eb = min(max(big >> 7, 14u), 254u);
         const float up = __uint_as_float((268 - eb) << 23), up4 = up * 0.0625f;
         float f = a.scale * 1.4426950408889634f * 1024.f * __uint_as_float(eb << 23);
+        // Where that is past float32's range in any column, all have its root, of scale's sign, and scores are multiplied
+        // by it twice (2^(eb - 127) as 2^odd times the square of a power of two; sqrt(log2 e) = 1.2011...).
+        const bool wide = __any_sync(0xffffffffu, isinf(f) && big < 0x7f80u);
+        if (wide) {
+          const uint32_t odd = ~eb & 1u;
+          f = sqrtf(fabsf(a.scale)) * (odd ? 1.6986436005760381f : 1.2011224087864498f) * 32.f *
+              __uint_as_float((127 + eb - odd) / 2 << 23);
+          f = copysignf(f, a.scale);
+        }
         if (big >= 0x7f80u) f = NAN;  // a q that is not finite
 #pragma unroll
         for (int j = 0; j < C; ++j) {
@@ -503,6 +512,8 @@ __global__ void __launch_bounds__(NW * 32, 1) kv4_attn_kernel(AttnParams p, int 
           }
           whole_lo = MODE == 0 ? lo : __reduce_max_sync(0xffffffffu, lo);
           whole_hi = MODE == 0 ? hi : __reduce_min_sync(0xffffffffu, hi);
+          // (an item whose factor is a root has no whole tiles: -1 says so, and costs the others no register)
+          if (wide) whole_hi = -1;
         }
 #pragma unroll
         for (int j = 0; j < J; ++j)
@@ -580,11 +591,12 @@ __global__ void __launch_bounds__(NW * 32, 1) kv4_attn_kernel(AttnParams p, int 
       if (!whole) {
 #pragma unroll
         for (int x = 0; x < NT; ++x) {
+          const float again = whole_hi < 0 ? fabsf(factor[x]) : 1.f;
           sight[x] = (bits_below(end[x] - p0) & ~bits_below(low[x] - p0)) | bits_below(min(a.sinks, end[x]) - p0);
           sight[x] >>= g;
 #pragma unroll
           for (int k = 0; k < 4; ++k)
-            if (!(sight[x] >> (8 * k) & 1u)) s[k >> 1][k & 1][x] = -INFINITY;
+            s[k >> 1][k & 1][x] = sight[x] >> (8 * k) & 1u ? s[k >> 1][k & 1][x] * again : -INFINITY;
         }
       }
       // the running maximum moves when it is passed by more than a factor of two
