@@ -604,26 +604,32 @@ class GatedPrefill:
         each of `beams` beams per sample under the prompt's gates, with
         attention to the last `window` positions and the first `sinks` only
         if window > 0. A beam that takes the id `eos` is finished and stands
-        for itself from then on (eos < 0: none does).
+        for itself from then on (eos < 0: none does). The cache has room for
+        the longest prompt after token selection and the steps - 1 rows fed
+        behind it: ValueError, before the prefill, where those are more than
+        the model's max_seq positions.
 
         Returns tensors on the device, the best beam first: tokens
         [B, beams, steps] int32 (a finished beam's tail is eos), scores
         [B, beams] float32 (log-probabilities, summed), finished [B, beams]
-        uint8, cache_len [B * beams]. Nothing waits for the device between
-        the steps."""
+        uint8, cache_len [B * beams]. The host waits for the prompts'
+        lengths once, and for nothing between the steps."""
         d, B, W = self.dims, batch["B"], int(beams)
         if W < 1 or steps < 1:
             raise ValueError(f"beams {beams}, steps {steps}: at least one of each")
         dev = batch["vis"].device
         nv, nt = batch["vis"].shape[0], int(batch["text_ids"].shape[0])
-        prompt = (batch["vis_off"][1:] - batch["vis_off"][:-1]) + (batch["text_off"][1:] - batch["text_off"][:-1])
-        max_len = min(int(prompt.max()) + steps, self.desc.max_seq)
+        out = self.run(batch, stages=("select", "pack"))
+        longest = int((out["cu_seqlens"][1:] - out["cu_seqlens"][:-1]).max())
+        max_len = max(longest + steps - 1, 1)
+        if max_len > self.desc.max_seq:
+            raise ValueError(f"a prompt of {longest} rows and {steps} steps need {max_len} positions, and the model's "
+                             f"max_seq is {self.desc.max_seq}")
         desc = Kv4Desc(B * W, d.n_kv_heads, d.d_head, max_len)
         u8 = dict(dtype=torch.uint8, device=dev)
         i32 = dict(dtype=torch.int32, device=dev)
         cache = torch.empty(d.n_layers * svl_kv4_cache_size(desc), **u8)
         cache_len = torch.empty(B * W, **i32)
-        out = self.run(batch, stages=("select", "pack"))
         ws, wsb = self.workspace(B, nv, nt, dev, ("prefill",))
         svl_gated_prefill_kv4(self.handle, B, max(nv + nt, 1), out["X"], out["cu_seqlens"], out["pos"],
                               batch["layer_gate"], batch["group_gate"], SVL_LOGITS_LAST, out["logits"], cache, max_len,
