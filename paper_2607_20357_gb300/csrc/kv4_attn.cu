@@ -975,17 +975,22 @@ int kv4_attn_launches(const Kv4Attn& a) { return attn_run(a) ? 1 : 2; }
 
 template <int DH, int NS, int NW, int MODE>
 static cudaError_t launch_attn(const AttnParams& p, int slot_floats, int grid, cudaStream_t s) {
-  int smem = NW * (NS * kv4_tile_bytes(DH) + slot_floats * 4);
+  // The limit belongs to the kernel, not to the call: every call sets the one for the most columns of its mode, whatever
+  // other threads launch meanwhile.
+  const int most = part_floats(MODE == 0 ? 1 : MODE == 1 ? 4 : kCols, DH) * 4;
+  constexpr int kRings = NW * NS * kv4_tile_bytes(DH);
+  int smem = kRings + NW * slot_floats * 4;
   if (p.run) {
     smem += slot_floats * 4;
     const auto kernel = kv4_attn_kernel<DH, NS, NW, MODE, true>;
-    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+    const cudaError_t e =
+        cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kRings + (NW + 1) * most);
     if (e != cudaSuccess) return e;
     const unsigned items = static_cast<unsigned>(p.a.c.n_slots * p.a.c.kv * p.col_tiles);
     return launch_pdl_cluster(kernel, dim3(items * p.run), NW * 32, smem, p.run, s, p, slot_floats);
   }
   const auto kernel = kv4_attn_kernel<DH, NS, NW, MODE, false>;
-  cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+  cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kRings + NW * most);
   if (e != cudaSuccess) return e;
   e = launch_pdl(kernel, dim3(grid), NW * 32, smem, s, p, slot_floats);
   if (e != cudaSuccess) return e;
