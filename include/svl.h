@@ -453,7 +453,8 @@ svl_status svl_beam_select(int32_t n_samples, int32_t beams, int32_t vocab, int3
  * [n_slots / beams] int32, device: positions below it are the same in all
  * beams, as a shared prompt's are, and stay; NULL: 0). Both ends widen to
  * whole tiles of 32 positions: from[b] rounds down. A slot whose parent is out
- * of range keeps its rows and sets SVL_DEV_BAD_INDEX in *status (or NULL). */
+ * of range keeps its rows and sets SVL_DEV_BAD_INDEX in *status (or NULL).
+ * n_layers * n_slots / beams is at most 2^30 (else SVL_ERR_UNSUPPORTED). */
 svl_status svl_kv4_reorder(const svl_kv4_desc* desc, void* cache, int32_t n_layers, int32_t beams,
                            const int32_t* parent, const int32_t* from, const int32_t* len, uint32_t* status,
                            void* stream);

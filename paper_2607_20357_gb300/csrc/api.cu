@@ -1751,7 +1751,7 @@ svl_status svl_kv4_reorder(const svl_kv4_desc* desc, void* cache, int32_t n_laye
   if (st != SVL_OK) return st;
   if (n_layers <= 0 || beams <= 0 || !parent || !len) return SVL_ERR_INVALID_ARG;
   if (a.c.n_slots % beams) return SVL_ERR_SHAPE;
-  if (beams > kKv4MaxBeams || static_cast<int64_t>(n_layers) * (a.c.n_slots / beams) > kKv4MaxSlots)
+  if (beams > kKv4MaxBeams || static_cast<int64_t>(n_layers) * (a.c.n_slots / beams) > (1 << 30))
     return SVL_ERR_UNSUPPORTED;
   a.layers = n_layers;
   a.W = beams;
@@ -1759,7 +1759,7 @@ svl_status svl_kv4_reorder(const svl_kv4_desc* desc, void* cache, int32_t n_laye
   a.from = from;
   a.len = len;
   a.status = status;
-  g_launches++;
+  g_launches += kv4_reorder_launches(a);
   if (launch_kv4_reorder(a, static_cast<cudaStream_t>(stream)) != cudaSuccess) return SVL_ERR_CUDA;
   return last_error();
 }

@@ -435,11 +435,12 @@ cudaError_t launch_kv4_lengths(const int* cu_seqlens, int B, int beams, int* len
 // writes any of them, so the slots change in place whatever the parents are. Bound by the bytes read and written (the
 // slots that stay are not touched); a slot's bytes of a head are contiguous. 32 whole slots of 300 to 640 positions, 32
 // heads, four layers: 43.8 us (90 MB read, 166 MB written, 5.8 TB/s); the last 1 to 64 positions of 16 slots: 5.4 us.
-constexpr int kMoveThreads = 256;
+constexpr int kMoveThreads = 256, kMoveUnits = 65535;
 template <int W>
 __global__ void __launch_bounds__(kMoveThreads) kv4_reorder_kernel(Kv4Reorder a) {
   pdl_begin(false);
-  const int samples = a.c.n_slots / a.W, sample = blockIdx.z % samples, layer = blockIdx.z / samples;
+  const uint32_t samples = a.c.n_slots / a.W, unit = a.unit0 + blockIdx.z;
+  const int sample = unit % samples, layer = unit / samples;
   const int s0 = sample * a.W, TB = kv4_tile_bytes(a.c.dh);
   const int first = (a.from ? max(a.from[sample], 0) : 0) / kKv4Tile;
   // of each slot that moves: the parent, and the tiles that it holds
@@ -475,17 +476,24 @@ __global__ void __launch_bounds__(kMoveThreads) kv4_reorder_kernel(Kv4Reorder a)
   }
 }
 
-// Parts of at least 4 KB (a step of a block), as many as give each SM eight blocks.
-cudaError_t launch_kv4_reorder(const Kv4Reorder& a, cudaStream_t s) {
-  const int64_t heads = static_cast<int64_t>(a.c.kv) * a.layers * (a.c.n_slots / a.W);
+// Parts of at least 4 KB (a step of a block), as many as give each SM eight blocks; a launch for every 65,535 layers and
+// samples (along x, the only longer axis, they would be the fastest to change: the large call 43.8 -> 44.9 us).
+int kv4_reorder_launches(const Kv4Reorder& a) { return (a.layers * (a.c.n_slots / a.W) - 1) / kMoveUnits + 1; }
+cudaError_t launch_kv4_reorder(Kv4Reorder a, cudaStream_t s) {
+  const int units = a.layers * (a.c.n_slots / a.W);
+  const int64_t heads = static_cast<int64_t>(a.c.kv) * units;
   const int64_t words = static_cast<int64_t>(a.c.tiles) * kv4_tile_bytes(a.c.dh) / 16;
   const int64_t steps = (words + kMoveThreads - 1) / kMoveThreads;
   int64_t parts = (8 * 152 + heads - 1) / heads;
   parts = parts < steps ? parts : steps;
-  const dim3 grid(static_cast<unsigned>(parts), a.c.kv, a.c.n_slots / a.W * a.layers);
-  if (a.W <= 4) return launch_pdl(kv4_reorder_kernel<4>, grid, kMoveThreads, 0, s, a);
-  if (a.W <= 8) return launch_pdl(kv4_reorder_kernel<8>, grid, kMoveThreads, 0, s, a);
-  return launch_pdl(kv4_reorder_kernel<16>, grid, kMoveThreads, 0, s, a);
+  const auto kernel = a.W <= 4 ? kv4_reorder_kernel<4> : a.W <= 8 ? kv4_reorder_kernel<8> : kv4_reorder_kernel<16>;
+  for (a.unit0 = 0; a.unit0 < units; a.unit0 += kMoveUnits) {
+    const int n = units - a.unit0 < kMoveUnits ? units - a.unit0 : kMoveUnits;
+    const dim3 grid(static_cast<unsigned>(parts), a.c.kv, static_cast<unsigned>(n));
+    const cudaError_t e = launch_pdl(kernel, grid, kMoveThreads, 0, s, a);
+    if (e != cudaSuccess) return e;
+  }
+  return cudaSuccess;
 }
 
 }  // namespace svl

@@ -92,13 +92,15 @@ constexpr int kKv4MaxRows = 16;  // query rows per slot
 struct Kv4Reorder {
   Kv4Cache c;
   int layers, W;
+  int unit0;  // the launch's first (layer, sample)
   const int* parent;
   const int* from;
   const int* len;
   uint32_t* status;
 };
 constexpr int kKv4MaxBeams = 16;
-cudaError_t launch_kv4_reorder(const Kv4Reorder& a, cudaStream_t s);
+cudaError_t launch_kv4_reorder(Kv4Reorder a, cudaStream_t s);
+int kv4_reorder_launches(const Kv4Reorder& a);
 
 struct BeamArgs {
   int S, W, V, K;
