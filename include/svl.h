@@ -462,7 +462,7 @@ svl_status svl_kv4_reorder(const svl_kv4_desc* desc, void* cache, int32_t n_laye
 /* svl_gated_prefill_kv and svl_decode_step over a 4-bit cache: the caches of
  * the model's n_layers layers one after the other (n_layers *
  * svl_kv4_cache_size of {slots, n_kv_heads, d_head, max_len} bytes), max_len <=
- * the model's max_seq.
+ * the model's max_seq, and at most 4,096 slots (else SVL_ERR_UNSUPPORTED).
  * The prefill has room for `beams` slots per sample: sample b's prompt goes to
  * slot b * beams (svl_kv4_reorder with parent 0 hands it to the others), and
  * cache_len[b * beams + w] is its length for every w < beams. Prompt rows past

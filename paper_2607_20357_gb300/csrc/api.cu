@@ -108,7 +108,7 @@ size_t align256(size_t x) { return (x + 255) & ~size_t(255); }
 
 int round128(int x) { return (x + 127) & ~127; }
 
-constexpr int kMaxPrefillBatch = 4096;  // samples per prefill call
+constexpr int kMaxPrefillBatch = 4096;  // samples per prefill call, slots per decode step
 
 // Row capacity from which the QKV and gate/up GEMMs run on CTA pairs, which move
 // a third less per MMA. The host knows the capacity only; the rows are what the
@@ -1779,7 +1779,7 @@ svl_status svl_gated_prefill_kv4(svl_model* m, int32_t B, int32_t t_cap, void* X
                                  int32_t logits_mode, float* logits, void* cache, int32_t max_len, int32_t beams,
                                  int32_t* cache_len, void* ws, size_t ws_bytes, void* stream) {
   if (!m || B <= 0 || !cache_len || max_len <= 0 || max_len > m->d.max_seq || beams <= 0) return SVL_ERR_INVALID_ARG;
-  if (B > kKv4MaxSlots / beams) return SVL_ERR_UNSUPPORTED;
+  if (B > kMaxPrefillBatch / beams) return SVL_ERR_UNSUPPORTED;  // (more slots than a decode step takes)
   Kv4Cache c;
   const svl_status st = model_kv4(m, B * beams, max_len, cache, &c);
   if (st != SVL_OK) return st;
@@ -1791,7 +1791,7 @@ svl_status svl_gated_prefill_kv4(svl_model* m, int32_t B, int32_t t_cap, void* X
 }
 
 size_t svl_decode_kv4_workspace_size(const svl_model* m, int32_t n_slots, int32_t max_len) {
-  if (!m || n_slots <= 0) return 0;
+  if (!m || n_slots <= 0 || n_slots > kMaxPrefillBatch) return 0;
   const svl_kv4_desc d{n_slots, m->d.n_kv_heads, m->d.d_model / m->d.n_heads, max_len};
   const size_t attn = svl_kv4_attention_workspace_size(&d, m->d.n_heads, 1);
   return attn ? decode_kv4_attn_at(m, n_slots) + attn : 0;
@@ -1804,6 +1804,7 @@ svl_status svl_decode_step_kv4(svl_model* m, int32_t n_slots, const int32_t* tok
   if (!m || n_slots <= 0 || !tokens || max_len <= 0 || max_len > m->d.max_seq || !cache_len || !layer_gate ||
       !group_gate || !logits || window < 0 || sinks < 0)
     return SVL_ERR_INVALID_ARG;
+  if (n_slots > kMaxPrefillBatch) return SVL_ERR_UNSUPPORTED;
   Kv4Cache c;
   svl_status st = model_kv4(m, n_slots, max_len, cache, &c);
   if (st != SVL_OK) return st;
