@@ -364,7 +364,8 @@ svl_status svl_decode_step(svl_model* model, int32_t B, const int32_t* tokens, v
  * several layers' caches one after the other are one cache of
  * n_layers * n_slots slots. What a position holds before it is written, and
  * what lies past the positions a call names, is never used.
- * d_head is 64 or 128 (else SVL_ERR_UNSUPPORTED), n_slots at most 65,535. */
+ * d_head is 64 or 128, n_slots and n_kv_heads are at most 65,535, and a cache
+ * has less than 2^63 bytes (else SVL_ERR_UNSUPPORTED). */
 typedef struct svl_kv4_desc {
   int32_t n_slots;
   int32_t n_kv_heads;

@@ -1595,7 +1595,10 @@ svl_status kv4_cache(const svl_kv4_desc* d, const void* cache, bool sizes_only, 
   c->dh = d->d_head;
   c->max_len = d->max_len;
   c->tiles = (d->max_len - 1) / kKv4Tile + 1;
-  return SVL_OK;
+  // (65,535 slots of 65,535 heads of 2^31 positions are 2^70 bytes)
+  const uint64_t heads = static_cast<uint64_t>(c->n_slots) * c->kv;
+  const uint64_t head = static_cast<uint64_t>(c->tiles) * kv4_tile_bytes(c->dh);
+  return head > static_cast<uint64_t>(INT64_MAX) / heads ? SVL_ERR_UNSUPPORTED : SVL_OK;
 }
 
 svl_status kv4_rows(const svl_kv4_desc* d, const void* cache, const void* k, int64_t ld_k, const void* v, int64_t ld_v,
@@ -1631,7 +1634,7 @@ int device_sms() {
 size_t svl_kv4_cache_size(const svl_kv4_desc* desc) {
   Kv4Cache c;
   if (kv4_cache(desc, nullptr, true, &c) != SVL_OK) return 0;
-  return static_cast<size_t>(c.n_slots) * c.kv * c.tiles * kv4_tile_bytes(c.dh);
+  return kv4_layer_bytes(c);
 }
 
 svl_status svl_kv4_write(const svl_kv4_desc* desc, void* cache, const void* k, int64_t ld_k, const void* v,
