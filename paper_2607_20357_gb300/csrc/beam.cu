@@ -305,7 +305,9 @@ __global__ void __launch_bounds__(kKv4MaxBeams * 32) beam_join_kernel(BeamArgs a
 }
 
 // Parts of a row. 608 blocks (four on each SM) run at once, and a part costs a block as much as some 8,000 logits more:
-// the fewest waves times that, with parts of at least 4,096 logits (a chunk for each warp).
+// the fewest waves times that, with at most a part for every 4,096 logits or what is left of them (a chunk for each warp of
+// a whole one; equal parts can be shorter, so that some of the warps have no chunk: 2,560 logits each of 4,097 to 5,120).
+// All rows have as many parts: 256 rows of 152,064 have two each, 512 blocks in one wave.
 static BeamParts beam_parts(int S, int W, int V) {
   BeamParts p{};
   const int64_t rows = static_cast<int64_t>(S) * W;
