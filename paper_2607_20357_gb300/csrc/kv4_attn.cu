@@ -10,12 +10,15 @@
 //  - The products run on mma.m16n8 with float32 sums: S = K q with 16 positions as
 //    rows and 8 columns, O^T = V^T P with 16 dimensions as rows. A column is a query
 //    head of the KV head or one of its rows (drafted tokens); up to eight share one
-//    pass over the cache. (tcgen05 has 128 rows and takes its operands from shared
-//    memory, to which every dequantised value would have to be written first.)
+//    pass over the cache. (tcgen05 would take 128 rows at a time, from shared or tensor
+//    memory, to which every dequantised value would have to be written first, and leaves
+//    its sums in tensor memory, from which they would come back for each 32 dimensions,
+//    to be multiplied by their scales. Here codes and sums stay in registers.)
 //  - K's codes become float16 operands by masking alone: n * 2^-24 and n * 2^-20
 //    (subnormal numbers), both exact; q is scaled by a power of two to fill
 //    float16's range (bf16 has fewer bits, so that it is exact but for elements
-//    under 2^-29 of the head's largest), times 2^-4 where it meets the second kind.
+//    under 2^-31 of the head's largest), times 2^-4 where it meets the second kind,
+//    the odd dimensions (exact but for elements under 2^-27 of the largest).
 //    The -8 of s * (n - 8) costs nothing: the accumulators start at -8 * sum q of the
 //    group. The scales multiply the 32-dimension partial sums in float32. (e4m3
 //    operands would take fewer masks, but mma.sync converts them to float16 first.)
