@@ -17,8 +17,10 @@
 //
 // Measured (a copy runs at 6.8 TB/s, writing alone at 4.0): 7,156 rows of 32 KV heads
 // of 128 written in 29.4 us (150 MB, 5.1 TB/s; the ALU is busy two thirds of the time
-// with maxima, masks and codes, five operations a value), 16 rows in 3.3 us; 38,458
-// rows of four KV heads read in 17.3 us (101 MB, 5.8 TB/s; four fifths of the bytes are
+// with maxima, masks and codes, five operations a value), 16 rows in 3.3 us; the same
+// 7,156 rows with V transposed, as the prefill leaves it, in 59 us (30 by rows under the
+// same profiler: V comes in pieces of two bytes); 38,458
+// rows of four KV heads read in 17.5 us (101 MB, 5.8 TB/s; four fifths of the bytes are
 // written), 183 rows in 1.9 us. A thread per group instead took 491 and 257 us for the
 // large calls: its loads and stores are strided.
 #include "kv4.cuh"
@@ -275,9 +277,9 @@ __global__ void __launch_bounds__(kRowThreads) kv4_write_kernel(Kv4Rows a) {
     reinterpret_cast<uint16_t*>(tile + kv4_v_scales(DH))[(quad * 4 + t) * 2 * J + g] = static_cast<uint16_t>(s);
 }
 
-// One row per slot: a warp per (slot, KV head, K or V), four dimensions a lane. Bound by latency: a layer of a decode
-// step with 16 slots of 32 KV heads of 128 takes 5 us less, with 64 slots 7 us less than with the warps of the kernel
-// above, of whose eight positions one has a row.
+// One row per slot: a warp per (slot, KV head, K or V), four dimensions a lane. Bound by latency: 16 slots of 32 KV heads
+// of 128 take 1.8 us, 3.3 with the warps of the kernel above, of whose eight positions one has a row (V transposed, in a
+// decode step, the layer took 5 us less, with 64 slots 7).
 template <int DH, bool VT>
 __global__ void __launch_bounds__(kRowThreads) kv4_append_kernel(Kv4Rows a) {
   constexpr int J = DH / 32;

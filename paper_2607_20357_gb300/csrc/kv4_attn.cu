@@ -41,15 +41,15 @@
 //
 // Measured, d_head 128 (times of the call in a graph, rates of the cache's bytes; a
 // copy runs at 6.8 TB/s):
-//  - 32 heads of their own, 8 slots of 4,000 to 16,000 positions: 55.9 us, 5.7 TB/s
+//  - 32 heads of their own, 8 slots of 4,000 to 16,000 positions: 55.0 us, 5.8 TB/s
 //    (52.5 us without any arithmetic, some 6 of them launching and joining). Some 620
 //    instructions a tile, of which 337 are the ALU's, keep it busy 62 % of the time.
 //    16 slots of 250 to 450 positions: 12.3 us (8.6), two or three tiles a warp.
 //  - 28 heads on 4 KV heads (seven columns), 8 slots of 20,000 to 40,000 positions:
-//    37.5 us (26.7), 3.5 TB/s; four rows (28 columns, four passes) 112 us (45). Three warps
+//    37.6 us (26.7), 3.4 TB/s; four rows (28 columns, four passes) 113 us (45). Three warps
 //    per scheduler are all that the registers allow, each a chain of products,
-//    shuffles and exponentials: instructions issue in 62 % of the cycles, and no
-//    single kind of arithmetic left out saves more than 8 %.
+//    shuffles and exponentials: instructions issue in 47 and 58 % of the cycles, and
+//    no single kind of arithmetic left out saves more than 8 %.
 //  - one slot of 1,900 positions, 28 heads on 4 KV heads: 7.4 us of latencies (8.4 with
 //    the second launch): launching 0.8, queries and first tile 1.3, a tile 1.1, its end
 //    0.5, the warps' parts 1.0, the cluster's some 1.
