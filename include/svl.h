@@ -321,6 +321,71 @@ svl_status svl_quantize_rows_e4m3(const void* src, const void* gain, int64_t row
 svl_status svl_gemm_e4m3(svl_model* model, const void* A, const float* a_scale, const void* B, const float* b_scale,
                          int32_t M, int32_t N, int32_t K, float* C, void* stream);
 
+/* ------------------------------------------------------------------------
+ * Matrices in 4-bit floating point with a scale for every 32 values (MXFP4),
+ * 4.25 bits a value, and their product (the paper calls quantisation orthogonal
+ * to its method, Sec. 5). No model is needed.
+ *
+ * A matrix [rows, cols] is held as codes and scales, both caller-owned device
+ * memory, 16-byte aligned. Codes: e2m1 (0, 0.5, 1, 1.5, 2, 3, 4, 6, with a sign in
+ * bit 3), two to a byte, the earlier value in the low nibble; a row takes
+ * ceil(cols / 32) * 16 bytes, rows are `ld` BYTES apart (a multiple of 16), and
+ * behind a row's end the last block holds zeros. Scales: a byte b for every 32
+ * values stands for 2^(b - 127), 255 for NaN; 128 rows by 4 blocks make 512
+ * bytes, [ceil(rows / 128)][ceil(cols / 128)][row % 32][row % 128 / 32]
+ * [block % 4], svl_mxf4_scale_size() bytes in all (0 on bad arguments). The
+ * scales of blocks behind a row's end are zeros; those of rows that do not exist
+ * are never used. cols is at most 2^30 (else SVL_ERR_UNSUPPORTED). */
+size_t svl_mxf4_scale_size(int64_t rows, int32_t cols);
+
+/* Quantises rows of bf16 (`ld_src` elements apart). With x = src[r, c] * gain[c]
+ * (float32; gain is a device bf16 [cols] vector, or NULL for x = src[r, c]) and a
+ * the largest |x| of a block, the block's exponent is the smallest e >= -127
+ * with a <= 6 * 2^e, its scale byte e + 127 and its codes e2m1(x * 2^-e), rounded
+ * to nearest, ties to the even code. A block with a NaN or an infinity gets the
+ * scale 255 and codes of zero. With inv_rms (device float32 [rows], or NULL) it
+ * also writes 1 / sqrt(mean(src[r, :]^2) + eps): an RMSNorm's factor of the
+ * whole row, which svl_gemm_mxf4 applies after the product (row_factor).
+ * Nothing outside the rows is written, but for the zeros that fill up their last
+ * block and their tiles of scales along the columns.
+ * Requires cols and ld_src multiples of 8, ld_src >= cols, 16-byte aligned src
+ * (and gain), ld_dst >= ceil(cols / 32) * 16, eps finite and not negative (else
+ * SVL_ERR_INVALID_ARG). rows may be 0. Asynchronous on `stream`, as all calls
+ * here. */
+svl_status svl_quantize_rows_mxf4(const void* src, const void* gain, int64_t rows, int32_t cols, int64_t ld_src,
+                                  void* dst, int64_t ld_dst, void* scale, float eps, float* inv_rms, void* stream);
+
+/* The hidden rows of a gated MLP, quantised as they are made: the same of
+ * x = gate / (1 + exp(-gate)) * up (float32, each operation rounded). gate and up
+ * are bf16 rows, ld_gate and ld_up elements apart (they may be the two halves of
+ * the rows of one product). */
+svl_status svl_swiglu_rows_mxf4(const void* gate, int64_t ld_gate, const void* up, int64_t ld_up, int64_t rows,
+                                int32_t cols, void* dst, int64_t ld_dst, void* scale, void* stream);
+
+/* Reads rows back as bf16 (`ld_dst` elements apart): 2^(b - 127) times the code's
+ * value, exact wherever bf16 has it (a block with values above 5 * 2^125 may read
+ * as infinity). Requires cols and ld_dst multiples of 8, ld_dst >= cols and a
+ * 16-byte aligned dst (else SVL_ERR_INVALID_ARG). */
+svl_status svl_dequantize_rows_mxf4(const void* src, int64_t ld_src, const void* scale, int64_t rows, int32_t cols,
+                                    void* dst, int64_t ld_dst, void* stream);
+
+/* C[m, n] = row_factor[m] * sum_k A[m, k] B[n, k] + residual[m, n] of two matrices
+ * held as above, A [M, K] (activations) and B [N, K] (a weight, nn.Linear layout):
+ * the sum in float32 on the block-scaled tensor cores, the factor (device
+ * float32 [M], or NULL for 1) and the sum with the residual (C's type, ld_residual
+ * elements apart, or NULL for none) in float32, and one rounding to C's type
+ * (SVL_OUT_F32 or SVL_OUT_BF16; ld_c elements apart). C may be the residual
+ * itself, and overlaps no other argument. The result does not depend on what
+ * else runs. Any M (0: nothing is done), N and K; ld_c and ld_residual at least N
+ * (else SVL_ERR_INVALID_ARG). A device wait that ran out of time sets
+ * SVL_DEV_TIMEOUT in *status (device uint32, or NULL). */
+#define SVL_OUT_F32 0
+#define SVL_OUT_BF16 1
+svl_status svl_gemm_mxf4(const void* A, int64_t ld_a, const void* a_scale, const void* B, int64_t ld_b,
+                         const void* b_scale, int32_t M, int32_t N, int32_t K, const float* row_factor,
+                         const void* residual, int64_t ld_residual, void* C, int64_t ld_c, int32_t type,
+                         uint32_t* status, void* stream);
+
 /* svl_gated_prefill that also stores every layer's keys and values of the
  * prompt into the cache and writes cache_len[B] (device int32) = the prompt
  * length S_b of each sample. Errors: as svl_gated_prefill; prompt rows past

@@ -12,6 +12,7 @@
 #include "gemm.cuh"
 #include "kernels.cuh"
 #include "kv4.cuh"
+#include "mxf4.cuh"
 
 using namespace svl;
 
@@ -103,6 +104,23 @@ bool make_map8(CUtensorMap* m, const void* ptr, uint64_t rows, uint64_t cols, ui
                   CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
   return r == CUDA_SUCCESS;
 }
+
+}  // namespace
+
+bool svl::make_byte_map(CUtensorMap* m, const void* ptr, uint64_t rows, uint64_t bytes, uint64_t ld, uint32_t box_rows) {
+  auto fn = encode_fn();
+  if (!fn || !ptr || rows == 0 || bytes == 0 || (reinterpret_cast<uintptr_t>(ptr) & 15) || (ld & 15)) return false;
+  cuuint64_t dims[2] = {bytes, rows};
+  cuuint64_t strides[1] = {ld};
+  cuuint32_t box[2] = {128, box_rows};
+  cuuint32_t estr[2] = {1, 1};
+  CUresult r = fn(m, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void*>(ptr), dims, strides, box, estr,
+                  CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                  CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  return r == CUDA_SUCCESS;
+}
+
+namespace {
 
 size_t align256(size_t x) { return (x + 255) & ~size_t(255); }
 
@@ -1864,6 +1882,131 @@ svl_status svl_gemm_e4m3(svl_model* m, const void* A, const float* a_scale, cons
   svl_status st = launch(EPI_F32, m, SVL_TAG_LMHEAD, p, static_cast<int64_t>(p.grid_m) * p.grid_n,
                          static_cast<cudaStream_t>(stream), true);
   return st != SVL_OK ? st : last_error();
+}
+
+// ---------------------------------------------------------------- MXFP4
+namespace {
+constexpr int kMxMaxCols = 1 << 30;  // (column counts rounded up to a tile stay in 32 bits)
+
+bool mxf4_held(const void* codes, int64_t ld, const void* scale, int64_t cols) {
+  return codes && scale && aligned16(codes) && aligned16(scale) && ld >= mxf4_row_bytes(cols) && !(ld & 15);
+}
+bool rows_of_8(const void* p, int64_t ld, int32_t cols) { return p && aligned16(p) && ld >= cols && !(ld & 7); }
+
+// What quantising, SwiGLU and reading back check alike.
+svl_status mxf4_rows(int64_t rows, int32_t cols, const void* codes, int64_t ld_codes, const void* scale, int* sms) {
+  if (rows < 0 || cols <= 0 || (cols & 7) || !mxf4_held(codes, ld_codes, scale, cols)) return SVL_ERR_INVALID_ARG;
+  if (cols > kMxMaxCols || rows > INT64_MAX / 4 / cols) return SVL_ERR_UNSUPPORTED;
+  if (rows > 0 && !(*sms = device_sms())) return SVL_ERR_CUDA;
+  return SVL_OK;
+}
+}  // namespace
+
+size_t svl_mxf4_scale_size(int64_t rows, int32_t cols) {
+  if (rows <= 0 || cols <= 0 || cols > kMxMaxCols || rows > INT64_MAX / 4 / (cols + 127)) return 0;
+  return static_cast<size_t>(mxf4_scale_bytes(rows, cols));
+}
+
+svl_status svl_quantize_rows_mxf4(const void* src, const void* gain, int64_t rows, int32_t cols, int64_t ld_src,
+                                  void* dst, int64_t ld_dst, void* scale, float eps, float* inv_rms, void* stream) {
+  Mxf4Rows a;
+  std::memset(&a, 0, sizeof(a));
+  if (!rows_of_8(src, ld_src, cols) || (gain && !aligned16(gain)) || (reinterpret_cast<uintptr_t>(inv_rms) & 3) ||
+      (inv_rms && !(eps >= 0.f && std::isfinite(eps))))
+    return SVL_ERR_INVALID_ARG;
+  const svl_status st = mxf4_rows(rows, cols, dst, ld_dst, scale, &a.num_sms);
+  if (st != SVL_OK || rows == 0) return st;
+  a.src = static_cast<const __nv_bfloat16*>(src);
+  a.other = static_cast<const __nv_bfloat16*>(gain);
+  a.ld_src = ld_src;
+  a.rows = rows;
+  a.cols = cols;
+  a.codes = static_cast<uint8_t*>(dst);
+  a.ld_codes = ld_dst;
+  a.scale = static_cast<uint8_t*>(scale);
+  a.eps = eps;
+  a.inv_rms = inv_rms;
+  g_launches++;
+  if (launch_mxf4_quantize(gain ? MX_GAIN : MX_ROWS, a, static_cast<cudaStream_t>(stream)) != cudaSuccess)
+    return SVL_ERR_CUDA;
+  return last_error();
+}
+
+svl_status svl_swiglu_rows_mxf4(const void* gate, int64_t ld_gate, const void* up, int64_t ld_up, int64_t rows,
+                                int32_t cols, void* dst, int64_t ld_dst, void* scale, void* stream) {
+  Mxf4Rows a;
+  std::memset(&a, 0, sizeof(a));
+  if (!rows_of_8(gate, ld_gate, cols) || !rows_of_8(up, ld_up, cols)) return SVL_ERR_INVALID_ARG;
+  const svl_status st = mxf4_rows(rows, cols, dst, ld_dst, scale, &a.num_sms);
+  if (st != SVL_OK || rows == 0) return st;
+  a.src = static_cast<const __nv_bfloat16*>(gate);
+  a.other = static_cast<const __nv_bfloat16*>(up);
+  a.ld_src = ld_gate;
+  a.ld_other = ld_up;
+  a.rows = rows;
+  a.cols = cols;
+  a.codes = static_cast<uint8_t*>(dst);
+  a.ld_codes = ld_dst;
+  a.scale = static_cast<uint8_t*>(scale);
+  g_launches++;
+  if (launch_mxf4_quantize(MX_SWIGLU, a, static_cast<cudaStream_t>(stream)) != cudaSuccess) return SVL_ERR_CUDA;
+  return last_error();
+}
+
+svl_status svl_dequantize_rows_mxf4(const void* src, int64_t ld_src, const void* scale, int64_t rows, int32_t cols,
+                                    void* dst, int64_t ld_dst, void* stream) {
+  Mxf4Read a;
+  std::memset(&a, 0, sizeof(a));
+  if (!rows_of_8(dst, ld_dst, cols)) return SVL_ERR_INVALID_ARG;
+  const svl_status st = mxf4_rows(rows, cols, src, ld_src, scale, &a.num_sms);
+  if (st != SVL_OK || rows == 0) return st;
+  a.codes = static_cast<const uint8_t*>(src);
+  a.ld_codes = ld_src;
+  a.scale = static_cast<const uint8_t*>(scale);
+  a.rows = rows;
+  a.cols = cols;
+  a.dst = static_cast<__nv_bfloat16*>(dst);
+  a.ld_dst = ld_dst;
+  g_launches++;
+  if (launch_mxf4_dequantize(a, static_cast<cudaStream_t>(stream)) != cudaSuccess) return SVL_ERR_CUDA;
+  return last_error();
+}
+
+svl_status svl_gemm_mxf4(const void* A, int64_t ld_a, const void* a_scale, const void* B, int64_t ld_b,
+                         const void* b_scale, int32_t M, int32_t N, int32_t K, const float* row_factor,
+                         const void* residual, int64_t ld_residual, void* C, int64_t ld_c, int32_t type,
+                         uint32_t* status, void* stream) {
+  if (M < 0 || N <= 0 || K <= 0 || !mxf4_held(A, ld_a, a_scale, K) || !mxf4_held(B, ld_b, b_scale, K) || !C ||
+      ld_c < N || (residual && ld_residual < N) || (type != SVL_OUT_F32 && type != SVL_OUT_BF16) ||
+      (reinterpret_cast<uintptr_t>(row_factor) & 3) || (reinterpret_cast<uintptr_t>(status) & 3))
+    return SVL_ERR_INVALID_ARG;
+  const uintptr_t size = type == SVL_OUT_F32 ? 4 : 2;
+  if (reinterpret_cast<uintptr_t>(C) % size || reinterpret_cast<uintptr_t>(residual) % size) return SVL_ERR_INVALID_ARG;
+  if (K > kMxMaxCols) return SVL_ERR_UNSUPPORTED;
+  if (M == 0) return SVL_OK;
+  Mxf4Gemm g;
+  std::memset(&g, 0, sizeof(g));
+  g.a = static_cast<const uint8_t*>(A);
+  g.b = static_cast<const uint8_t*>(B);
+  g.ld_a = ld_a;
+  g.ld_b = ld_b;
+  g.a_scale = static_cast<const uint8_t*>(a_scale);
+  g.b_scale = static_cast<const uint8_t*>(b_scale);
+  g.M = M;
+  g.N = N;
+  g.K = K;
+  g.row_factor = row_factor;
+  g.residual = residual;
+  g.ld_residual = ld_residual;
+  g.c = C;
+  g.ld_c = ld_c;
+  g.f32 = type == SVL_OUT_F32;
+  g.status = status;
+  if (!(g.num_sms = device_sms())) return SVL_ERR_CUDA;
+  g_launches++;
+  const cudaError_t e = launch_mxf4_gemm(g, static_cast<cudaStream_t>(stream));
+  if (e != cudaSuccess) return e == cudaErrorInvalidValue ? SVL_ERR_INVALID_ARG : SVL_ERR_CUDA;
+  return last_error();
 }
 
 svl_status svl_flops(const svl_model_desc* d, int32_t s_text, int32_t s_vis, int32_t n_vis, const uint8_t* lg,

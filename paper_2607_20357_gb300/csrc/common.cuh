@@ -488,6 +488,48 @@ __host__ __device__ constexpr uint32_t idesc_e4m3_f32(int M, int N) {
   return (1u << 4) | (static_cast<uint32_t>(N >> 3) << 17) | (static_cast<uint32_t>(M >> 4) << 24);
 }
 
+// ---------------------------------------------------------------- block-scaled MMA (kind::mxf4)
+// D[tmem] (+)= (A * SA)[smem] * (B * SB)[smem]^T with e2m1 operands, two to a
+// byte, K = 64 per instruction (the same 32 bytes of each swizzled row), and a
+// power-of-two scale (ue8m0) for every 32 values of K. The scales are in tensor
+// memory: a 32-bit column holds those of 32 rows, one per lane and repeated in
+// all four lane quarters, for four blocks of K, of which the instruction
+// descriptor picks two.
+SVL_DEVINL void tc_mma_mxf4(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t sa_tmem,
+                            uint32_t sb_tmem, uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "setp.ne.b32 p, %6, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;\n\t}" ::"r"(
+          d_tmem),
+      "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(sa_tmem), "r"(sb_tmem), "r"(accumulate)
+      : "memory");
+}
+
+// 512 bytes of scales (32 rows of 16 bytes, shared memory) to four columns of
+// tensor memory, in all four lane quarters. In order with the MMAs that the same
+// thread issues before and after it.
+SVL_DEVINL void tc_copy_scales(uint32_t d_tmem, uint64_t desc) {
+  asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(d_tmem), "l"(desc) : "memory");
+}
+
+// Descriptor of those 512 bytes: rows of 16 bytes without swizzle, eight-row
+// groups 128 bytes apart.
+SVL_DEVINL uint64_t smem_desc_scales(uint32_t smem_addr) {
+  return static_cast<uint64_t>((smem_addr >> 4) & 0x3FFF) | (static_cast<uint64_t>(128 >> 4) << 32) |
+         (static_cast<uint64_t>(1) << 46);
+}
+
+// kind::mxf4 instruction descriptor: A and B e2m1 (format 1 in bits 7-9 and
+// 10-12), N >> 3 at bits 17-22, ue8m0 scales (bit 23), M >> 4 at bits 24-28;
+// `half` (0 or 1): the first or the last two of the columns' four blocks (bytes
+// 0 or 2, at bits 29-30 for A and 4-5 for B).
+__host__ __device__ constexpr uint32_t idesc_mxf4(int M, int N, int half) {
+  return (1u << 7) | (1u << 10) | (static_cast<uint32_t>(N >> 3) << 17) | (1u << 23) |
+         (static_cast<uint32_t>(M >> 4) << 24) | (static_cast<uint32_t>(2 * half) << 29) |
+         (static_cast<uint32_t>(2 * half) << 4);
+}
+
 // Two floats to two e4m3 codes, round to nearest even, saturating to the
 // largest finite value (448).
 SVL_DEVINL uint16_t e4m3x2(float lo, float hi) {

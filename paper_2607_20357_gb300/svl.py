@@ -24,6 +24,7 @@ SVL_FLAG_OVER_BUDGET = 1
 SVL_FLAG_GROUPS_DROPPED = 2
 SVL_DEV_NONFINITE, SVL_DEV_TIMEOUT, SVL_DEV_BAD_INDEX = 1, 2, 4
 SVL_GEMM_BF16, SVL_GEMM_E4M3 = 0, 1
+SVL_OUT_F32, SVL_OUT_BF16 = 0, 1
 SVL_LAYER_QKV, SVL_LAYER_ATTN, SVL_LAYER_OPROJ, SVL_LAYER_GATEUP, SVL_LAYER_DOWN = 0, 1, 2, 3, 4
 
 SYMBOLS = ["svl_model_create", "svl_model_destroy", "svl_workspace_size", "svl_score_select", "svl_pack",
@@ -35,7 +36,8 @@ SYMBOLS = ["svl_model_create", "svl_model_destroy", "svl_workspace_size", "svl_s
            "svl_quantize_rows_e4m3", "svl_gemm_e4m3", "svl_layer_stage", "svl_ksplit_plan", "svl_kv4_cache_size",
            "svl_kv4_write", "svl_kv4_read", "svl_kv4_attention_workspace_size", "svl_kv4_attention",
            "svl_beam_select_workspace_size", "svl_beam_select", "svl_kv4_reorder", "svl_gated_prefill_kv4",
-           "svl_decode_kv4_workspace_size", "svl_decode_step_kv4"]
+           "svl_decode_kv4_workspace_size", "svl_decode_step_kv4", "svl_mxf4_scale_size", "svl_quantize_rows_mxf4",
+           "svl_swiglu_rows_mxf4", "svl_dequantize_rows_mxf4", "svl_gemm_mxf4"]
 
 TAGS = ["budget_embed", "score", "select", "pack", "projector", "schedule", "rmsnorm", "qkv_gemm", "attention",
         "o_gemm", "gateup_gemm", "down_gemm", "lm_head", "host_copy", "quant"]
@@ -163,6 +165,16 @@ def lib():
         L.svl_decode_kv4_workspace_size.restype = sz
         L.svl_decode_step_kv4.argtypes = [vp, i32, vp, vp, i32, vp, vp, vp, i32, i32, vp, vp, vp, sz, vp]
         L.svl_decode_step_kv4.restype = ctypes.c_int
+        L.svl_mxf4_scale_size.argtypes = [i64, i32]
+        L.svl_mxf4_scale_size.restype = sz
+        L.svl_quantize_rows_mxf4.argtypes = [vp, vp, i64, i32, i64, vp, i64, vp, ctypes.c_float, vp, vp]
+        L.svl_quantize_rows_mxf4.restype = ctypes.c_int
+        L.svl_swiglu_rows_mxf4.argtypes = [vp, i64, vp, i64, i64, i32, vp, i64, vp, vp]
+        L.svl_swiglu_rows_mxf4.restype = ctypes.c_int
+        L.svl_dequantize_rows_mxf4.argtypes = [vp, i64, vp, i64, i32, vp, i64, vp]
+        L.svl_dequantize_rows_mxf4.restype = ctypes.c_int
+        L.svl_gemm_mxf4.argtypes = [vp, i64, vp, vp, i64, vp, i32, i32, i32, vp, vp, i64, vp, i64, i32, vp, vp]
+        L.svl_gemm_mxf4.restype = ctypes.c_int
         _lib = L
     return _lib
 
@@ -259,6 +271,39 @@ def svl_quantize_rows_e4m3(src, rows, cols, ld_src, dst, ld_dst, scale, stream=N
 def svl_gemm_e4m3(model, A, a_scale, B, b_scale, M, N, K, C, stream=None):
     _check("svl_gemm_e4m3", lib().svl_gemm_e4m3(model, _p(A), _p(a_scale), _p(B), _p(b_scale), int(M), int(N),
                                                 int(K), _p(C), _stream(stream)))
+
+
+def svl_mxf4_scale_size(rows, cols) -> int:
+    """Bytes of the scales of a [rows, cols] MXFP4 matrix (0 on bad arguments)."""
+    return int(lib().svl_mxf4_scale_size(int(rows), int(cols)))
+
+
+def svl_quantize_rows_mxf4(src, rows, cols, ld_src, dst, ld_dst, scale, stream=None, gain=None, eps=0.0, inv_rms=None):
+    """bf16 rows (times a gain) to MXFP4, and the rows' 1/rms (see svl.h; ld_dst in bytes)."""
+    _check("svl_quantize_rows_mxf4", lib().svl_quantize_rows_mxf4(
+        _p(src), _p(gain), int(rows), int(cols), int(ld_src), _p(dst), int(ld_dst), _p(scale), float(eps), _p(inv_rms),
+        _stream(stream)))
+
+
+def svl_swiglu_rows_mxf4(gate, ld_gate, up, ld_up, rows, cols, dst, ld_dst, scale, stream=None):
+    """SiLU(gate) * up to MXFP4 (see svl.h; ld_dst in bytes)."""
+    _check("svl_swiglu_rows_mxf4", lib().svl_swiglu_rows_mxf4(
+        _p(gate), int(ld_gate), _p(up), int(ld_up), int(rows), int(cols), _p(dst), int(ld_dst), _p(scale),
+        _stream(stream)))
+
+
+def svl_dequantize_rows_mxf4(src, ld_src, scale, rows, cols, dst, ld_dst, stream=None):
+    """MXFP4 rows back to bf16 (see svl.h; ld_src in bytes)."""
+    _check("svl_dequantize_rows_mxf4", lib().svl_dequantize_rows_mxf4(
+        _p(src), int(ld_src), _p(scale), int(rows), int(cols), _p(dst), int(ld_dst), _stream(stream)))
+
+
+def svl_gemm_mxf4(A, ld_a, a_scale, B, ld_b, b_scale, M, N, K, C, ld_c, out_type, stream=None, row_factor=None,
+                  residual=None, ld_residual=0, status=None):
+    """C = row_factor * (A B^T) + residual of MXFP4 matrices (see svl.h; ld_a and ld_b in bytes)."""
+    _check("svl_gemm_mxf4", lib().svl_gemm_mxf4(
+        _p(A), int(ld_a), _p(a_scale), _p(B), int(ld_b), _p(b_scale), int(M), int(N), int(K), _p(row_factor),
+        _p(residual), int(ld_residual), _p(C), int(ld_c), int(out_type), _p(status), _stream(stream)))
 
 
 def svl_layer_stage(model, stage, layer, B, t_cap, X, cu_seqlens, pos, layer_gate, group_gate, q=None, k=None,
