@@ -107,17 +107,33 @@ bool make_map8(CUtensorMap* m, const void* ptr, uint64_t rows, uint64_t cols, ui
 
 }  // namespace
 
-bool svl::make_byte_map(CUtensorMap* m, const void* ptr, uint64_t rows, uint64_t bytes, uint64_t ld, uint32_t box_rows) {
+// A 2-D map without further ado: `inner` elements a row, `ld` bytes apart.
+static bool make_map_2d(CUtensorMap* m, CUtensorMapDataType type, const void* ptr, uint64_t inner, uint64_t rows,
+                        uint64_t ld, uint32_t box_inner, uint32_t box_rows, CUtensorMapSwizzle swizzle) {
   auto fn = encode_fn();
-  if (!fn || !ptr || rows == 0 || bytes == 0 || (reinterpret_cast<uintptr_t>(ptr) & 15) || (ld & 15)) return false;
-  cuuint64_t dims[2] = {bytes, rows};
+  if (!fn || !ptr || rows == 0 || inner == 0 || (reinterpret_cast<uintptr_t>(ptr) & 15) || (ld & 15)) return false;
+  cuuint64_t dims[2] = {inner, rows};
   cuuint64_t strides[1] = {ld};
-  cuuint32_t box[2] = {128, box_rows};
+  cuuint32_t box[2] = {box_inner, box_rows};
   cuuint32_t estr[2] = {1, 1};
-  CUresult r = fn(m, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void*>(ptr), dims, strides, box, estr,
-                  CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-                  CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  CUresult r = fn(m, type, 2, const_cast<void*>(ptr), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle,
+                  CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
   return r == CUDA_SUCCESS;
+}
+
+bool svl::make_byte_map(CUtensorMap* m, const void* ptr, uint64_t rows, uint64_t bytes, uint64_t ld, uint32_t box_rows) {
+  return make_map_2d(m, CU_TENSOR_MAP_DATA_TYPE_UINT8, ptr, bytes, rows, ld, 128, box_rows, CU_TENSOR_MAP_SWIZZLE_128B);
+}
+
+bool svl::make_scale_map(CUtensorMap* m, const void* ptr, int64_t rows, int64_t cols, uint32_t box_tiles) {
+  const int64_t tiles = mxf4_scale_tiles(cols);
+  return make_map_2d(m, CU_TENSOR_MAP_DATA_TYPE_UINT32, ptr, tiles * (kMxTileBytes / 4), (rows + 127) / 128,
+                     tiles * kMxTileBytes, 2 * kMxTileBytes / 4, box_tiles, CU_TENSOR_MAP_SWIZZLE_NONE);
+}
+
+bool svl::make_result_map(CUtensorMap* m, const void* ptr, bool f32, uint64_t rows, uint64_t cols, uint64_t ld) {
+  return make_map_2d(m, f32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, ptr, cols, rows,
+                     ld * (f32 ? 4 : 2), f32 ? 32 : 64, 32, CU_TENSOR_MAP_SWIZZLE_128B);
 }
 
 namespace {

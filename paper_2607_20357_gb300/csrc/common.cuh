@@ -506,11 +506,29 @@ SVL_DEVINL void tc_mma_mxf4(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, u
       : "memory");
 }
 
+// The same of a CTA pair (M = 256). Each CTA's tensor memory holds the scales of
+// its own 128 rows of A and of all rows of B.
+SVL_DEVINL void tc_mma_mxf4_pair(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t sa_tmem,
+                                 uint32_t sb_tmem, uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "setp.ne.b32 p, %6, 0;\n\t"
+      "tcgen05.mma.cta_group::2.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;\n\t}" ::"r"(
+          d_tmem),
+      "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(sa_tmem), "r"(sb_tmem), "r"(accumulate)
+      : "memory");
+}
+
 // 512 bytes of scales (32 rows of 16 bytes, shared memory) to four columns of
 // tensor memory, in all four lane quarters. In order with the MMAs that the same
 // thread issues before and after it.
 SVL_DEVINL void tc_copy_scales(uint32_t d_tmem, uint64_t desc) {
   asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(d_tmem), "l"(desc) : "memory");
+}
+
+// Both CTAs of a pair copy from their own shared memory to their own tensor memory.
+SVL_DEVINL void tc_copy_scales_pair(uint32_t d_tmem, uint64_t desc) {
+  asm volatile("tcgen05.cp.cta_group::2.32x128b.warpx4 [%0], %1;" ::"r"(d_tmem), "l"(desc) : "memory");
 }
 
 // Descriptor of those 512 bytes: rows of 16 bytes without swizzle, eight-row

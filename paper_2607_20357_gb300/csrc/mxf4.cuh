@@ -76,9 +76,20 @@ struct Mxf4Gemm {
 };
 // cudaErrorInvalidValue: strides that no tensor map takes
 cudaError_t launch_mxf4_gemm(const Mxf4Gemm& g, cudaStream_t s);
+// Its kernel for large products, on CTA pairs.
+cudaError_t launch_mxf4_pair(const Mxf4Gemm& g, cudaStream_t s);
 
 // 2-D tensor map of `rows` rows of `bytes` bytes, `ld` bytes apart: boxes of
 // 128 bytes x box_rows with 128-byte swizzle; what lies outside reads as zeros.
 bool make_byte_map(CUtensorMap* m, const void* ptr, uint64_t rows, uint64_t bytes, uint64_t ld, uint32_t box_rows);
+// The scales of `rows` rows of `cols` values: boxes of two tiles (256 columns) x box_tiles tiles of 128 rows.
+bool make_scale_map(CUtensorMap* m, const void* ptr, int64_t rows, int64_t cols, uint32_t box_tiles);
+// A result [rows, cols] of float32 or bf16, `ld` elements apart: boxes of 128 bytes x 32 rows with 128-byte swizzle.
+bool make_result_map(CUtensorMap* m, const void* ptr, bool f32, uint64_t rows, uint64_t cols, uint64_t ld);
+
+SVL_DEVINL void mx_abort(volatile int* abort, uint32_t* status) {
+  *abort = 1;
+  report(status, SVL_DEV_TIMEOUT);
+}
 
 }  // namespace svl

@@ -58,11 +58,6 @@ SVL_DEVINL Mxf4Tile mxf4_tile(const Mxf4Params& p) {
 // Scale tiles (of 128 columns) in stage s.
 SVL_DEVINL int stage_k_tiles(int K, int s) { return K - s * kMxK > 128 ? 2 : 1; }
 
-SVL_DEVINL void mx_abort(volatile int* abort, uint32_t* status) {
-  *abort = 1;
-  report(status, SVL_DEV_TIMEOUT);
-}
-
 // One thread loads B (OP 0), one A (OP 1). Stage: codes of B, codes of A, scales of
 // B [k tile], scales of A [chunk of 128 rows][k tile].
 template <int OP>
@@ -247,6 +242,7 @@ __global__ void __launch_bounds__(kMxGemmThreads, 1) mxf4_tile_kernel(const __gr
 }
 
 cudaError_t launch_mxf4_gemm(const Mxf4Gemm& g, cudaStream_t s) {
+  if (g.M >= 1024) return launch_mxf4_pair(g, s);
   Mxf4Params p;
   p.g = g;
   p.nt = g.M <= kMxXMax ? (g.M + 15) / 16 * 16 : kMxXMax;

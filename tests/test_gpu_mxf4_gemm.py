@@ -70,7 +70,7 @@ def test_exact_sums(m, n, k, ld_a, ld_b, ld_c, kept, factor, residual):
     b, sb, vb = operand(n + k + 1, n, k, ld_b, 126, 129)
     f, r = whole(m, n, factor, residual, kept)
     assert np.sqrt((va ** 2).sum(1).max() * (vb ** 2).sum(1).max()) < 2 ** 18  # bounds any sum of magnitudes
-    ld_r = n + 3
+    ld_r = n + 3 if ld_c else n
     rr = None
     if residual:
         rr = torch.full((m, ld_r), float("nan"), dtype=kept)
