@@ -185,6 +185,8 @@ SVL_DEVINL void bulk_commit() { asm volatile("cp.async.bulk.commit_group;" ::: "
 SVL_DEVINL void bulk_wait_read0() { asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory"); }
 // ... of every committed store but the most recent one
 SVL_DEVINL void bulk_wait_read1() { asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory"); }
+// ... but the two most recent ones
+SVL_DEVINL void bulk_wait_read2() { asm volatile("cp.async.bulk.wait_group.read 2;" ::: "memory"); }
 // every committed store is complete
 SVL_DEVINL void bulk_wait0() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
 
@@ -399,6 +401,13 @@ SVL_DEVINL float4 ld_cluster4(uint32_t cluster_addr) {
 // Arrive on an mbarrier of another CTA of the cluster (release at cluster scope).
 SVL_DEVINL void mbar_arrive_cluster(uint32_t cluster_addr) {
   asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
+}
+
+// The same without release: for an arrival that orders tensor memory reads (complete
+// after tcgen05.wait::ld) before another thread's MMAs, and no memory accesses. Waiting
+// for the warp's earlier stores costs some 1,200 cycles behind a tile's results.
+SVL_DEVINL void mbar_arrive_cluster_relaxed(uint32_t cluster_addr) {
+  asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
 }
 
 // Every thread of both CTAs arrives, then waits (release / acquire at cluster scope).

@@ -242,7 +242,10 @@ __global__ void __launch_bounds__(kMxGemmThreads, 1) mxf4_tile_kernel(const __gr
 }
 
 cudaError_t launch_mxf4_gemm(const Mxf4Gemm& g, cudaStream_t s) {
-  if (g.M >= 1024) return launch_mxf4_pair(g, s);
+  #ifndef PAIR_MIN
+#define PAIR_MIN 1024
+#endif
+  if (g.M >= PAIR_MIN) return launch_mxf4_pair(g, s);
   Mxf4Params p;
   p.g = g;
   p.nt = g.M <= kMxXMax ? (g.M + 15) / 16 * 16 : kMxXMax;

@@ -219,7 +219,7 @@ SVL_DEVINL void mx_pair_epilogue(const Mxf4PairParams& p, uint64_t* done, uint64
         (ch.it & 1) ? (kPrOverlap + kCols - 1) / kCols : ch.n - (kPrTile - kPrOverlap) / kCols;
     if (ch.n == 0 || in_overlap <= 0) {
       __syncwarp();
-      if (lane == 0) mbar_arrive_cluster(release);
+      if (lane == 0) mbar_arrive_cluster_relaxed(release);
     }
     for (; ch.i < ch.n; ++ch.i) {
       float v[kCols];
@@ -229,7 +229,7 @@ SVL_DEVINL void mx_pair_epilogue(const Mxf4PairParams& p, uint64_t* done, uint64
       if (ch.i + 1 == min(in_overlap, ch.n)) {
         tc_fence_before();
         __syncwarp();
-        if (lane == 0) mbar_arrive_cluster(release);
+        if (lane == 0) mbar_arrive_cluster_relaxed(release);
       }
       if (p.tma) {
         uint8_t* slot0 = mine + buf * kPrChunk + lane * 128;
@@ -270,8 +270,13 @@ SVL_DEVINL void mx_pair_epilogue(const Mxf4PairParams& p, uint64_t* done, uint64
         if (lane == 0) {
           tma_store_2d(&p.c, mine + buf * kPrChunk, ch.n0 + col, ch.row0);
           bulk_commit();
-          bulk_wait_read1();  // the store before this one has read its buffer, which is the next but one
-          if (resid) request();
+          // a store's buffer is read before it is used again: by the chunk after the next two, or for its residual
+          if (resid) {
+            bulk_wait_read1();
+            request();
+          } else {
+            bulk_wait_read2();
+          }
         }
         __syncwarp();
         buf = buf == kPrChunks - 1 ? 0 : buf + 1;
