@@ -356,8 +356,8 @@ svl_status svl_quantize_rows_mxf4(const void* src, const void* gain, int64_t row
                                   void* dst, int64_t ld_dst, void* scale, float eps, float* inv_rms, void* stream);
 
 /* The hidden rows of a gated MLP, quantised as they are made: the same of
- * x = gate / (1 + exp(-gate)) * up (float32, each operation rounded). gate and up
- * are bf16 rows, ld_gate and ld_up elements apart (they may be the two halves of
+ * x = gate / (1 + exp(-gate)) * up (float32, within 7 * 2^-23 of it; gates under
+ * -87 may give 0). gate and up are bf16 rows, ld_gate and ld_up elements apart (they may be the two halves of
  * the rows of one product). */
 svl_status svl_swiglu_rows_mxf4(const void* gate, int64_t ld_gate, const void* up, int64_t ld_up, int64_t rows,
                                 int32_t cols, void* dst, int64_t ld_dst, void* scale, void* stream);
