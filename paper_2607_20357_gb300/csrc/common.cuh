@@ -415,6 +415,30 @@ SVL_DEVINL void cluster_sync() {
   asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
 
+// The same in two halves, without ordering memory: the arrival says that this thread
+// got here (its barriers' initialisation goes by fence_barrier_init).
+SVL_DEVINL void cluster_arrive_relaxed() { asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory"); }
+SVL_DEVINL void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
+
+// Four floats into a CTA of the cluster, counted as 16 bytes on an mbarrier there: data
+// and signal in one, where a store and an arrival would need a fence of some
+// 1,000 cycles between them. 16-byte aligned.
+SVL_DEVINL void st_async4(uint32_t cluster_addr, uint32_t cluster_bar, const float* v) {
+  asm volatile("st.async.weak.shared::cluster.mbarrier::complete_tx::bytes.v4.f32 [%0], {%1, %2, %3, %4}, [%5];" ::"r"(
+                   cluster_addr),
+               "f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]), "r"(cluster_bar)
+               : "memory");
+}
+
+// `bytes` (a multiple of 16) of this CTA's shared memory into another CTA's of the
+// cluster, counted on an mbarrier there; all 16-byte aligned.
+SVL_DEVINL void bulk_to_cluster(uint32_t cluster_addr, const void* smem_src, uint32_t bytes, uint32_t cluster_bar) {
+  asm volatile("cp.async.bulk.shared::cluster.shared::cta.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(
+                   cluster_addr),
+               "r"(smem_u32(smem_src)), "r"(bytes), "r"(cluster_bar)
+               : "memory");
+}
+
 // TMA load into this CTA's shared memory whose completion is counted on an
 // mbarrier of either CTA of the pair (`mbar` a shared::cluster address).
 SVL_DEVINL void tma_load_2d_pair(void* smem_dst, const CUtensorMap* map, uint32_t mbar, int x, int y) {
@@ -460,11 +484,12 @@ SVL_DEVINL void tc_mma_e4m3_pair(uint32_t d_tmem, uint64_t a_desc, uint64_t b_de
 
 // Arrives on the mbarrier at `bar`'s offset in both CTAs of the pair once
 // every pair MMA issued so far by this thread is done.
-SVL_DEVINL void tc_commit_pair(uint64_t* bar) {
+// (`ctas`: the pair's bits among the cluster's CTAs, where it has more than one pair.)
+SVL_DEVINL void tc_commit_pair(uint64_t* bar, uint16_t ctas = 3) {
   asm volatile(
       "tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(
           smem_u32(bar)),
-      "h"(static_cast<uint16_t>(3))
+      "h"(ctas)
       : "memory");
 }
 

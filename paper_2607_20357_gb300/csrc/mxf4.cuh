@@ -76,8 +76,10 @@ struct Mxf4Gemm {
 };
 // cudaErrorInvalidValue: strides that no tensor map takes
 cudaError_t launch_mxf4_gemm(const Mxf4Gemm& g, cudaStream_t s);
-// Its kernel for large products, on CTA pairs.
+// Its kernel for more than 128 rows, on CTA pairs.
 cudaError_t launch_mxf4_pair(const Mxf4Gemm& g, cudaStream_t s);
+// How many clusters of 2, 4 or 8 CTAs the device runs at once, an SM to a CTA.
+int mxf4_clusters(int ctas);
 
 // 2-D tensor map of `rows` rows of `bytes` bytes, `ld` bytes apart: boxes of
 // 128 bytes x box_rows with 128-byte swizzle; what lies outside reads as zeros.

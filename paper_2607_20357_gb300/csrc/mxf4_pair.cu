@@ -15,7 +15,10 @@
 // (in both CTAs: the MMAs have read stage s), done (in both: a tile's MMAs are
 // complete), taken (leader's: both epilogues have read the overlap, so the
 // tile before is read altogether).
+//
+// Where tiles are few, clusters of two or four pairs share a tile's K.
 #include <algorithm>
+#include <atomic>
 
 #include "mxf4.cuh"
 
@@ -29,9 +32,9 @@ constexpr int kPrScalesB = 4 * kMxTileBytes;
 constexpr int kPrStageBytes = 2 * kPrCodes + kPrScalesA + kPrScalesB;
 constexpr int kPrStages = 5;
 constexpr int kPrChunk = 32 * 128;  // bytes of an epilogue chunk: 32 rows of 128 bytes
-constexpr int kPrChunks = 3;        // buffers of a warp
-constexpr int kPrSmem = 1024 + kPrStages * kPrStageBytes + 1024 + 4 * kPrChunks * kPrChunk;
-constexpr int kPrThreads = 192;  // warp 0 loads, warp 1 MMAs (leader), warps 2-5 epilogue
+constexpr int kPrOutWarps = 8;      // two for each quarter of the lanes, with every other chunk of columns
+constexpr int kPrSmem = 1024 + kPrStages * kPrStageBytes + 1024 + kPrOutWarps * kPrChunk;
+constexpr int kPrThreads = 64 + 32 * kPrOutWarps;  // warp 0 loads, warp 1 MMAs (leader), the others epilogue
 constexpr int kPrSets = 2;       // sets of scales in tensor memory, used in turn
 constexpr int kPrOverlap = 24 * kPrSets;
 constexpr int kPrGroup = 8;  // tiles of rows that are walked together
@@ -41,8 +44,29 @@ struct Mxf4PairParams {
   CUtensorMap a, b, a_scale, b_scale, c, residual;
   Mxf4Gemm g;
   int m_tiles, n_tiles, tiles;
-  bool tma;  // C and the residual go by TMA
+  int log_split;  // pairs of a cluster, each with a share of K
+  bool tma;       // C and the residual go by TMA
 };
+
+// What is the same for all of a CTA's tiles.
+struct PairPlace {
+  int rank, part;       // in the pair; the pair in its cluster
+  uint32_t leader;      // the leader's rank in the cluster
+  int first, stride;    // tiles
+  int s0, s1;           // stages of K
+};
+SVL_DEVINL PairPlace pair_place(const Mxf4PairParams& p) {
+  PairPlace w;
+  const int cr = static_cast<int>(cluster_rank()), all = (p.g.K - 1) / kPrK + 1;
+  w.rank = cr & 1;
+  w.part = cr >> 1;
+  w.leader = static_cast<uint32_t>(cr & ~1);
+  w.first = static_cast<int>(blockIdx.x >> (1 + p.log_split));
+  w.stride = static_cast<int>(gridDim.x >> (1 + p.log_split));
+  w.s0 = (all * w.part) >> p.log_split;
+  w.s1 = (all * (w.part + 1)) >> p.log_split;
+  return w;
+}
 
 struct PairTile {
   int m0, n0;
@@ -58,11 +82,8 @@ SVL_DEVINL PairTile pair_tile(const Mxf4PairParams& p, int t) {
   return ti;
 }
 
-SVL_DEVINL int pair_stages(int K) { return (K - 1) / kPrK + 1; }
-
-SVL_DEVINL void mx_pair_producer(const Mxf4PairParams& p, uint8_t* stages, uint64_t* full, uint64_t* empty,
-                                 uint32_t rank, volatile int* abort) {
-  const int n_stages = pair_stages(p.g.K);
+SVL_DEVINL void mx_pair_producer(const Mxf4PairParams& p, const PairPlace& w, uint8_t* stages, uint64_t* full,
+                                 uint64_t* empty, volatile int* abort) {
   int s = 0;
   uint32_t ph = 1;
   auto next = [&]() {
@@ -71,14 +92,14 @@ SVL_DEVINL void mx_pair_producer(const Mxf4PairParams& p, uint8_t* stages, uint6
       ph ^= 1;
     }
   };
-  for (int t = blockIdx.x >> 1; t < p.tiles; t += gridDim.x >> 1) {
+  for (int t = w.first; t < p.tiles; t += w.stride) {
     const PairTile ti = pair_tile(p, t);
-    const int m0 = ti.m0 + static_cast<int>(rank) * 128, n0 = ti.n0 + static_cast<int>(rank) * 128;
-    for (int k = 0; k < n_stages; ++k, next()) {
+    const int m0 = ti.m0 + w.rank * 128, n0 = ti.n0 + w.rank * 128;
+    for (int k = w.s0; k < w.s1; ++k, next()) {
       if (!mbar_wait(&empty[s], ph, abort)) return mx_abort(abort, p.g.status);
       uint8_t* st = stages + s * kPrStageBytes;
-      if (rank == 0) mbar_arrive_expect_tx(&full[s], 2 * kPrStageBytes);
-      const uint32_t fb = mapa_shared(&full[s], 0);
+      if (w.rank == 0) mbar_arrive_expect_tx(&full[s], 2 * kPrStageBytes);
+      const uint32_t fb = mapa_shared(&full[s], w.leader);
       tma_load_2d_pair(st, &p.a, fb, k * 128, m0);
       tma_load_2d_pair(st + kPrCodes, &p.b, fb, k * 128, n0);
       tma_load_2d_pair(st + 2 * kPrCodes, &p.a_scale, fb, k * 256, m0 >> 7);
@@ -92,19 +113,19 @@ SVL_DEVINL void mx_pair_producer(const Mxf4PairParams& p, uint8_t* stages, uint6
 
 SVL_DEVINL uint32_t pair_acc(uint32_t tmem, int it) { return tmem + ((it & 1) ? kPrTile - kPrOverlap : 0); }
 
-SVL_DEVINL void mx_pair_mma(const Mxf4PairParams& p, uint8_t* stages, uint64_t* full, uint64_t* empty, uint64_t* done,
-                            uint64_t* taken, uint32_t tmem, volatile int* abort) {
-  const int n_stages = pair_stages(p.g.K);
+SVL_DEVINL void mx_pair_mma(const Mxf4PairParams& p, const PairPlace& w, uint8_t* stages, uint64_t* full,
+                            uint64_t* empty, uint64_t* done, uint64_t* taken, uint32_t tmem, volatile int* abort) {
   const uint32_t base = smem_u32(stages);
   constexpr uint32_t id0 = idesc_mxf4(kPrTile, kPrTile, 0), id1 = idesc_mxf4(kPrTile, kPrTile, 1);
+  const uint16_t ctas = static_cast<uint16_t>(3u << w.leader);
   int s = 0, it = 0;
   uint32_t ph = 0, set = 0;
-  for (int t = blockIdx.x >> 1; t < p.tiles; t += gridDim.x >> 1, ++it) {
+  for (int t = w.first; t < p.tiles; t += w.stride, ++it) {
     if (it > 0 && !mbar_wait(taken, (it - 1) & 1, abort)) return mx_abort(abort, p.g.status);
     tc_fence_after();
     const uint32_t d = pair_acc(tmem, it);
     uint32_t accumulate = 0;
-    for (int k = 0; k < n_stages; ++k) {
+    for (int k = w.s0; k < w.s1; ++k) {
       if (!mbar_wait(&full[s], ph, abort)) return mx_abort(abort, p.g.status);
       tc_fence_after();
       const uint32_t st = base + s * kPrStageBytes, sc = st + 2 * kPrCodes;
@@ -128,49 +149,48 @@ SVL_DEVINL void mx_pair_mma(const Mxf4PairParams& p, uint8_t* stages, uint64_t* 
           accumulate = 1;
         }
       }
-      tc_commit_pair(&empty[s]);
+      tc_commit_pair(&empty[s], ctas);
       if (++s == kPrStages) {
         s = 0;
         ph ^= 1;
       }
       if (++set == kPrSets) set = 0;
     }
-    tc_commit_pair(done);
+    tc_commit_pair(done, ctas);
   }
 }
 
-// The chunks of a warp, over all of its tiles: 128 bytes of 32 rows of C. In
-// accumulator 1 they are taken from the left, in accumulator 0 from the right.
+// The chunks of a warp, over all of its tiles: 128 bytes of 32 rows of C, every
+// other of a tile's. In accumulator 1 they are taken from the left, in accumulator
+// 0 from the right. Where K is shared (one tile a cluster), a CTA has the columns
+// that it adds up.
 template <bool F32>
 struct PairChunks {
   static constexpr int kCols = F32 ? 32 : 64;
   const Mxf4PairParams& p;
-  int t, it, row0, quarter;  // tile, its number, the warp's first row, its rows' offset in the tile
-  int n0, n, i;              // tile's first column, its chunks (0: no rows of the warp exist), the present one
-  SVL_DEVINL PairChunks(const Mxf4PairParams& params, int offset) : p(params), quarter(offset) {
-    t = blockIdx.x >> 1;
-    it = 0;
+  const PairPlace& w;
+  int t, it, row0, offset, half;  // tile, its number, the warp's first row, its rows' offset in the tile, first chunk
+  int n0, n, i;                   // tile's first column, its chunks (0: no rows of the warp exist), the present one
+  SVL_DEVINL PairChunks(const Mxf4PairParams& params, const PairPlace& place, int rows_at, int first)
+      : p(params), w(place), t(place.first), it(0), offset(rows_at), half(first) {
     enter();
   }
   SVL_DEVINL void enter() {
-    i = 0;
+    i = half;
     n = 0;
     if (t >= p.tiles) return;
     const PairTile ti = pair_tile(p, t);
-    row0 = ti.m0 + quarter;
-    n0 = ti.n0;
-    if (row0 < p.g.M) n = (min(kPrTile, p.g.N - n0) + kCols - 1) / kCols;
+    row0 = ti.m0 + offset;
+    const int width = kPrTile >> p.log_split;
+    n0 = ti.n0 + w.part * width;
+    if (row0 < p.g.M) n = (max(0, min(width, p.g.N - n0)) + kCols - 1) / kCols;
   }
   SVL_DEVINL void next_tile() {
-    t += gridDim.x >> 1;
+    t += w.stride;
     ++it;
     enter();
   }
-  // the next chunk there is, in this tile or a later one
-  SVL_DEVINL void next_chunk() {
-    ++i;
-    settle();
-  }
+  // to a chunk that there is, in this tile or a later one
   SVL_DEVINL void settle() {
     while (i >= n && t < p.tiles) next_tile();
   }
@@ -178,142 +198,235 @@ struct PairChunks {
   SVL_DEVINL int column() const { return ((it & 1) ? i : n - 1 - i) * kCols; }
 };
 
+// A warp's results on their way out: its buffer in shared memory, and the next
+// chunk of the residual, requested when the buffer is free.
 template <bool F32>
-SVL_DEVINL void mx_pair_epilogue(const Mxf4PairParams& p, uint64_t* done, uint64_t* taken, uint64_t* loaded,
-                                 uint32_t tmem, uint32_t rank, uint8_t* buffers, volatile int* abort) {
-  constexpr int kCols = F32 ? 32 : 64;
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, q = warp & 3;
-  uint8_t* mine = buffers + q * kPrChunks * kPrChunk;
-  loaded += q * kPrChunks;
-  const int offset = static_cast<int>(rank) * 128 + q * 32;
-  const uint32_t release = mapa_shared(taken, 0);
-  PairChunks<F32> ch(p, offset), ahead(p, offset);
-  const bool resid = p.g.residual != nullptr;
-  int buf = 0, ahead_buf = 0;  // buffers of the present chunk and of the one that is requested next
-  uint32_t parity = 0;         // of each buffer's next wait
-  auto request = [&]() {
-    if (ahead.more()) {
-      mbar_arrive_expect_tx(&loaded[ahead_buf], kPrChunk);
-      tma_load_2d(mine + ahead_buf * kPrChunk, &p.residual, &loaded[ahead_buf], ahead.n0 + ahead.column(), ahead.row0);
-      ahead_buf = ahead_buf == kPrChunks - 1 ? 0 : ahead_buf + 1;
-      ahead.next_chunk();
-    }
-  };
-  if (resid && p.tma) {
-    ahead.settle();
-    if (lane == 0) {
-      request();
-      request();
-    }
+struct PairOut {
+  static constexpr int kCols = F32 ? 32 : 64;
+  const Mxf4PairParams& p;
+  uint8_t* buffer;
+  uint64_t* loaded;
+  PairChunks<F32> ahead;
+  volatile int* abort;
+  uint32_t parity = 0;
+  SVL_DEVINL PairOut(const Mxf4PairParams& params, const PairChunks<F32>& chunks, uint8_t* room, uint64_t* bar,
+                     volatile int* flag)
+      : p(params), buffer(room), loaded(bar), ahead(chunks), abort(flag) {
+    if (p.g.residual && p.tma && (threadIdx.x & 31) == 0) request();
   }
+  SVL_DEVINL void request() {
+    ahead.settle();
+    if (!ahead.more()) return;
+    mbar_arrive_expect_tx(loaded, kPrChunk);
+    tma_load_2d(buffer, &p.residual, loaded, ahead.n0 + ahead.column(), ahead.row0);
+    ahead.i += 2;
+  }
+  // The chunk from column n0 and row row0 on: the factor and the sum with the
+  // residual in float32, one rounding to C's type.
+  SVL_DEVINL bool chunk(const float* v, float factor, int n0, int row0) {
+    const int lane = threadIdx.x & 31;
+    const bool resid = p.g.residual != nullptr;
+    if (p.tma) {
+      if (resid) {
+        const bool got = mbar_wait(loaded, parity, abort);
+        parity ^= 1;
+        __syncwarp();
+        if (!__all_sync(0xffffffffu, got)) return false;
+      } else {
+        if (lane == 0) bulk_wait_read0();  // the store before has read the buffer
+        __syncwarp();
+      }
+      uint8_t* slot0 = buffer + lane * 128;
+#pragma unroll
+      for (int c = 0; c < 8; ++c) {
+        // 16-byte piece c of the row, where the 128-byte swizzle has it
+        uint4* slot = reinterpret_cast<uint4*>(slot0 + ((c ^ (lane & 7)) << 4));
+        uint32_t o[4];
+        uint4 x = make_uint4(0, 0, 0, 0);
+        if (resid) x = *slot;
+        const uint32_t xw[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          if constexpr (F32) {
+            float y = __fmul_rn(v[4 * c + k], factor);
+            if (resid) y = __fadd_rn(y, __uint_as_float(xw[k]));
+            o[k] = __float_as_uint(y);
+          } else {
+            float y0 = __fmul_rn(v[8 * c + 2 * k], factor), y1 = __fmul_rn(v[8 * c + 2 * k + 1], factor);
+            if (resid) {
+              const float2 f = unpack_bf16x2(xw[k]);
+              y0 = __fadd_rn(y0, f.x);
+              y1 = __fadd_rn(y1, f.y);
+            }
+            o[k] = pack_bf16x2(y0, y1);
+          }
+        }
+        *slot = make_uint4(o[0], o[1], o[2], o[3]);
+      }
+      fence_proxy_async();  // generic-proxy writes, read by the TMA unit
+      __syncwarp();
+      if (lane == 0) {
+        tma_store_2d(&p.c, buffer, n0, row0);
+        bulk_commit();
+        if (resid) {
+          bulk_wait_read0();
+          request();
+        }
+      }
+      return true;
+    }
+    // rows of any alignment: turned in shared memory, a row of the chunk by a warp's consecutive lanes
+    float* turn = reinterpret_cast<float*>(buffer);
+#pragma unroll
+    for (int c = 0; c < kCols; c += 32) {
+#pragma unroll
+      for (int j = 0; j < 32; ++j) turn[lane * 32 + (j ^ lane)] = __fmul_rn(v[c + j], factor);
+      __syncwarp();
+      const int n = n0 + c + lane;
+      if (n < p.g.N) {
+        // (eight rows' residuals are requested before the first of them is stored over)
+        for (int r0 = 0; r0 < 32; r0 += 8) {
+          float y[8];
+#pragma unroll
+          for (int r = 0; r < 8; ++r) {
+            const int64_t m = row0 + r0 + r;
+            y[r] = 0.f;
+            if (resid && m < p.g.M)
+              y[r] = F32 ? static_cast<const float*>(p.g.residual)[m * p.g.ld_residual + n]
+                         : __bfloat162float(static_cast<const __nv_bfloat16*>(p.g.residual)[m * p.g.ld_residual + n]);
+          }
+#pragma unroll
+          for (int r = 0; r < 8; ++r) {
+            const int64_t m = row0 + r0 + r;
+            if (m >= p.g.M) break;
+            float x = turn[(r0 + r) * 32 + (lane ^ (r0 + r))];
+            if (resid) x = __fadd_rn(x, y[r]);
+            if constexpr (F32)
+              static_cast<float*>(p.g.c)[m * p.g.ld_c + n] = x;
+            else
+              static_cast<__nv_bfloat16*>(p.g.c)[m * p.g.ld_c + n] = __float2bfloat16_rn(x);
+          }
+        }
+      }
+      __syncwarp();
+    }
+    return true;
+  }
+};
+
+// Where a warp reads the accumulators, and its chunks.
+struct PairWarp {
+  int lane, q, half;  // quarter of the lanes, first chunk
+  SVL_DEVINL PairWarp() : lane(threadIdx.x & 31), q((threadIdx.x >> 5) & 3), half((threadIdx.x - 64) >> 7) {}
+  SVL_DEVINL int index() const { return q * 2 + half; }
+  SVL_DEVINL uint32_t lanes() const { return static_cast<uint32_t>(q * 32) << 16; }
+};
+
+template <bool F32>
+SVL_DEVINL void mx_pair_epilogue(const Mxf4PairParams& p, const PairPlace& w, uint64_t* done, uint64_t* taken,
+                                 uint64_t* loaded, uint32_t tmem, uint8_t* buffers, volatile int* abort) {
+  constexpr int kCols = F32 ? 32 : 64;
+  const PairWarp me;
+  const uint32_t release = mapa_shared(taken, w.leader);
+  PairChunks<F32> ch(p, w, w.rank * 128 + me.q * 32, me.half);
+  PairOut<F32> out(p, ch, buffers + me.index() * kPrChunk, loaded + me.index(), abort);
   for (; ch.more(); ch.next_tile()) {
-    const int row = ch.row0 + lane;
+    const int row = ch.row0 + me.lane;
     const float factor = p.g.row_factor && ch.n > 0 && row < p.g.M ? p.g.row_factor[row] : 1.f;
     const bool ok = mbar_wait(done, ch.it & 1, abort);
     __syncwarp();
     if (!__all_sync(0xffffffffu, ok)) return mx_abort(abort, p.g.status);
     tc_fence_after();
-    const uint32_t acc = pair_acc(tmem, ch.it) + (static_cast<uint32_t>(q * 32) << 16);
-    // chunks that hold the overlap: where the tile's columns end before it, there is nothing to wait for
-    const int in_overlap =
-        (ch.it & 1) ? (kPrOverlap + kCols - 1) / kCols : ch.n - (kPrTile - kPrOverlap) / kCols;
-    if (ch.n == 0 || in_overlap <= 0) {
-      __syncwarp();
-      if (lane == 0) mbar_arrive_cluster_relaxed(release);
-    }
-    for (; ch.i < ch.n; ++ch.i) {
+    const uint32_t acc = pair_acc(tmem, ch.it) + me.lanes();
+    // Chunks that hold the overlap come first; a warp hands over when it has read the last of its own. (Where the
+    // tile's columns end before the overlap, there is none.)
+    const int in_overlap = min(
+        ch.n, (ch.it & 1) ? (kPrOverlap + kCols - 1) / kCols : ch.n - (kPrTile - kPrOverlap) / kCols);
+    bool handed = ch.i >= in_overlap;
+    if (handed && me.lane == 0) mbar_arrive_cluster_relaxed(release);
+    for (; ch.i < ch.n; ch.i += 2) {
       float v[kCols];
       const int col = ch.column();
 #pragma unroll
       for (int c = 0; c < kCols; c += 32) tmem_ld32(acc + col + c, v + c);
-      if (ch.i + 1 == min(in_overlap, ch.n)) {
+      if (!handed && ch.i + 2 >= in_overlap) {
         tc_fence_before();
         __syncwarp();
-        if (lane == 0) mbar_arrive_cluster_relaxed(release);
+        if (me.lane == 0) mbar_arrive_cluster_relaxed(release);
+        handed = true;
       }
-      if (p.tma) {
-        uint8_t* slot0 = mine + buf * kPrChunk + lane * 128;
-        if (resid) {
-          const bool got = mbar_wait(&loaded[buf], (parity >> buf) & 1, abort);
-          parity ^= 1u << buf;
-          __syncwarp();
-          if (!__all_sync(0xffffffffu, got)) return mx_abort(abort, p.g.status);
-        }
-#pragma unroll
-        for (int c = 0; c < 8; ++c) {
-          // 16-byte piece c of the row, where the 128-byte swizzle has it
-          uint4* slot = reinterpret_cast<uint4*>(slot0 + ((c ^ (lane & 7)) << 4));
-          uint32_t o[4];
-          uint4 x = make_uint4(0, 0, 0, 0);
-          if (resid) x = *slot;
-          const uint32_t xw[4] = {x.x, x.y, x.z, x.w};
-#pragma unroll
-          for (int k = 0; k < 4; ++k) {
-            if constexpr (F32) {
-              float w = __fmul_rn(v[4 * c + k], factor);
-              if (resid) w = __fadd_rn(w, __uint_as_float(xw[k]));
-              o[k] = __float_as_uint(w);
-            } else {
-              float w0 = __fmul_rn(v[8 * c + 2 * k], factor), w1 = __fmul_rn(v[8 * c + 2 * k + 1], factor);
-              if (resid) {
-                const float2 f = unpack_bf16x2(xw[k]);
-                w0 = __fadd_rn(w0, f.x);
-                w1 = __fadd_rn(w1, f.y);
-              }
-              o[k] = pack_bf16x2(w0, w1);
-            }
-          }
-          *slot = make_uint4(o[0], o[1], o[2], o[3]);
-        }
-        fence_proxy_async();  // generic-proxy writes, read by the TMA unit
-        __syncwarp();
-        if (lane == 0) {
-          tma_store_2d(&p.c, mine + buf * kPrChunk, ch.n0 + col, ch.row0);
-          bulk_commit();
-          // a store's buffer is read before it is used again: by the chunk after the next two, or for its residual
-          if (resid) {
-            bulk_wait_read1();
-            request();
-          } else {
-            bulk_wait_read2();
-          }
-        }
-        __syncwarp();
-        buf = buf == kPrChunks - 1 ? 0 : buf + 1;
-      } else {
-        // rows of any alignment: turned in shared memory, a row of the chunk by a warp's consecutive lanes
-        float* turn = reinterpret_cast<float*>(mine);
-#pragma unroll
-        for (int c = 0; c < kCols; c += 32) {
-#pragma unroll
-          for (int j = 0; j < 32; ++j) turn[lane * 33 + j] = __fmul_rn(v[c + j], factor);
-          __syncwarp();
-          const int n = ch.n0 + col + c + lane;
-          if (n < p.g.N) {
-#pragma unroll 8
-            for (int r = 0; r < 32; ++r) {
-              const int64_t m = ch.row0 + r;
-              if (m >= p.g.M) break;
-              float w = turn[r * 33 + lane];
-              if constexpr (F32) {
-                if (resid) w = __fadd_rn(w, static_cast<const float*>(p.g.residual)[m * p.g.ld_residual + n]);
-                static_cast<float*>(p.g.c)[m * p.g.ld_c + n] = w;
-              } else {
-                if (resid)
-                  w = __fadd_rn(w, __bfloat162float(static_cast<const __nv_bfloat16*>(p.g.residual)[m * p.g.ld_residual + n]));
-                static_cast<__nv_bfloat16*>(p.g.c)[m * p.g.ld_c + n] = __float2bfloat16_rn(w);
-              }
-            }
-          }
-          __syncwarp();
-        }
-      }
+      if (!out.chunk(v, factor, ch.n0 + col, ch.row0)) return mx_abort(abort, p.g.status);
     }
   }
-  if (lane == 0) bulk_wait0();  // this warp's stores are complete
+  if (me.lane == 0) bulk_wait0();  // this warp's stores are complete
 }
 
+// The same where a cluster's pairs share a tile's K: each CTA sends the columns
+// that others add up to them, over the stages, which are used up everywhere
+// (`free_bar`), and adds what arrives to its own, in the order of the others.
+// Layout: [the others in order][group of four columns][128 rows][4].
 template <bool F32>
+SVL_DEVINL void mx_pair_shares(const Mxf4PairParams& p, const PairPlace& w, uint64_t* done, uint64_t* free_bar,
+                               uint64_t* arrived, uint64_t* loaded, uint32_t tmem, uint8_t* stages, uint8_t* buffers,
+                               volatile int* abort) {
+  constexpr int kCols = F32 ? 32 : 64;
+  const PairWarp me;
+  const int split = 1 << p.log_split, width = kPrTile >> p.log_split;
+  const int share = (width / 4) * 128 * 16;  // bytes
+  PairChunks<F32> ch(p, w, w.rank * 128 + me.q * 32, me.half);
+  PairOut<F32> out(p, ch, buffers + me.index() * kPrChunk, loaded + me.index(), abort);
+  const bool rows = ch.row0 < p.g.M;  // of this warp, which the other pairs' warps with the same place have too
+  const float factor = p.g.row_factor && ch.row0 + me.lane < p.g.M ? p.g.row_factor[ch.row0 + me.lane] : 1.f;
+  bool ok = mbar_wait(done, 0, abort);
+  __syncwarp();
+  ok = __all_sync(0xffffffffu, ok);
+  if (ok) {
+    if (me.index() == 0 && me.lane < split) mbar_arrive_cluster_relaxed(mapa_shared(free_bar, 2 * me.lane + w.rank));
+    ok = mbar_wait(free_bar, 0, abort);
+    __syncwarp();
+    ok = __all_sync(0xffffffffu, ok);
+  }
+  if (!ok) return mx_abort(abort, p.g.status);
+  if (!rows) return;
+  tc_fence_after();
+  const uint32_t acc = tmem + me.lanes();
+  const uint32_t place = static_cast<uint32_t>(me.q * 32 + me.lane) * 16;
+  for (int i = 1; i < split; ++i) {
+    const int o = (w.part + i) & (split - 1);  // (a CTA's first receiver is no other's)
+    const uint32_t to = mapa_shared(stages, 2 * o + w.rank) + (w.part < o ? w.part : w.part - 1) * share + place;
+    const uint32_t bar = mapa_shared(arrived, 2 * o + w.rank);
+    for (int c = 32 * me.half; c < width; c += 64) {
+      float v[32];
+      tmem_ld32(acc + o * width + c, v);
+#pragma unroll
+      for (int j = 0; j < 32; j += 4) st_async4(to + static_cast<uint32_t>((c + j) >> 2) * (128 * 16), bar, v + j);
+    }
+  }
+  ok = mbar_wait(arrived, 0, abort);
+  __syncwarp();
+  if (!__all_sync(0xffffffffu, ok)) return mx_abort(abort, p.g.status);
+  for (; ch.i < ch.n; ch.i += 2) {
+    float v[kCols];
+    const int col = ch.column();
+#pragma unroll
+    for (int c = 0; c < kCols; c += 32) tmem_ld32(acc + w.part * width + col + c, v + c);
+    const uint8_t* from = stages + (col >> 2) * (128 * 16) + place;
+    for (int s = 1; s < split; ++s, from += share) {
+#pragma unroll
+      for (int j = 0; j < kCols; j += 4) {
+        const float4 x = *reinterpret_cast<const float4*>(from + (j >> 2) * (128 * 16));
+        v[j] = __fadd_rn(v[j], x.x);
+        v[j + 1] = __fadd_rn(v[j + 1], x.y);
+        v[j + 2] = __fadd_rn(v[j + 2], x.z);
+        v[j + 3] = __fadd_rn(v[j + 3], x.w);
+      }
+    }
+    if (!out.chunk(v, factor, ch.n0 + col, ch.row0)) return mx_abort(abort, p.g.status);
+  }
+  if (me.lane == 0) bulk_wait0();
+}
+
+template <bool F32, bool SHARED>
 __global__ void __launch_bounds__(kPrThreads, 1) mxf4_pair_kernel(const __grid_constant__ Mxf4PairParams p) {
   extern __shared__ uint8_t smem_raw[];
   uint8_t* stages = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
@@ -321,10 +434,12 @@ __global__ void __launch_bounds__(kPrThreads, 1) mxf4_pair_kernel(const __grid_c
   uint64_t* empty = full + kPrStages;
   uint64_t* done = empty + kPrStages;
   uint64_t* taken = done + 1;
-  uint64_t* loaded = taken + 1;  // [4 warps][kPrChunks]
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(loaded + 4 * kPrChunks);
+  uint64_t* free_bar = taken + 1;
+  uint64_t* arrived = free_bar + 1;
+  uint64_t* loaded = arrived + 1;  // [epilogue warp]
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(loaded + kPrOutWarps);
   volatile int* abort = reinterpret_cast<volatile int*>(tmem_slot + 1);
-  const uint32_t rank = cluster_rank();
+  const PairPlace w = pair_place(p);
   const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0);  // uniform over the warp
   if (threadIdx.x == 0) {
     for (int i = 0; i < kPrStages; ++i) {
@@ -332,11 +447,19 @@ __global__ void __launch_bounds__(kPrThreads, 1) mxf4_pair_kernel(const __grid_c
       mbar_init(&empty[i], 1);
     }
     mbar_init(done, 1);
-    mbar_init(taken, 8);  // the epilogue warps of both CTAs
-    for (int i = 0; i < 4 * kPrChunks; ++i) mbar_init(&loaded[i], 1);
+    mbar_init(taken, 2 * kPrOutWarps);  // the epilogue warps of both CTAs
+    for (int i = 0; i < kPrOutWarps; ++i) mbar_init(&loaded[i], 1);
+    mbar_init(free_bar, 1u << p.log_split);
+    mbar_init(arrived, 1);
     *abort = 0;
     fence_barrier_init();
     fence_proxy_async();
+    if (SHARED) {
+      // from every other pair, for each warp here that has rows, 32 of them of a share
+      const int rows = p.g.M - pair_tile(p, w.first).m0 - w.rank * 128, warps = max(0, min(4, (rows + 31) >> 5));
+      const int others = (1 << p.log_split) - 1, width = kPrTile >> p.log_split;
+      mbar_arrive_expect_tx(arrived, static_cast<uint32_t>(others * warps * 32 * width * 4));
+    }
     prefetch_tmap(&p.a);
     prefetch_tmap(&p.b);
     prefetch_tmap(&p.a_scale);
@@ -349,16 +472,20 @@ __global__ void __launch_bounds__(kPrThreads, 1) mxf4_pair_kernel(const __grid_c
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  cluster_sync();  // both CTAs' barriers exist before any load or arrive reaches them
+  cluster_arrive_relaxed();
+  cluster_wait();  // the cluster's barriers exist before any load or arrive reaches them
   const uint32_t tmem = *tmem_slot;
   pdl_begin(false);
 
+  uint8_t* buffers = stages + kPrStages * kPrStageBytes + 1024;
   if (warp == 0) {
-    if (elect_one()) mx_pair_producer(p, stages, full, empty, rank, abort);
+    if (elect_one()) mx_pair_producer(p, w, stages, full, empty, abort);
   } else if (warp == 1) {
-    if (rank == 0 && elect_one()) mx_pair_mma(p, stages, full, empty, done, taken, tmem, abort);
+    if (w.rank == 0 && elect_one()) mx_pair_mma(p, w, stages, full, empty, done, taken, tmem, abort);
+  } else if constexpr (SHARED) {
+    mx_pair_shares<F32>(p, w, done, free_bar, arrived, loaded, tmem, stages, buffers, abort);
   } else {
-    mx_pair_epilogue<F32>(p, done, taken, loaded, tmem, rank, stages + kPrStages * kPrStageBytes + 1024, abort);
+    mx_pair_epilogue<F32>(p, w, done, taken, loaded, tmem, buffers, abort);
   }
 
   __syncwarp();
@@ -370,11 +497,48 @@ __global__ void __launch_bounds__(kPrThreads, 1) mxf4_pair_kernel(const __grid_c
   }
   tc_fence_before();
   __syncthreads();
-  cluster_sync();  // the peer is done with this CTA's barriers and tensor memory
+  // The peer is done with this CTA's barriers and tensor memory. (Nothing that was written is handed over here; with
+  // release semantics the barrier waits 1,000 cycles for the stores of results.)
+  cluster_arrive_relaxed();
+  cluster_wait();
   if (warp == 1) {
     tc_fence_after();
     tmem_dealloc_pair(tmem, 512);
   }
+}
+
+using PairKernel = void (*)(Mxf4PairParams);
+static PairKernel pair_kernel(int log_split, bool f32) {
+  return log_split ? (f32 ? mxf4_pair_kernel<true, true> : mxf4_pair_kernel<false, true>)
+                   : (f32 ? mxf4_pair_kernel<true, false> : mxf4_pair_kernel<false, false>);
+}
+
+// The answer is the device's (76, 36 and 15 clusters of 2, 4 and 8 CTAs on one
+// with 152 SMs): asked once, of the kernel that has an SM to a CTA.
+int mxf4_clusters(int ctas) {
+  static std::atomic<int> known[16][3];  // (0: not known yet)
+  const int log = ctas == 8 ? 2 : ctas == 4 ? 1 : 0;
+  int dev = 0, n = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess) return 0;
+  std::atomic<int>* place = dev < 16 ? &known[dev][log] : nullptr;
+  if (place && (n = place->load(std::memory_order_relaxed))) return n - 1;
+  PairKernel kernel = pair_kernel(log, true);
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(2u << log);
+  cfg.blockDim = dim3(kPrThreads);
+  cfg.dynamicSmemBytes = kPrSmem;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = 2u << log;
+  attr[0].val.clusterDim.y = 1;
+  attr[0].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kPrSmem) != cudaSuccess ||
+      cudaOccupancyMaxActiveClusters(&n, kernel, &cfg) != cudaSuccess)
+    return 0;
+  if (place) place->store(n + 1, std::memory_order_relaxed);
+  return n;
 }
 
 cudaError_t launch_mxf4_pair(const Mxf4Gemm& g, cudaStream_t s) {
@@ -389,14 +553,22 @@ cudaError_t launch_mxf4_pair(const Mxf4Gemm& g, cudaStream_t s) {
   if (!make_byte_map(&p.a, g.a, g.M, bytes, g.ld_a, 128) || !make_byte_map(&p.b, g.b, g.N, bytes, g.ld_b, 128) ||
       !make_scale_map(&p.a_scale, g.a_scale, g.M, g.K, 1) || !make_scale_map(&p.b_scale, g.b_scale, g.N, g.K, 2))
     return cudaErrorInvalidValue;
-  // Tensor stores want 16-byte rows; anything else goes by plain ones.
-  p.tma = make_result_map(&p.c, g.c, g.f32, g.M, g.N, g.ld_c) &&
+  // Tensor stores want 16-byte rows, and end a row at a multiple of 16 bytes; anything else goes by plain ones.
+  p.tma = (static_cast<int64_t>(g.N) * (g.f32 ? 4 : 2)) % 16 == 0 && make_result_map(&p.c, g.c, g.f32, g.M, g.N, g.ld_c) &&
           (!g.residual || make_result_map(&p.residual, g.residual, g.f32, g.M, g.N, g.ld_residual));
-  void (*kernel)(Mxf4PairParams) = g.f32 ? mxf4_pair_kernel<true> : mxf4_pair_kernel<false>;
+  // A cluster's pairs share K where all of its tiles' clusters run at once and K has the stages to make up for the
+  // sums' way. us for 1, 2 and 4 pairs: K 4,096 (16 stages), 8 tiles 9.2, 8.8, 8.5; 11,008, 4 tiles 17.2, 12.9, 10.4
+  // and 18 tiles 17.7, 14.0; 18,944, 14 tiles 26.3, 18.4, 14.7.
+  int log_split = 0;
+  if ((g.K - 1) / kPrK + 1 >= 16)
+    for (int l = 1; l <= 2 && tiles <= mxf4_clusters(2 << l); ++l) log_split = l;
+  p.log_split = log_split;
+  void (*kernel)(Mxf4PairParams) = pair_kernel(log_split, g.f32);
   cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kPrSmem);
   if (e != cudaSuccess) return e;
-  const int pairs = static_cast<int>(std::min<int64_t>(tiles, std::max(1, g.num_sms / 2)));
-  return launch_pdl_cluster(kernel, dim3(2 * pairs), kPrThreads, kPrSmem, 2, s, p);
+  const int ctas = 2 << log_split;
+  const int64_t clusters = log_split ? tiles : std::min<int64_t>(tiles, std::max(1, mxf4_clusters(2)));
+  return launch_pdl_cluster(kernel, dim3(static_cast<unsigned>(clusters * ctas)), kPrThreads, kPrSmem, ctas, s, p);
 }
 
 }  // namespace svl

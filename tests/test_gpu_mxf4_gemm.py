@@ -57,7 +57,10 @@ SHAPES = [
     (300, 3584, 1024, None, None, None), (384, 896, 2400, None, None, None), (513, 2050, 264, None, None, 2051),
     (700, 5000, 1152, None, None, None), (1025, 4224, 512, None, None, None), (2000, 7, 4096, None, None, None),
     (2600, 4096, 1312, None, None, None), (8, 32000, 4096, None, None, None), (1, 3584, 18944, None, None, None),
-    (40, 77, 18944, None, None, 80),
+    (40, 77, 18944, None, None, 80), (24, 300, 2000, None, None, None), (50, 640, 12288, None, None, 645),
+    (100, 640, 6000, None, None, None), (128, 300, 18944, None, None, None), (70, 20000, 320, None, None, None),
+    (16, 20000, 512, None, None, None), (130, 700, 4128, None, None, 703), (300, 3584, 4352, None, None, None),
+    (520, 1300, 8192, None, None, None), (1100, 129, 640, None, None, 136), (1100, 2052, 256, None, None, 2056),
 ]
 
 
