@@ -79,6 +79,7 @@ SVL_DEVINL void mx_producer(const Mxf4Params& p, const Mxf4Tile& t, uint8_t* sta
   scales += static_cast<int64_t>(t.s0) * (2 * kMxTileBytes);
   int slot = 0;
   uint32_t ph = 1;
+  pdl_wait();
   for (int s = t.s0; s < t.s1; ++s, scales += 2 * kMxTileBytes) {
     if (s - t.s0 >= p.stages && !mbar_wait(&empty[slot], ph, abort)) return mx_abort(abort, p.g.status);
     uint8_t* st = stages + slot * p.stage_bytes;
@@ -279,6 +280,7 @@ __global__ void __launch_bounds__(kMxGemmThreads, 2) mxf4_tile_kernel(const __gr
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(arrived + 1);
   volatile int* abort = reinterpret_cast<volatile int*>(tmem_slot + 1);
   const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
+  pdl_trigger();
   const Mxf4Tile t = mxf4_tile(p);
   const int split = 1 << p.log_split;
   const int mine = max(0, min(p.own, p.g.M - t.part * p.own));  // the columns of this CTA that exist
@@ -298,6 +300,8 @@ __global__ void __launch_bounds__(kMxGemmThreads, 2) mxf4_tile_kernel(const __gr
     prefetch_tmap(&p.w);
     prefetch_tmap(&p.x);
   }
+  __syncwarp();
+  if (split > 1) cluster_arrive_relaxed();  // (the first warp behind its barriers' initialisation)
   if (warp == 1) {
     tmem_alloc(tmem_slot, p.tmem_cols);
     tmem_relinquish();
@@ -305,9 +309,7 @@ __global__ void __launch_bounds__(kMxGemmThreads, 2) mxf4_tile_kernel(const __gr
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  if (split > 1) cluster_arrive_relaxed();
   const uint32_t tmem = *tmem_slot;
-  pdl_begin(false);
 
   if (warp == 0) {
     if (elect_one()) mx_producer<MX_W>(p, t, stages, full, empty, abort);
@@ -319,6 +321,7 @@ __global__ void __launch_bounds__(kMxGemmThreads, 2) mxf4_tile_kernel(const __gr
     if (elect_one()) mx_mma(p, t, stages, full, empty, done, tmem, abort);
   }
   __syncwarp();
+  pdl_wait();
   bool ok = mbar_wait(done, 0, abort);
   __syncwarp();
   ok = __all_sync(0xffffffffu, ok);

@@ -37,8 +37,12 @@ constexpr int kPrSmem = 1024 + kPrStages * kPrStageBytes + 1024 + kPrOutWarps * 
 constexpr int kPrThreads = 64 + 32 * kPrOutWarps;  // warp 0 loads, warp 1 MMAs (leader), the others epilogue
 constexpr int kPrSets = 2;       // sets of scales in tensor memory, used in turn
 constexpr int kPrOverlap = 24 * kPrSets;
+// The epilogue warps' second buffers are the end of the stages (behind shares of K, 96 KB at most), so many bytes
+// in front of their first.
+constexpr int kPrSecondBack = 1024 + kPrOutWarps * kPrChunk;
 constexpr int kPrGroup = 8;  // tiles of rows that are walked together
 static_assert(kPrSmem <= 232448, "shared memory per CTA");
+static_assert(kPrStages * kPrStageBytes - kPrOutWarps * kPrChunk >= 96 * 1024, "second buffers");
 
 struct Mxf4PairParams {
   CUtensorMap a, b, a_scale, b_scale, c, residual;
@@ -92,8 +96,9 @@ SVL_DEVINL void mx_pair_producer(const Mxf4PairParams& p, const PairPlace& w, ui
       ph ^= 1;
     }
   };
-  for (int t = w.first; t < p.tiles; t += w.stride) {
-    const PairTile ti = pair_tile(p, t);
+  PairTile ti = pair_tile(p, w.first);
+  pdl_wait();
+  for (int t = w.first; t < p.tiles; t += w.stride, ti = pair_tile(p, t)) {
     const int m0 = ti.m0 + w.rank * 128, n0 = ti.n0 + w.rank * 128;
     for (int k = w.s0; k < w.s1; ++k, next()) {
       if (!mbar_wait(&empty[s], ph, abort)) return mx_abort(abort, p.g.status);
@@ -199,27 +204,37 @@ struct PairChunks {
 };
 
 // A warp's results on their way out: its buffer in shared memory, and the next
-// chunk of the residual, requested when the buffer is free.
+// chunk of the residual, requested when the buffer is free. In the CTA's last tile
+// the stages are used up, and a second buffer in their place takes every other
+// chunk (a store holds its buffer for some 900 cycles).
 template <bool F32>
 struct PairOut {
   static constexpr int kCols = F32 ? 32 : 64;
   const Mxf4PairParams& p;
-  uint8_t* buffer;
-  uint64_t* loaded;
+  uint8_t* own;
+  uint64_t* loaded;  // [2]
   PairChunks<F32> ahead;
   volatile int* abort;
-  uint32_t parity = 0;
-  SVL_DEVINL PairOut(const Mxf4PairParams& params, const PairChunks<F32>& chunks, uint8_t* room, uint64_t* bar,
+  uint32_t parity = 0;  // of each buffer's next wait
+  bool last = false;    // in the last tile
+  int slot = 0;
+  SVL_DEVINL PairOut(const Mxf4PairParams& params, const PairChunks<F32>& chunks, uint8_t* first, uint64_t* bars,
                      volatile int* flag)
-      : p(params), buffer(room), loaded(bar), ahead(chunks), abort(flag) {
-    if (p.g.residual && p.tma && (threadIdx.x & 31) == 0) request();
+      : p(params), own(first), loaded(bars), ahead(chunks), abort(flag) {
+    if (p.g.residual && p.tma && (threadIdx.x & 31) == 0) request(0);
   }
-  SVL_DEVINL void request() {
+  SVL_DEVINL uint8_t* buffer(int b) const { return own - b * kPrSecondBack; }
+  SVL_DEVINL void request(int b) {
     ahead.settle();
     if (!ahead.more()) return;
-    mbar_arrive_expect_tx(loaded, kPrChunk);
-    tma_load_2d(buffer, &p.residual, loaded, ahead.n0 + ahead.column(), ahead.row0);
+    mbar_arrive_expect_tx(&loaded[b], kPrChunk);
+    tma_load_2d(buffer(b), &p.residual, &loaded[b], ahead.n0 + ahead.column(), ahead.row0);
     ahead.i += 2;
+  }
+  // The last tile's MMAs are complete.
+  SVL_DEVINL void enter_last() {
+    last = true;
+    if (p.g.residual && p.tma && (threadIdx.x & 31) == 0) request(1);
   }
   // The chunk from column n0 and row row0 on: the factor and the sum with the
   // residual in float32, one rounding to C's type.
@@ -227,16 +242,22 @@ struct PairOut {
     const int lane = threadIdx.x & 31;
     const bool resid = p.g.residual != nullptr;
     if (p.tma) {
+      uint8_t* const at = buffer(slot);
       if (resid) {
-        const bool got = mbar_wait(loaded, parity, abort);
-        parity ^= 1;
+        const bool got = mbar_wait(&loaded[slot], (parity >> slot) & 1, abort);
+        parity ^= 1u << slot;
         __syncwarp();
         if (!__all_sync(0xffffffffu, got)) return false;
       } else {
-        if (lane == 0) bulk_wait_read0();  // the store before has read the buffer
+        if (lane == 0) {  // the store before (in the last tile, the one before that) has read the buffer
+          if (last)
+            bulk_wait_read1();
+          else
+            bulk_wait_read0();
+        }
         __syncwarp();
       }
-      uint8_t* slot0 = buffer + lane * 128;
+      uint8_t* slot0 = at + lane * 128;
 #pragma unroll
       for (int c = 0; c < 8; ++c) {
         // 16-byte piece c of the row, where the 128-byte swizzle has it
@@ -266,17 +287,18 @@ struct PairOut {
       fence_proxy_async();  // generic-proxy writes, read by the TMA unit
       __syncwarp();
       if (lane == 0) {
-        tma_store_2d(&p.c, buffer, n0, row0);
+        tma_store_2d(&p.c, at, n0, row0);
         bulk_commit();
         if (resid) {
           bulk_wait_read0();
-          request();
+          request(slot);
         }
       }
+      if (last) slot ^= 1;
       return true;
     }
     // rows of any alignment: turned in shared memory, a row of the chunk by a warp's consecutive lanes
-    float* turn = reinterpret_cast<float*>(buffer);
+    float* turn = reinterpret_cast<float*>(own);
 #pragma unroll
     for (int c = 0; c < kCols; c += 32) {
 #pragma unroll
@@ -329,7 +351,8 @@ SVL_DEVINL void mx_pair_epilogue(const Mxf4PairParams& p, const PairPlace& w, ui
   const PairWarp me;
   const uint32_t release = mapa_shared(taken, w.leader);
   PairChunks<F32> ch(p, w, w.rank * 128 + me.q * 32, me.half);
-  PairOut<F32> out(p, ch, buffers + me.index() * kPrChunk, loaded + me.index(), abort);
+  pdl_wait();
+  PairOut<F32> out(p, ch, buffers + me.index() * kPrChunk, loaded + 2 * me.index(), abort);
   for (; ch.more(); ch.next_tile()) {
     const int row = ch.row0 + me.lane;
     const float factor = p.g.row_factor && ch.n > 0 && row < p.g.M ? p.g.row_factor[row] : 1.f;
@@ -337,6 +360,7 @@ SVL_DEVINL void mx_pair_epilogue(const Mxf4PairParams& p, const PairPlace& w, ui
     __syncwarp();
     if (!__all_sync(0xffffffffu, ok)) return mx_abort(abort, p.g.status);
     tc_fence_after();
+    if (ch.t + w.stride >= p.tiles) out.enter_last();
     const uint32_t acc = pair_acc(tmem, ch.it) + me.lanes();
     // Chunks that hold the overlap come first; a warp hands over when it has read the last of its own. (Where the
     // tile's columns end before the overlap, there is none.)
@@ -374,13 +398,15 @@ SVL_DEVINL void mx_pair_shares(const Mxf4PairParams& p, const PairPlace& w, uint
   const int split = 1 << p.log_split, width = kPrTile >> p.log_split;
   const int share = (width / 4) * 128 * 16;  // bytes
   PairChunks<F32> ch(p, w, w.rank * 128 + me.q * 32, me.half);
-  PairOut<F32> out(p, ch, buffers + me.index() * kPrChunk, loaded + me.index(), abort);
+  pdl_wait();
+  PairOut<F32> out(p, ch, buffers + me.index() * kPrChunk, loaded + 2 * me.index(), abort);
   const bool rows = ch.row0 < p.g.M;  // of this warp, which the other pairs' warps with the same place have too
   const float factor = p.g.row_factor && ch.row0 + me.lane < p.g.M ? p.g.row_factor[ch.row0 + me.lane] : 1.f;
   bool ok = mbar_wait(done, 0, abort);
   __syncwarp();
   ok = __all_sync(0xffffffffu, ok);
   if (ok) {
+    out.enter_last();
     if (me.index() == 0 && me.lane < split) mbar_arrive_cluster_relaxed(mapa_shared(free_bar, 2 * me.lane + w.rank));
     ok = mbar_wait(free_bar, 0, abort);
     __syncwarp();
@@ -436,9 +462,10 @@ __global__ void __launch_bounds__(kPrThreads, 1) mxf4_pair_kernel(const __grid_c
   uint64_t* taken = done + 1;
   uint64_t* free_bar = taken + 1;
   uint64_t* arrived = free_bar + 1;
-  uint64_t* loaded = arrived + 1;  // [epilogue warp]
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(loaded + kPrOutWarps);
+  uint64_t* loaded = arrived + 1;  // [epilogue warp][2]
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(loaded + 2 * kPrOutWarps);
   volatile int* abort = reinterpret_cast<volatile int*>(tmem_slot + 1);
+  pdl_trigger();
   const PairPlace w = pair_place(p);
   const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0);  // uniform over the warp
   if (threadIdx.x == 0) {
@@ -448,7 +475,7 @@ __global__ void __launch_bounds__(kPrThreads, 1) mxf4_pair_kernel(const __grid_c
     }
     mbar_init(done, 1);
     mbar_init(taken, 2 * kPrOutWarps);  // the epilogue warps of both CTAs
-    for (int i = 0; i < kPrOutWarps; ++i) mbar_init(&loaded[i], 1);
+    for (int i = 0; i < 2 * kPrOutWarps; ++i) mbar_init(&loaded[i], 1);
     mbar_init(free_bar, 1u << p.log_split);
     mbar_init(arrived, 1);
     *abort = 0;
@@ -460,11 +487,16 @@ __global__ void __launch_bounds__(kPrThreads, 1) mxf4_pair_kernel(const __grid_c
       const int others = (1 << p.log_split) - 1, width = kPrTile >> p.log_split;
       mbar_arrive_expect_tx(arrived, static_cast<uint32_t>(others * warps * 32 * width * 4));
     }
+  } else if (threadIdx.x == 64) {
     prefetch_tmap(&p.a);
     prefetch_tmap(&p.b);
     prefetch_tmap(&p.a_scale);
     prefetch_tmap(&p.b_scale);
+    if (p.tma) prefetch_tmap(&p.c);
+    if (p.tma && p.g.residual) prefetch_tmap(&p.residual);
   }
+  __syncwarp();
+  cluster_arrive_relaxed();  // (the first warp behind its barriers' initialisation)
   if (warp == 1) {
     tmem_alloc_pair(tmem_slot, 512);
     tmem_relinquish_pair();
@@ -472,10 +504,8 @@ __global__ void __launch_bounds__(kPrThreads, 1) mxf4_pair_kernel(const __grid_c
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  cluster_arrive_relaxed();
   cluster_wait();  // the cluster's barriers exist before any load or arrive reaches them
   const uint32_t tmem = *tmem_slot;
-  pdl_begin(false);
 
   uint8_t* buffers = stages + kPrStages * kPrStageBytes + 1024;
   if (warp == 0) {
