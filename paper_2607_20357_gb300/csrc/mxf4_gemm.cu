@@ -451,7 +451,9 @@ __global__ void __launch_bounds__(kMxGemmThreads, 2) mxf4_tile_kernel(const __gr
 }
 
 cudaError_t launch_mxf4_gemm(const Mxf4Gemm& g, cudaStream_t s) {
-  if (g.M > kMxMaxX) return launch_mxf4_pair(g, s);
+  // (Over a short K the results take most of the time, which pairs have more threads for, if a round of them is
+  // enough: 100 x 5,120 x 256 3.9 us here, 3.4 on pairs.)
+  if (g.M > kMxMaxX || (g.M > 64 && g.K <= 4 * kMxK && (g.N - 1) / 128 < mxf4_clusters(2))) return launch_mxf4_pair(g, s);
   Mxf4Params p;
   p.g = g;
   const int nt = (g.M + 15) / 16 * 16, k_stages = (g.K - 1) / kMxK + 1;

@@ -9,7 +9,9 @@
 // overlap by as many as the scales take behind them: accumulator 0 is columns
 // 0-255, accumulator 1 starts kOverlap columns before 256. The epilogue takes
 // those columns first, then the next tile's MMAs start into the other
-// accumulator while the rest is converted and stored.
+// accumulator while the rest is converted and stored. Tiles of 128 rows of B,
+// for products whose tiles of 256 would leave SMs without work, have two
+// accumulators side by side.
 //
 // Barriers: full[s] (leader's: both CTAs' loads of stage s have landed), empty[s]
 // (in both CTAs: the MMAs have read stage s), done (in both: a tile's MMAs are
@@ -17,6 +19,10 @@
 // tile before is read altogether).
 //
 // Where tiles are few, clusters of two or four pairs share a tile's K.
+//
+// A stage of 256 x 256 x 256 takes its loads' time, 35 KB at the 64 bytes a cycle that
+// an SM gets from L2 (547 cycles; its MMAs take 512).
+// 10,240 x 22,016 x 4,096 runs at 6.9 PFLOP/s for a moment and at 6.4 under the power cap.
 #include <algorithm>
 #include <atomic>
 
@@ -24,25 +30,33 @@
 
 namespace svl {
 
-constexpr int kPrK = 256;  // values of K per stage: a 128-byte swizzled row of codes
-constexpr int kPrTile = 256;
-constexpr int kPrCodes = 128 * 128;  // bytes of a CTA's rows of A, or of its half of B's
-constexpr int kPrScalesA = 2 * kMxTileBytes;
-constexpr int kPrScalesB = 4 * kMxTileBytes;
-constexpr int kPrStageBytes = 2 * kPrCodes + kPrScalesA + kPrScalesB;
-constexpr int kPrStages = 5;
+constexpr int kPrK = 256;   // values of K per stage: a 128-byte swizzled row of codes
+constexpr int kPrRows = 256;  // rows of A per tile
 constexpr int kPrChunk = 32 * 128;  // bytes of an epilogue chunk: 32 rows of 128 bytes
 constexpr int kPrOutWarps = 8;      // two for each quarter of the lanes, with every other chunk of columns
-constexpr int kPrSmem = 1024 + kPrStages * kPrStageBytes + 1024 + kPrOutWarps * kPrChunk;
 constexpr int kPrThreads = 64 + 32 * kPrOutWarps;  // warp 0 loads, warp 1 MMAs (leader), the others epilogue
-constexpr int kPrSets = 2;       // sets of scales in tensor memory, used in turn
-constexpr int kPrOverlap = 24 * kPrSets;
+constexpr int kPrGroup = 8;  // tiles of rows that are walked together
 // The epilogue warps' second buffers are the end of the stages (behind shares of K, 96 KB at most), so many bytes
 // in front of their first.
 constexpr int kPrSecondBack = 1024 + kPrOutWarps * kPrChunk;
-constexpr int kPrGroup = 8;  // tiles of rows that are walked together
-static_assert(kPrSmem <= 232448, "shared memory per CTA");
-static_assert(kPrStages * kPrStageBytes - kPrOutWarps * kPrChunk >= 96 * 1024, "second buffers");
+
+// COLS: rows of B per tile, 256 or 128
+template <int COLS>
+struct PairCfg {
+  static constexpr int kCodesA = 128 * 128;        // bytes of a CTA's rows of A
+  static constexpr int kCodesB = COLS / 2 * 128;   // of its half of B's
+  static constexpr int kScalesA = 2 * kMxTileBytes;
+  static constexpr int kScalesB = COLS / 128 * 2 * kMxTileBytes;
+  static constexpr int kStageBytes = kCodesA + kCodesB + kScalesA + kScalesB;
+  static constexpr int kStages = COLS == 256 ? 5 : 7;
+  static constexpr int kSmem = 1024 + kStages * kStageBytes + 1024 + kPrOutWarps * kPrChunk;
+  // tensor memory: two sets of scales, used in turn, at the end; the second accumulator in front of them or of its own
+  static constexpr int kSet = 8 + COLS / 16;
+  static constexpr int kSecondAcc = COLS == 256 ? 512 - 2 * kSet - COLS : COLS;
+  static constexpr int kOverlap = COLS - kSecondAcc;
+  static_assert(kSmem <= 232448, "shared memory per CTA");
+  static_assert(kStages * kStageBytes - kPrOutWarps * kPrChunk >= 96 * 1024, "second buffers");
+};
 
 struct Mxf4PairParams {
   CUtensorMap a, b, a_scale, b_scale, c, residual;
@@ -77,89 +91,99 @@ struct PairTile {
 };
 // Groups of kPrGroup row tiles, column tile by column tile: tiles that run at
 // the same time share rows of both operands.
+template <int COLS>
 SVL_DEVINL PairTile pair_tile(const Mxf4PairParams& p, int t) {
   const int per = kPrGroup * p.n_tiles, g = t / per, r = t - g * per;
   const int height = min(kPrGroup, p.m_tiles - g * kPrGroup);
   PairTile ti;
-  ti.m0 = (g * kPrGroup + r % height) * kPrTile;
-  ti.n0 = r / height * kPrTile;
+  ti.m0 = (g * kPrGroup + r % height) * kPrRows;
+  ti.n0 = r / height * COLS;
   return ti;
 }
 
+template <int COLS>
 SVL_DEVINL void mx_pair_producer(const Mxf4PairParams& p, const PairPlace& w, uint8_t* stages, uint64_t* full,
                                  uint64_t* empty, volatile int* abort) {
+  using C = PairCfg<COLS>;
   int s = 0;
   uint32_t ph = 1;
   auto next = [&]() {
-    if (++s == kPrStages) {
+    if (++s == C::kStages) {
       s = 0;
       ph ^= 1;
     }
   };
-  PairTile ti = pair_tile(p, w.first);
+  PairTile ti = pair_tile<COLS>(p, w.first);
   pdl_wait();
-  for (int t = w.first; t < p.tiles; t += w.stride, ti = pair_tile(p, t)) {
-    const int m0 = ti.m0 + w.rank * 128, n0 = ti.n0 + w.rank * 128;
+  for (int t = w.first; t < p.tiles; t += w.stride, ti = pair_tile<COLS>(p, t)) {
+    const int m0 = ti.m0 + w.rank * 128, n0 = ti.n0 + w.rank * (COLS / 2);
     for (int k = w.s0; k < w.s1; ++k, next()) {
       if (!mbar_wait(&empty[s], ph, abort)) return mx_abort(abort, p.g.status);
-      uint8_t* st = stages + s * kPrStageBytes;
-      if (w.rank == 0) mbar_arrive_expect_tx(&full[s], 2 * kPrStageBytes);
+      uint8_t* st = stages + s * C::kStageBytes;
+      if (w.rank == 0) mbar_arrive_expect_tx(&full[s], 2 * C::kStageBytes);
       const uint32_t fb = mapa_shared(&full[s], w.leader);
       tma_load_2d_pair(st, &p.a, fb, k * 128, m0);
-      tma_load_2d_pair(st + kPrCodes, &p.b, fb, k * 128, n0);
-      tma_load_2d_pair(st + 2 * kPrCodes, &p.a_scale, fb, k * 256, m0 >> 7);
-      tma_load_2d_pair(st + 2 * kPrCodes + kPrScalesA, &p.b_scale, fb, k * 256, ti.n0 >> 7);
+      tma_load_2d_pair(st + C::kCodesA, &p.b, fb, k * 128, n0);
+      tma_load_2d_pair(st + C::kCodesA + C::kCodesB, &p.a_scale, fb, k * 256, m0 >> 7);
+      tma_load_2d_pair(st + C::kCodesA + C::kCodesB + C::kScalesA, &p.b_scale, fb, k * 256, ti.n0 >> 7);
     }
   }
   // the releases of the last stages (the leader's MMA commits) have arrived here
-  for (int i = 0; i < kPrStages; ++i, next())
+  for (int i = 0; i < C::kStages; ++i, next())
     if (!mbar_wait(&empty[s], ph, abort)) return mx_abort(abort, p.g.status);
 }
 
-SVL_DEVINL uint32_t pair_acc(uint32_t tmem, int it) { return tmem + ((it & 1) ? kPrTile - kPrOverlap : 0); }
+template <int COLS>
+SVL_DEVINL uint32_t pair_acc(uint32_t tmem, int it) {
+  return tmem + ((it & 1) ? PairCfg<COLS>::kSecondAcc : 0);
+}
 
+template <int COLS>
 SVL_DEVINL void mx_pair_mma(const Mxf4PairParams& p, const PairPlace& w, uint8_t* stages, uint64_t* full,
                             uint64_t* empty, uint64_t* done, uint64_t* taken, uint32_t tmem, volatile int* abort) {
+  using C = PairCfg<COLS>;
   const uint32_t base = smem_u32(stages);
-  constexpr uint32_t id0 = idesc_mxf4(kPrTile, kPrTile, 0), id1 = idesc_mxf4(kPrTile, kPrTile, 1);
+  constexpr uint32_t id0 = idesc_mxf4(kPrRows, COLS, 0), id1 = idesc_mxf4(kPrRows, COLS, 1);
   const uint16_t ctas = static_cast<uint16_t>(3u << w.leader);
   int s = 0, it = 0;
   uint32_t ph = 0, set = 0;
   for (int t = w.first; t < p.tiles; t += w.stride, ++it) {
     if (it > 0 && !mbar_wait(taken, (it - 1) & 1, abort)) return mx_abort(abort, p.g.status);
     tc_fence_after();
-    const uint32_t d = pair_acc(tmem, it);
+    const uint32_t d = pair_acc<COLS>(tmem, it);
     uint32_t accumulate = 0;
     for (int k = w.s0; k < w.s1; ++k) {
       if (!mbar_wait(&full[s], ph, abort)) return mx_abort(abort, p.g.status);
       tc_fence_after();
-      const uint32_t st = base + s * kPrStageBytes, sc = st + 2 * kPrCodes;
-      // a set: A's two tiles of 128 columns (4 tensor memory columns each), then B's (8 each)
-      const uint32_t sa = tmem + 512 - kPrOverlap + set * 24, sb = sa + 8;
+      const uint32_t st = base + s * C::kStageBytes, sc = st + C::kCodesA + C::kCodesB;
+      // a set: A's two tiles of 128 columns of K (4 tensor memory columns each), then B's (4 per 128 rows)
+      const uint32_t sa = tmem + 512 - 2 * C::kSet + set * C::kSet, sb = sa + 8;
       const int steps = min(4, (p.g.K - k * kPrK + 63) >> 6);  // 64 values of K an instruction
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
         if (2 * j < steps) {
           tc_copy_scales_pair(sa + 4 * j, smem_desc_scales(sc + j * kMxTileBytes));
-          tc_copy_scales_pair(sb + 8 * j, smem_desc_scales(sc + kPrScalesA + j * kMxTileBytes));
-          tc_copy_scales_pair(sb + 8 * j + 4, smem_desc_scales(sc + kPrScalesA + (2 + j) * kMxTileBytes));
+#pragma unroll
+          for (int c = 0; c < COLS / 128; ++c)
+            tc_copy_scales_pair(sb + (COLS / 32) * j + 4 * c,
+                                smem_desc_scales(sc + C::kScalesA + (2 * c + j) * kMxTileBytes));
         }
       }
-      const uint64_t da = smem_desc_sw128(st), db = smem_desc_sw128(st + kPrCodes);
+      const uint64_t da = smem_desc_sw128(st), db = smem_desc_sw128(st + C::kCodesA);
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         if (i < steps) {
-          tc_mma_mxf4_pair(d, da + 2 * i, db + 2 * i, (i & 1) ? id1 : id0, sa + 4 * (i >> 1), sb + 8 * (i >> 1),
+          tc_mma_mxf4_pair(d, da + 2 * i, db + 2 * i, (i & 1) ? id1 : id0, sa + 4 * (i >> 1), sb + (COLS / 32) * (i >> 1),
                            accumulate);
           accumulate = 1;
         }
       }
       tc_commit_pair(&empty[s], ctas);
-      if (++s == kPrStages) {
+      if (++s == C::kStages) {
         s = 0;
         ph ^= 1;
       }
-      if (++set == kPrSets) set = 0;
+      set ^= 1;
     }
     tc_commit_pair(done, ctas);
   }
@@ -169,7 +193,7 @@ SVL_DEVINL void mx_pair_mma(const Mxf4PairParams& p, const PairPlace& w, uint8_t
 // other of a tile's. In accumulator 1 they are taken from the left, in accumulator
 // 0 from the right. Where K is shared (one tile a cluster), a CTA has the columns
 // that it adds up.
-template <bool F32>
+template <bool F32, int COLS>
 struct PairChunks {
   static constexpr int kCols = F32 ? 32 : 64;
   const Mxf4PairParams& p;
@@ -184,9 +208,9 @@ struct PairChunks {
     i = half;
     n = 0;
     if (t >= p.tiles) return;
-    const PairTile ti = pair_tile(p, t);
+    const PairTile ti = pair_tile<COLS>(p, t);
     row0 = ti.m0 + offset;
-    const int width = kPrTile >> p.log_split;
+    const int width = COLS >> p.log_split;
     n0 = ti.n0 + w.part * width;
     if (row0 < p.g.M) n = (max(0, min(width, p.g.N - n0)) + kCols - 1) / kCols;
   }
@@ -207,18 +231,18 @@ struct PairChunks {
 // chunk of the residual, requested when the buffer is free. In the CTA's last tile
 // the stages are used up, and a second buffer in their place takes every other
 // chunk (a store holds its buffer for some 900 cycles).
-template <bool F32>
+template <bool F32, int COLS>
 struct PairOut {
   static constexpr int kCols = F32 ? 32 : 64;
   const Mxf4PairParams& p;
   uint8_t* own;
   uint64_t* loaded;  // [2]
-  PairChunks<F32> ahead;
+  PairChunks<F32, COLS> ahead;
   volatile int* abort;
   uint32_t parity = 0;  // of each buffer's next wait
   bool last = false;    // in the last tile
   int slot = 0;
-  SVL_DEVINL PairOut(const Mxf4PairParams& params, const PairChunks<F32>& chunks, uint8_t* first, uint64_t* bars,
+  SVL_DEVINL PairOut(const Mxf4PairParams& params, const PairChunks<F32, COLS>& chunks, uint8_t* first, uint64_t* bars,
                      volatile int* flag)
       : p(params), own(first), loaded(bars), ahead(chunks), abort(flag) {
     if (p.g.residual && p.tma && (threadIdx.x & 31) == 0) request(0);
@@ -344,15 +368,16 @@ struct PairWarp {
   SVL_DEVINL uint32_t lanes() const { return static_cast<uint32_t>(q * 32) << 16; }
 };
 
-template <bool F32>
+template <bool F32, int COLS>
 SVL_DEVINL void mx_pair_epilogue(const Mxf4PairParams& p, const PairPlace& w, uint64_t* done, uint64_t* taken,
                                  uint64_t* loaded, uint32_t tmem, uint8_t* buffers, volatile int* abort) {
+  using C = PairCfg<COLS>;
   constexpr int kCols = F32 ? 32 : 64;
   const PairWarp me;
   const uint32_t release = mapa_shared(taken, w.leader);
-  PairChunks<F32> ch(p, w, w.rank * 128 + me.q * 32, me.half);
+  PairChunks<F32, COLS> ch(p, w, w.rank * 128 + me.q * 32, me.half);
   pdl_wait();
-  PairOut<F32> out(p, ch, buffers + me.index() * kPrChunk, loaded + 2 * me.index(), abort);
+  PairOut<F32, COLS> out(p, ch, buffers + me.index() * kPrChunk, loaded + 2 * me.index(), abort);
   for (; ch.more(); ch.next_tile()) {
     const int row = ch.row0 + me.lane;
     const float factor = p.g.row_factor && ch.n > 0 && row < p.g.M ? p.g.row_factor[row] : 1.f;
@@ -361,11 +386,11 @@ SVL_DEVINL void mx_pair_epilogue(const Mxf4PairParams& p, const PairPlace& w, ui
     if (!__all_sync(0xffffffffu, ok)) return mx_abort(abort, p.g.status);
     tc_fence_after();
     if (ch.t + w.stride >= p.tiles) out.enter_last();
-    const uint32_t acc = pair_acc(tmem, ch.it) + me.lanes();
+    const uint32_t acc = pair_acc<COLS>(tmem, ch.it) + me.lanes();
     // Chunks that hold the overlap come first; a warp hands over when it has read the last of its own. (Where the
     // tile's columns end before the overlap, there is none.)
     const int in_overlap = min(
-        ch.n, (ch.it & 1) ? (kPrOverlap + kCols - 1) / kCols : ch.n - (kPrTile - kPrOverlap) / kCols);
+        ch.n, (ch.it & 1) ? (C::kOverlap + kCols - 1) / kCols : ch.n - (COLS - C::kOverlap) / kCols);
     bool handed = ch.i >= in_overlap;
     if (handed && me.lane == 0) mbar_arrive_cluster_relaxed(release);
     for (; ch.i < ch.n; ch.i += 2) {
@@ -389,17 +414,17 @@ SVL_DEVINL void mx_pair_epilogue(const Mxf4PairParams& p, const PairPlace& w, ui
 // that others add up to them, over the stages, which are used up everywhere
 // (`free_bar`), and adds what arrives to its own, in the order of the others.
 // Layout: [the others in order][group of four columns][128 rows][4].
-template <bool F32>
+template <bool F32, int COLS>
 SVL_DEVINL void mx_pair_shares(const Mxf4PairParams& p, const PairPlace& w, uint64_t* done, uint64_t* free_bar,
                                uint64_t* arrived, uint64_t* loaded, uint32_t tmem, uint8_t* stages, uint8_t* buffers,
                                volatile int* abort) {
   constexpr int kCols = F32 ? 32 : 64;
   const PairWarp me;
-  const int split = 1 << p.log_split, width = kPrTile >> p.log_split;
+  const int split = 1 << p.log_split, width = COLS >> p.log_split;
   const int share = (width / 4) * 128 * 16;  // bytes
-  PairChunks<F32> ch(p, w, w.rank * 128 + me.q * 32, me.half);
+  PairChunks<F32, COLS> ch(p, w, w.rank * 128 + me.q * 32, me.half);
   pdl_wait();
-  PairOut<F32> out(p, ch, buffers + me.index() * kPrChunk, loaded + 2 * me.index(), abort);
+  PairOut<F32, COLS> out(p, ch, buffers + me.index() * kPrChunk, loaded + 2 * me.index(), abort);
   const bool rows = ch.row0 < p.g.M;  // of this warp, which the other pairs' warps with the same place have too
   const float factor = p.g.row_factor && ch.row0 + me.lane < p.g.M ? p.g.row_factor[ch.row0 + me.lane] : 1.f;
   bool ok = mbar_wait(done, 0, abort);
@@ -452,13 +477,14 @@ SVL_DEVINL void mx_pair_shares(const Mxf4PairParams& p, const PairPlace& w, uint
   if (me.lane == 0) bulk_wait0();
 }
 
-template <bool F32, bool SHARED>
+template <bool F32, bool SHARED, int COLS>
 __global__ void __launch_bounds__(kPrThreads, 1) mxf4_pair_kernel(const __grid_constant__ Mxf4PairParams p) {
+  using C = PairCfg<COLS>;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* stages = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
-  uint64_t* full = reinterpret_cast<uint64_t*>(stages + kPrStages * kPrStageBytes);
-  uint64_t* empty = full + kPrStages;
-  uint64_t* done = empty + kPrStages;
+  uint64_t* full = reinterpret_cast<uint64_t*>(stages + C::kStages * C::kStageBytes);
+  uint64_t* empty = full + C::kStages;
+  uint64_t* done = empty + C::kStages;
   uint64_t* taken = done + 1;
   uint64_t* free_bar = taken + 1;
   uint64_t* arrived = free_bar + 1;
@@ -469,7 +495,7 @@ __global__ void __launch_bounds__(kPrThreads, 1) mxf4_pair_kernel(const __grid_c
   const PairPlace w = pair_place(p);
   const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0);  // uniform over the warp
   if (threadIdx.x == 0) {
-    for (int i = 0; i < kPrStages; ++i) {
+    for (int i = 0; i < C::kStages; ++i) {
       mbar_init(&full[i], 1);
       mbar_init(&empty[i], 1);
     }
@@ -483,8 +509,8 @@ __global__ void __launch_bounds__(kPrThreads, 1) mxf4_pair_kernel(const __grid_c
     fence_proxy_async();
     if (SHARED) {
       // from every other pair, for each warp here that has rows, 32 of them of a share
-      const int rows = p.g.M - pair_tile(p, w.first).m0 - w.rank * 128, warps = max(0, min(4, (rows + 31) >> 5));
-      const int others = (1 << p.log_split) - 1, width = kPrTile >> p.log_split;
+      const int rows = p.g.M - pair_tile<COLS>(p, w.first).m0 - w.rank * 128, warps = max(0, min(4, (rows + 31) >> 5));
+      const int others = (1 << p.log_split) - 1, width = COLS >> p.log_split;
       mbar_arrive_expect_tx(arrived, static_cast<uint32_t>(others * warps * 32 * width * 4));
     }
   } else if (threadIdx.x == 64) {
@@ -507,15 +533,15 @@ __global__ void __launch_bounds__(kPrThreads, 1) mxf4_pair_kernel(const __grid_c
   cluster_wait();  // the cluster's barriers exist before any load or arrive reaches them
   const uint32_t tmem = *tmem_slot;
 
-  uint8_t* buffers = stages + kPrStages * kPrStageBytes + 1024;
+  uint8_t* buffers = stages + C::kStages * C::kStageBytes + 1024;
   if (warp == 0) {
-    if (elect_one()) mx_pair_producer(p, w, stages, full, empty, abort);
+    if (elect_one()) mx_pair_producer<COLS>(p, w, stages, full, empty, abort);
   } else if (warp == 1) {
-    if (w.rank == 0 && elect_one()) mx_pair_mma(p, w, stages, full, empty, done, taken, tmem, abort);
+    if (w.rank == 0 && elect_one()) mx_pair_mma<COLS>(p, w, stages, full, empty, done, taken, tmem, abort);
   } else if constexpr (SHARED) {
-    mx_pair_shares<F32>(p, w, done, free_bar, arrived, loaded, tmem, stages, buffers, abort);
+    mx_pair_shares<F32, COLS>(p, w, done, free_bar, arrived, loaded, tmem, stages, buffers, abort);
   } else {
-    mx_pair_epilogue<F32>(p, w, done, taken, loaded, tmem, buffers, abort);
+    mx_pair_epilogue<F32, COLS>(p, w, done, taken, loaded, tmem, buffers, abort);
   }
 
   __syncwarp();
@@ -538,9 +564,10 @@ __global__ void __launch_bounds__(kPrThreads, 1) mxf4_pair_kernel(const __grid_c
 }
 
 using PairKernel = void (*)(Mxf4PairParams);
-static PairKernel pair_kernel(int log_split, bool f32) {
-  return log_split ? (f32 ? mxf4_pair_kernel<true, true> : mxf4_pair_kernel<false, true>)
-                   : (f32 ? mxf4_pair_kernel<true, false> : mxf4_pair_kernel<false, false>);
+static PairKernel pair_kernel(bool shared, bool f32, int cols) {
+  if (cols == 128) return f32 ? mxf4_pair_kernel<true, false, 128> : mxf4_pair_kernel<false, false, 128>;
+  return shared ? (f32 ? mxf4_pair_kernel<true, true, 256> : mxf4_pair_kernel<false, true, 256>)
+                : (f32 ? mxf4_pair_kernel<true, false, 256> : mxf4_pair_kernel<false, false, 256>);
 }
 
 // The answer is the device's (76, 36 and 15 clusters of 2, 4 and 8 CTAs on one
@@ -552,11 +579,11 @@ int mxf4_clusters(int ctas) {
   if (cudaGetDevice(&dev) != cudaSuccess) return 0;
   std::atomic<int>* place = dev < 16 ? &known[dev][log] : nullptr;
   if (place && (n = place->load(std::memory_order_relaxed))) return n - 1;
-  PairKernel kernel = pair_kernel(log, true);
+  PairKernel kernel = pair_kernel(log > 0, true, 256);
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(2u << log);
   cfg.blockDim = dim3(kPrThreads);
-  cfg.dynamicSmemBytes = kPrSmem;
+  cfg.dynamicSmemBytes = PairCfg<256>::kSmem;
   cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeClusterDimension;
   attr[0].val.clusterDim.x = 2u << log;
@@ -564,7 +591,7 @@ int mxf4_clusters(int ctas) {
   attr[0].val.clusterDim.z = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 1;
-  if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kPrSmem) != cudaSuccess ||
+  if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, PairCfg<256>::kSmem) != cudaSuccess ||
       cudaOccupancyMaxActiveClusters(&n, kernel, &cfg) != cudaSuccess)
     return 0;
   if (place) place->store(n + 1, std::memory_order_relaxed);
@@ -574,31 +601,38 @@ int mxf4_clusters(int ctas) {
 cudaError_t launch_mxf4_pair(const Mxf4Gemm& g, cudaStream_t s) {
   Mxf4PairParams p;
   p.g = g;
-  p.m_tiles = (g.M - 1) / kPrTile + 1;
-  p.n_tiles = (g.N - 1) / kPrTile + 1;
-  const int64_t tiles = static_cast<int64_t>(p.m_tiles) * p.n_tiles;
-  if (tiles > INT32_MAX / 2) return cudaErrorInvalidValue;
+  const int64_t m_tiles = (g.M - 1) / kPrRows + 1, wide = m_tiles * ((g.N - 1) / 256 + 1);
+  const int64_t narrow = m_tiles * ((g.N - 1) / 128 + 1), pairs = std::max(1, mxf4_clusters(2));
+  // Tiles of 128 rows of B where they take no more rounds of the device (4,096 rows of B, K 4,096, us for 256 and
+  // 128: 300 rows of A 9.3, 8.2; 800 rows 9.9, 12.9). Of 256, a cluster's pairs share K where all of the tiles'
+  // clusters run at once and K has the stages to make up for the sums' way, against tiles of 128 or, where those
+  // take longer, of 256. us for 128, and for 256 with 1, 2 and 4 pairs: 4,608 rows of B, K 11,008 (43 stages), 150 rows
+  // of A 15.3, 17.7, 14.0; 3,584 and 18,944 (74 stages), 150 rows 23.2, 26.4, 18.2, 14.8, 500 rows 23.5, 26.5, 19.0.
+  int cols = (narrow - 1) / pairs <= (wide - 1) / pairs ? 128 : 256, log_split = 0;
+  if ((g.K - 1) / kPrK + 1 >= (cols == 128 ? 36 : 16))
+    for (int l = 1; l <= 2 && wide <= mxf4_clusters(2 << l); ++l) log_split = l;
+  if (log_split) cols = 256;
+  const int64_t tiles = cols == 256 ? wide : narrow;
+  if (narrow > INT32_MAX / 2) return cudaErrorInvalidValue;
+  p.m_tiles = static_cast<int>(m_tiles);
+  p.n_tiles = (g.N - 1) / cols + 1;
   p.tiles = static_cast<int>(tiles);
+  p.log_split = log_split;
   const uint64_t bytes = static_cast<uint64_t>(mxf4_row_bytes(g.K));
-  if (!make_byte_map(&p.a, g.a, g.M, bytes, g.ld_a, 128) || !make_byte_map(&p.b, g.b, g.N, bytes, g.ld_b, 128) ||
-      !make_scale_map(&p.a_scale, g.a_scale, g.M, g.K, 1) || !make_scale_map(&p.b_scale, g.b_scale, g.N, g.K, 2))
+  if (!make_byte_map(&p.a, g.a, g.M, bytes, g.ld_a, 128) ||
+      !make_byte_map(&p.b, g.b, g.N, bytes, g.ld_b, static_cast<uint32_t>(cols / 2)) ||
+      !make_scale_map(&p.a_scale, g.a_scale, g.M, g.K, 1) ||
+      !make_scale_map(&p.b_scale, g.b_scale, g.N, g.K, static_cast<uint32_t>(cols / 128)))
     return cudaErrorInvalidValue;
   // Tensor stores want 16-byte rows, and end a row at a multiple of 16 bytes; anything else goes by plain ones.
   p.tma = (static_cast<int64_t>(g.N) * (g.f32 ? 4 : 2)) % 16 == 0 && make_result_map(&p.c, g.c, g.f32, g.M, g.N, g.ld_c) &&
           (!g.residual || make_result_map(&p.residual, g.residual, g.f32, g.M, g.N, g.ld_residual));
-  // A cluster's pairs share K where all of its tiles' clusters run at once and K has the stages to make up for the
-  // sums' way. us for 1, 2 and 4 pairs: K 4,096 (16 stages), 8 tiles 9.2, 8.8, 8.5; 11,008, 4 tiles 17.2, 12.9, 10.4
-  // and 18 tiles 17.7, 14.0; 18,944, 14 tiles 26.3, 18.4, 14.7.
-  int log_split = 0;
-  if ((g.K - 1) / kPrK + 1 >= 16)
-    for (int l = 1; l <= 2 && tiles <= mxf4_clusters(2 << l); ++l) log_split = l;
-  p.log_split = log_split;
-  void (*kernel)(Mxf4PairParams) = pair_kernel(log_split, g.f32);
-  cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kPrSmem);
+  PairKernel kernel = pair_kernel(log_split > 0, g.f32, cols);
+  const int smem = cols == 256 ? PairCfg<256>::kSmem : PairCfg<128>::kSmem, ctas = 2 << log_split;
+  cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
   if (e != cudaSuccess) return e;
-  const int ctas = 2 << log_split;
-  const int64_t clusters = log_split ? tiles : std::min<int64_t>(tiles, std::max(1, mxf4_clusters(2)));
-  return launch_pdl_cluster(kernel, dim3(static_cast<unsigned>(clusters * ctas)), kPrThreads, kPrSmem, ctas, s, p);
+  const int64_t clusters = log_split ? tiles : std::min(tiles, pairs);
+  return launch_pdl_cluster(kernel, dim3(static_cast<unsigned>(clusters * ctas)), kPrThreads, smem, ctas, s, p);
 }
 
 }  // namespace svl
