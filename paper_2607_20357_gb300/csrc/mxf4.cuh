@@ -15,6 +15,8 @@
 //           [ceil(rows / 128)][ceil(cols / 128)].
 #pragma once
 
+#include <atomic>
+
 #include "common.cuh"
 
 namespace svl {
@@ -80,6 +82,19 @@ cudaError_t launch_mxf4_gemm(const Mxf4Gemm& g, cudaStream_t s);
 cudaError_t launch_mxf4_pair(const Mxf4Gemm& g, cudaStream_t s);
 // How many clusters of 2, 4 or 8 CTAs the device runs at once, an SM to a CTA.
 int mxf4_clusters(int ctas);
+
+// Lets `kernel` have `bytes` of shared memory, the same in every call. Asked of the
+// driver once per device (0.3 us of a call's 3.6); `devices`: the kernel's own.
+inline cudaError_t mxf4_allow_smem(const void* kernel, int bytes, std::atomic<uint64_t>* devices) {
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return e;
+  const uint64_t bit = dev < 64 ? uint64_t(1) << dev : 0;
+  if (devices->load(std::memory_order_relaxed) & bit) return cudaSuccess;
+  e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+  if (e == cudaSuccess) devices->fetch_or(bit, std::memory_order_relaxed);
+  return e;
+}
 
 // 2-D tensor map of `rows` rows of `bytes` bytes, `ld` bytes apart: boxes of
 // 128 bytes x box_rows with 128-byte swizzle; what lies outside reads as zeros.

@@ -494,8 +494,8 @@ cudaError_t launch_mxf4_gemm(const Mxf4Gemm& g, cudaStream_t s) {
     return cudaErrorInvalidValue;
   const int smem = p.bars_at + kMxBars + 1024;
   void (*kernel)(Mxf4Params) = g.f32 ? mxf4_tile_kernel<true> : mxf4_tile_kernel<false>;
-  // (the kernel's limit, not the call's: every call sets the same)
-  cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMxSmem);
+  static std::atomic<uint64_t> devices[2];
+  cudaError_t e = mxf4_allow_smem(reinterpret_cast<const void*>(kernel), kMxSmem, &devices[g.f32]);
   if (e != cudaSuccess) return e;
   return launch_pdl_cluster(kernel, dim3(static_cast<unsigned>(tiles * split)), kMxGemmThreads, smem, split,
                             s, p);

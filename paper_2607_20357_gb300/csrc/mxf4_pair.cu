@@ -629,7 +629,9 @@ cudaError_t launch_mxf4_pair(const Mxf4Gemm& g, cudaStream_t s) {
           (!g.residual || make_result_map(&p.residual, g.residual, g.f32, g.M, g.N, g.ld_residual));
   PairKernel kernel = pair_kernel(log_split > 0, g.f32, cols);
   const int smem = cols == 256 ? PairCfg<256>::kSmem : PairCfg<128>::kSmem, ctas = 2 << log_split;
-  cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+  static std::atomic<uint64_t> devices[3][2];  // of each kernel
+  cudaError_t e = mxf4_allow_smem(reinterpret_cast<const void*>(kernel), smem,
+                                  &devices[cols == 128 ? 2 : log_split > 0][g.f32]);
   if (e != cudaSuccess) return e;
   const int64_t clusters = log_split ? tiles : std::min(tiles, pairs);
   return launch_pdl_cluster(kernel, dim3(static_cast<unsigned>(clusters * ctas)), kPrThreads, smem, ctas, s, p);

@@ -194,9 +194,9 @@ def _p(x):
     """Device (or host) pointer of a tensor / int / None. (Plain ints: ctypes
     converts them by the declared argument type, and building a c_void_p for
     each argument doubled the host time of a small call.)"""
-    if isinstance(x, torch.Tensor):
-        return x.data_ptr()
-    return None if x is None else int(x)
+    if x is None:
+        return None
+    return x.data_ptr() if isinstance(x, torch.Tensor) else int(x)
 
 
 def _stream(stream):
