@@ -16,7 +16,7 @@
 // All of it is bound by memory (2 bytes in, 17/32 out per value; SwiGLU 4 in), if
 // a value costs no more than some ten issue slots: hence sixteen values a
 // thread, whose block and row are found once, and operations on pairs.
-// 18,944 x 3,584: rows 27.2 us (6.3 TB/s), with a gain 32.6 and with 1/rms 35.2,
+// 18,944 x 3,584: rows 27.2 us (6.3 TB/s), with a gain 28.6 and with 1/rms 31.5,
 // SwiGLU 48.2 (6.4 TB/s), reading back 32.7 (5.3 TB/s, four fifths of it writes).
 #include <algorithm>
 
@@ -81,7 +81,7 @@ SVL_DEVINL uint32_t e2m1x8(const uint64_t* v) {
 
 // Sixteen values of a row: half of a block.
 struct Half {
-  uint4 x[2], y[2];  // the values; gains or ups
+  uint4 x[2], y[2];  // the values; ups
 };
 
 template <int SRC>
@@ -92,9 +92,17 @@ SVL_DEVINL void load_half(const Mxf4Rows& a, int64_t row, int u, Half& v) {
     v.x[i] = v.y[i] = make_uint4(0, 0, 0, 0);
     if (row < a.rows && c < a.cols) {
       v.x[i] = *reinterpret_cast<const uint4*>(a.src + row * a.ld_src + c);
-      if (SRC == MX_GAIN) v.y[i] = *reinterpret_cast<const uint4*>(a.other + c);
       if (SRC == MX_SWIGLU) v.y[i] = *reinterpret_cast<const uint4*>(a.other + row * a.ld_other + c);
     }
+  }
+}
+
+// The gains of sixteen columns.
+SVL_DEVINL void load_gains(const Mxf4Rows& a, int u, uint4* gain) {
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const int c = u * 16 + i * 8;
+    gain[i] = c < a.cols ? *reinterpret_cast<const uint4*>(a.other + c) : make_uint4(0, 0, 0, 0);
   }
 }
 
@@ -124,7 +132,7 @@ SVL_DEVINL uint32_t max_u16x2(uint32_t a, uint32_t b) {
 // block. Every lane of the warp takes part.
 template <int SRC, bool RMS>
 SVL_DEVINL void store_half(const Mxf4Rows& a, int64_t row, int u, int n_units, int n_held, uint8_t* codes,
-                           uint8_t* scale, const Half& v, uint64_t* squares) {
+                           uint8_t* scale, const Half& v, const uint4* gain, uint64_t* squares) {
   uint64_t f[8];
   pairs8(v.x[0], f);
   pairs8(v.x[1], f + 4);
@@ -142,8 +150,8 @@ SVL_DEVINL void store_half(const Mxf4Rows& a, int64_t row, int u, int n_units, i
     top = max(m & 0xFFFF0000u, m << 16);
   } else {
     uint64_t y[8];
-    pairs8(v.y[0], y);
-    pairs8(v.y[1], y + 4);
+    pairs8(SRC == MX_GAIN ? gain[0] : v.y[0], y);
+    pairs8(SRC == MX_GAIN ? gain[1] : v.y[1], y + 4);
     float m = 0.f;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
@@ -165,48 +173,83 @@ SVL_DEVINL void store_half(const Mxf4Rows& a, int64_t row, int u, int n_units, i
   if ((u & 1) == 0 && u < n_units) scale[static_cast<int64_t>(u >> 3) * kMxTileBytes + ((u >> 1) & 3)] = static_cast<uint8_t>(b);
 }
 
-// A group of `group` threads (a power of two, 8 to kMxThreads) takes a row,
-// sixteen values a thread and step: eight threads' values are a tile's 128
-// columns, so a block's lanes and a tile's bytes stay together.
-template <int SRC, bool RMS>
+// A group of `group` threads (a power of two, 8 to kMxThreads) takes a row, or
+// AT_ONCE rows that share the loads of their gains, sixteen values a thread and
+// step: eight threads' values are a tile's 128 columns, so a block's lanes and a
+// tile's bytes stay together.
+template <int SRC, bool RMS, int AT_ONCE>
 __global__ void __launch_bounds__(kMxThreads, 4) mxf4_quantize_kernel(Mxf4Rows a, int group) {
-  constexpr int kBatch = SRC == MX_ROWS ? 4 : 2;  // halves a thread loads before it works on the first
-  __shared__ float red[2][kMxThreads / 32];
+  constexpr int kBatch = AT_ONCE > 1 ? 1 : SRC == MX_ROWS ? 4 : 2;  // steps loaded before work on the first
+  __shared__ float red[2][AT_ONCE][kMxThreads / 32];
   pdl_begin(false);
   const int j = threadIdx.x & (group - 1), per_cta = kMxThreads / group;
   const int64_t tiles = mxf4_scale_tiles(a.cols);
   const int n_units = static_cast<int>(tiles) * 8, n_held = (a.cols + kMxBlock - 1) / kMxBlock * 2;
   int n = 0;
-  for (int64_t r0 = static_cast<int64_t>(blockIdx.x) * per_cta; r0 < a.rows;
-       r0 += static_cast<int64_t>(gridDim.x) * per_cta, ++n) {
-    const int64_t row = r0 + threadIdx.x / group;
-    uint8_t* codes = a.codes + row * a.ld_codes;
-    uint8_t* scale = a.scale + (row >> 7) * tiles * kMxTileBytes + (row & 31) * 16 + ((row >> 5) & 3) * 4;
-    uint64_t squares[2] = {0, 0};
+  for (int64_t r0 = static_cast<int64_t>(blockIdx.x) * per_cta * AT_ONCE; r0 < a.rows;
+       r0 += static_cast<int64_t>(gridDim.x) * per_cta * AT_ONCE, ++n) {
+    int64_t row[AT_ONCE];
+    uint8_t *codes[AT_ONCE], *scale[AT_ONCE];
+    uint64_t squares[AT_ONCE][2];
+#pragma unroll
+    for (int q = 0; q < AT_ONCE; ++q) {
+      row[q] = r0 + q * per_cta + threadIdx.x / group;
+      codes[q] = a.codes + row[q] * a.ld_codes;
+      scale[q] = a.scale + (row[q] >> 7) * tiles * kMxTileBytes + (row[q] & 31) * 16 + ((row[q] >> 5) & 3) * 4;
+      squares[q][0] = squares[q][1] = 0;
+    }
     for (int u0 = 0; u0 < n_units; u0 += kBatch * group) {
-      Half v[kBatch];
+      Half v[kBatch][AT_ONCE];
+      uint4 gain[kBatch][2];
 #pragma unroll
-      for (int i = 0; i < kBatch; ++i)
-        if (u0 + i * group < n_units) load_half<SRC>(a, row, u0 + i * group + j, v[i]);
+      for (int i = 0; i < kBatch; ++i) {
+        if (u0 + i * group < n_units) {
+          if (SRC == MX_GAIN) load_gains(a, u0 + i * group + j, gain[i]);
 #pragma unroll
-      for (int i = 0; i < kBatch; ++i)
-        if (u0 + i * group < n_units)
-          store_half<SRC, RMS>(a, row, u0 + i * group + j, n_units, n_held, codes, scale, v[i], squares);
+          for (int q = 0; q < AT_ONCE; ++q) load_half<SRC>(a, row[q], u0 + i * group + j, v[i][q]);
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < kBatch; ++i) {
+        if (u0 + i * group < n_units) {
+#pragma unroll
+          for (int q = 0; q < AT_ONCE; ++q)
+            store_half<SRC, RMS>(a, row[q], u0 + i * group + j, n_units, n_held, codes[q], scale[q], v[i][q], gain[i],
+                                 squares[q]);
+        }
+      }
     }
     if (RMS) {
-      const uint64_t both = add2(squares[0], squares[1]);
-      float sum = __fadd_rn(lo2(both), hi2(both));
-      for (int off = min(group, 32) >> 1; off > 0; off >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, off);
-      if (group > 32) {
-        float* rd = red[n & 1];  // (alternate, so that one barrier a row is enough)
-        if ((threadIdx.x & 31) == 0) rd[threadIdx.x >> 5] = sum;
-        __syncthreads();
-        sum = 0.f;
-        if (j == 0)
-          for (int i = 0; i < group / 32; ++i) sum += rd[(threadIdx.x >> 5) + i];
+      float sum[AT_ONCE];
+#pragma unroll
+      for (int q = 0; q < AT_ONCE; ++q) {
+        const uint64_t both = add2(squares[q][0], squares[q][1]);
+        sum[q] = __fadd_rn(lo2(both), hi2(both));
       }
-      if (j == 0 && row < a.rows)
-        a.inv_rms[row] = __fdiv_rn(1.f, __fsqrt_rn(__fadd_rn(__fdiv_rn(sum, static_cast<float>(a.cols)), a.eps)));
+      for (int off = min(group, 32) >> 1; off > 0; off >>= 1) {
+#pragma unroll
+        for (int q = 0; q < AT_ONCE; ++q) sum[q] += __shfl_xor_sync(0xffffffffu, sum[q], off);
+      }
+      if (group > 32) {
+        // (alternate, so that one barrier a round is enough)
+        if ((threadIdx.x & 31) == 0) {
+#pragma unroll
+          for (int q = 0; q < AT_ONCE; ++q) red[n & 1][q][threadIdx.x >> 5] = sum[q];
+        }
+        __syncthreads();
+      }
+      if (j == 0) {
+#pragma unroll
+        for (int q = 0; q < AT_ONCE; ++q) {
+          if (group > 32) {
+            sum[q] = 0.f;
+            for (int i = 0; i < group / 32; ++i) sum[q] += red[n & 1][q][(threadIdx.x >> 5) + i];
+          }
+          if (row[q] < a.rows)
+            a.inv_rms[row[q]] =
+                __fdiv_rn(1.f, __fsqrt_rn(__fadd_rn(__fdiv_rn(sum[q], static_cast<float>(a.cols)), a.eps)));
+        }
+      }
     }
   }
 }
@@ -291,20 +334,24 @@ static unsigned grid_for(int64_t rows, int group, int num_sms) {
   return static_cast<unsigned>(std::min<int64_t>(ctas, 8 * static_cast<int64_t>(num_sms)));
 }
 
-template <int SRC>
-static cudaError_t launch_quantize(const Mxf4Rows& a, unsigned grid, int group, cudaStream_t s) {
-  return a.inv_rms ? launch_pdl(mxf4_quantize_kernel<SRC, true>, grid, kMxThreads, 0, s, a, group)
-                   : launch_pdl(mxf4_quantize_kernel<SRC, false>, grid, kMxThreads, 0, s, a, group);
+template <int SRC, int AT_ONCE>
+static cudaError_t launch_quantize(const Mxf4Rows& a, int group, cudaStream_t s) {
+  const unsigned grid = grid_for((a.rows + AT_ONCE - 1) / AT_ONCE, group, a.num_sms);
+  return a.inv_rms ? launch_pdl(mxf4_quantize_kernel<SRC, true, AT_ONCE>, grid, kMxThreads, 0, s, a, group)
+                   : launch_pdl(mxf4_quantize_kernel<SRC, false, AT_ONCE>, grid, kMxThreads, 0, s, a, group);
 }
 
 cudaError_t launch_mxf4_quantize(Mxf4Source source, const Mxf4Rows& a, cudaStream_t s) {
   const int group = group_for(a.rows, mxf4_scale_tiles(a.cols) * 8, a.num_sms);
-  const unsigned grid = grid_for(a.rows, group, a.num_sms);
-  switch (source) {
-    case MX_ROWS: return launch_quantize<MX_ROWS>(a, grid, group, s);
-    case MX_GAIN: return launch_quantize<MX_GAIN>(a, grid, group, s);
-    default: return launch_pdl(mxf4_quantize_kernel<MX_SWIGLU, false>, grid, kMxThreads, 0, s, a, group);
-  }
+  if (source == MX_ROWS) return launch_quantize<MX_ROWS, 1>(a, group, s);
+  if (source == MX_SWIGLU)
+    return launch_pdl(mxf4_quantize_kernel<MX_SWIGLU, false, 1>, grid_for(a.rows, group, a.num_sms), kMxThreads, 0, s, a,
+                      group);
+  // Two rows share the loads of their gains, where the SMs (four CTAs each) then pass over no more rows in all:
+  // 18,944 x 3,584 28.6 us instead of 31.7, but 5,403 x 11,008 33.4 instead of 30.5.
+  const int64_t round = static_cast<int64_t>(kMxThreads / group) * 4 * a.num_sms;
+  const int64_t ones = (a.rows + round - 1) / round, twos = (a.rows + 2 * round - 1) / (2 * round);
+  return ones > 1 && 2 * twos <= ones ? launch_quantize<MX_GAIN, 2>(a, group, s) : launch_quantize<MX_GAIN, 1>(a, group, s);
 }
 
 cudaError_t launch_mxf4_dequantize(const Mxf4Read& a, cudaStream_t s) {
