@@ -283,50 +283,58 @@ SVL_DEVINL uint4 bf16x8(uint32_t code, uint32_t s, uint32_t s2, bool far) {
 // Groups of threads take rows as in mxf4_quantize_kernel, eight values a thread
 // and step, so that a warp stores 512 consecutive bytes (16 values a thread, two
 // stores 32 bytes apart each: 42 us for 18,944 x 3,584, 32 with eight).
+template <int STEPS, int AT_ONCE>
 __global__ void __launch_bounds__(kMxThreads) mxf4_dequantize_kernel(Mxf4Read a, int group) {
-  constexpr int kBatch = 4;
   pdl_begin(false);
   const int j = threadIdx.x & (group - 1), per_cta = kMxThreads / group;
   const int64_t tiles = mxf4_scale_tiles(a.cols);
   const int n_units = a.cols / 8;
-  for (int64_t row = static_cast<int64_t>(blockIdx.x) * per_cta + threadIdx.x / group; row < a.rows;
-       row += static_cast<int64_t>(gridDim.x) * per_cta) {
-    const uint8_t* codes = a.codes + row * a.ld_codes;
-    const uint8_t* scale = a.scale + (row >> 7) * tiles * kMxTileBytes + (row & 31) * 16 + ((row >> 5) & 3) * 4;
-    __nv_bfloat16* dst = a.dst + row * a.ld_dst;
-    for (int u0 = j; u0 < n_units; u0 += kBatch * group) {
-      uint32_t code[kBatch];
-      int b[kBatch];
+  for (int64_t r0 = static_cast<int64_t>(blockIdx.x) * per_cta * AT_ONCE + threadIdx.x / group; r0 < a.rows;
+       r0 += static_cast<int64_t>(gridDim.x) * per_cta * AT_ONCE) {
+    for (int u0 = j; u0 < n_units; u0 += STEPS * group) {
+      uint32_t code[AT_ONCE][STEPS];
+      int b[AT_ONCE][STEPS];
 #pragma unroll
-      for (int i = 0; i < kBatch; ++i) {
-        const int u = u0 + i * group;
-        if (u < n_units) {
-          code[i] = *reinterpret_cast<const uint32_t*>(codes + static_cast<int64_t>(u) * 4);
-          b[i] = scale[static_cast<int64_t>(u >> 4) * kMxTileBytes + ((u >> 2) & 3)];
+      for (int q = 0; q < AT_ONCE; ++q) {
+        const int64_t row = r0 + q * per_cta;
+        const uint8_t* codes = a.codes + row * a.ld_codes;
+        const uint8_t* scale = a.scale + (row >> 7) * tiles * kMxTileBytes + (row & 31) * 16 + ((row >> 5) & 3) * 4;
+#pragma unroll
+        for (int i = 0; i < STEPS; ++i) {
+          const int u = u0 + i * group;
+          if (u < n_units && row < a.rows) {
+            code[q][i] = *reinterpret_cast<const uint32_t*>(codes + static_cast<int64_t>(u) * 4);
+            b[q][i] = scale[static_cast<int64_t>(u >> 4) * kMxTileBytes + ((u >> 2) & 3)];
+          }
         }
       }
 #pragma unroll
-      for (int i = 0; i < kBatch; ++i) {
-        const int u = u0 + i * group;
-        if (u >= n_units) break;
-        const bool far = b[i] > 142;
-        const uint32_t e = static_cast<uint32_t>(min(b[i], 142)) + 112;
-        const uint32_t e2 = b[i] == 255 ? 0x7FC0u : static_cast<uint32_t>(max(b[i], 142) - 142 + 127) << 7;
-        *reinterpret_cast<uint4*>(dst + static_cast<int64_t>(u) * 8) =
-            bf16x8(code[i], (e << 7) * 0x10001u, e2 * 0x10001u, far);
+      for (int q = 0; q < AT_ONCE; ++q) {
+        const int64_t row = r0 + q * per_cta;
+#pragma unroll
+        for (int i = 0; i < STEPS; ++i) {
+          const int u = u0 + i * group;
+          if (u >= n_units || row >= a.rows) break;
+          const bool far = b[q][i] > 142;
+          const uint32_t e = static_cast<uint32_t>(min(b[q][i], 142)) + 112;
+          const uint32_t e2 = b[q][i] == 255 ? 0x7FC0u : static_cast<uint32_t>(max(b[q][i], 142) - 142 + 127) << 7;
+          *reinterpret_cast<uint4*>(a.dst + row * a.ld_dst + static_cast<int64_t>(u) * 8) =
+              bf16x8(code[q][i], (e << 7) * 0x10001u, e2 * 0x10001u, far);
+        }
       }
     }
   }
 }
 
 // Threads per row: a warp, less for narrow rows (no lanes without values), more
-// while the rows' groups would not fill the SMs twice (5,403 x 11,008 quantised
-// in 25.5 us, 29.9 with half as many, 25.2 and with 1/rms 46 instead of 36 with
-// four times as many).
-static int group_for(int64_t rows, int64_t units, int num_sms) {
+// while the rows' groups have not `threads` in all, twice what the SMs hold when
+// quantising, four times when reading back (5,403 x 11,008 quantised in 25.5 us, 29.9
+// with half as many, 25.2 and with 1/rms 46 instead of 36 with four times as many;
+// read back in 28.9, 31.4 with half, 29.5 with twice as many).
+static int group_for(int64_t rows, int64_t units, int threads) {
   int group = 8;
   while (group < 32 && group < units) group *= 2;
-  while (group < kMxThreads && group < units && rows * group < 2048 * static_cast<int64_t>(num_sms)) group *= 2;
+  while (group < kMxThreads && group < units && rows * group < threads) group *= 2;
   return group;
 }
 static unsigned grid_for(int64_t rows, int group, int num_sms) {
@@ -342,21 +350,33 @@ static cudaError_t launch_quantize(const Mxf4Rows& a, int group, cudaStream_t s)
 }
 
 cudaError_t launch_mxf4_quantize(Mxf4Source source, const Mxf4Rows& a, cudaStream_t s) {
-  const int group = group_for(a.rows, mxf4_scale_tiles(a.cols) * 8, a.num_sms);
-  if (source == MX_ROWS) return launch_quantize<MX_ROWS, 1>(a, group, s);
-  if (source == MX_SWIGLU)
-    return launch_pdl(mxf4_quantize_kernel<MX_SWIGLU, false, 1>, grid_for(a.rows, group, a.num_sms), kMxThreads, 0, s, a,
-                      group);
-  // Two rows share the loads of their gains, where the SMs (four CTAs each) then pass over no more rows in all:
-  // 18,944 x 3,584 28.6 us instead of 31.7, but 5,403 x 11,008 33.4 instead of 30.5.
+  const int64_t units = mxf4_scale_tiles(a.cols) * 8;
+  const int group = group_for(a.rows, units, 2048 * a.num_sms);
+  // Two rows at a time where a row is a single step, so that each thread has more than one on its way, and where rows
+  // share the loads of their gains. Not where the SMs (four CTAs each) would then pass over more rows in all: 60,000 x
+  // 256 7.9 us instead of 10.1, 18,944 x 3,584 with gains 28.6 instead of 31.7, but 5,403 x 11,008 33.4 instead of 30.5.
   const int64_t round = static_cast<int64_t>(kMxThreads / group) * 4 * a.num_sms;
   const int64_t ones = (a.rows + round - 1) / round, twos = (a.rows + 2 * round - 1) / (2 * round);
-  return ones > 1 && 2 * twos <= ones ? launch_quantize<MX_GAIN, 2>(a, group, s) : launch_quantize<MX_GAIN, 1>(a, group, s);
+  const bool step = units <= group && ones > 2, fits = ones > 1 && 2 * twos <= ones;
+  switch (source) {
+    case MX_ROWS: return step ? launch_quantize<MX_ROWS, 2>(a, group, s) : launch_quantize<MX_ROWS, 1>(a, group, s);
+    case MX_GAIN:
+      return step || fits ? launch_quantize<MX_GAIN, 2>(a, group, s) : launch_quantize<MX_GAIN, 1>(a, group, s);
+    default:
+      return step ? launch_pdl(mxf4_quantize_kernel<MX_SWIGLU, false, 2>, grid_for((a.rows + 1) / 2, group, a.num_sms),
+                               kMxThreads, 0, s, a, group)
+                  : launch_pdl(mxf4_quantize_kernel<MX_SWIGLU, false, 1>, grid_for(a.rows, group, a.num_sms), kMxThreads,
+                               0, s, a, group);
+  }
 }
 
 cudaError_t launch_mxf4_dequantize(const Mxf4Read& a, cudaStream_t s) {
-  const int group = group_for(a.rows, a.cols / 8, a.num_sms);
-  return launch_pdl(mxf4_dequantize_kernel, grid_for(a.rows, group, a.num_sms), kMxThreads, 0, s, a, group);
+  const int group = group_for(a.rows, a.cols / 8, 4096 * a.num_sms);
+  // four steps of a row, or four rows of one step (60,000 x 256 8.1 us instead of 10.1)
+  if (a.cols / 8 <= group && a.rows > static_cast<int64_t>(kMxThreads / group) * 8 * a.num_sms)
+    return launch_pdl(mxf4_dequantize_kernel<1, 4>, grid_for((a.rows + 3) / 4, group, a.num_sms), kMxThreads, 0, s, a,
+                      group);
+  return launch_pdl(mxf4_dequantize_kernel<4, 1>, grid_for(a.rows, group, a.num_sms), kMxThreads, 0, s, a, group);
 }
 
 }  // namespace svl

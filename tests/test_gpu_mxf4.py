@@ -17,7 +17,8 @@ BF16, U8 = torch.bfloat16, torch.uint8
 # (rows, cols, elements between source rows, bytes between code rows)
 SHAPES = [(1, 8, 8, 16), (1, 32, 32, 16), (3, 40, 48, 48), (1, 4096, 4096, 2048), (2, 1000, 1000, 512),
           (31, 128, 128, 64), (33, 136, 144, 96), (129, 264, 520, 160), (130, 4096, 4096, 2048), (257, 72, 72, 48),
-          (5, 18944, 18944, 9472), (700, 1024, 1032, 528), (2049, 64, 64, 32)]
+          (5, 18944, 18944, 9472), (700, 1024, 1032, 528), (2049, 64, 64, 32),
+          (25001, 256, 256, 128), (70001, 40, 40, 32), (19500, 264, 264, 144)]
 
 
 def rows_of(seed, rows, cols, spread=1.0):
