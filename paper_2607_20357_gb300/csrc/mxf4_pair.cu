@@ -20,9 +20,11 @@
 //
 // Where tiles are few, clusters of two or four pairs share a tile's K.
 //
-// A stage of 256 x 256 x 256 takes its loads' time, 35 KB at the 64 bytes a cycle that
-// an SM gets from L2 (547 cycles; its MMAs take 512).
-// 10,240 x 22,016 x 4,096 runs at 6.9 PFLOP/s for a moment and at 6.4 under the power cap.
+// What bounds it is shared memory, 128 bytes a cycle: a stage of 256 columns of K
+// writes 35 KB and its MMAs read 32, 547 cycles where the MMAs alone take 512 (533
+// measured without loads, 594 with them). An MMA over more of K at a time would
+// change neither. 10,240 x 22,016 x 4,096 runs at 6.9 PFLOP/s for a moment and at
+// 6.4 under the power cap.
 #include <algorithm>
 #include <atomic>
 
@@ -30,11 +32,11 @@
 
 namespace svl {
 
-constexpr int kPrK = 256;   // values of K per stage: a 128-byte swizzled row of codes
-constexpr int kPrRows = 256;  // rows of A per tile
+constexpr int kPrK = 256;           // values of K per stage: a 128-byte swizzled row of codes
+constexpr int kPrRows = 256;        // rows of A per tile
 constexpr int kPrChunk = 32 * 128;  // bytes of an epilogue chunk: 32 rows of 128 bytes
 constexpr int kPrOutWarps = 8;      // two for each quarter of the lanes, with every other chunk of columns
-constexpr int kPrThreads = 64 + 32 * kPrOutWarps;  // warp 0 loads, warp 1 MMAs (leader), the others epilogue
+constexpr int kPrThreads = 96 + 32 * kPrOutWarps;  // warps 0 and 10 load A and B, warp 1 MMAs (leader), 2-9 epilogue
 constexpr int kPrGroup = 8;  // tiles of rows that are walked together
 // The epilogue warps' second buffers are the end of the stages (behind shares of K, 96 KB at most), so many bytes
 // in front of their first.
@@ -101,7 +103,8 @@ SVL_DEVINL PairTile pair_tile(const Mxf4PairParams& p, int t) {
   return ti;
 }
 
-template <int COLS>
+// One thread a CTA loads its rows of A (OP 0), one its half of B (OP 1), each with the scales.
+template <int COLS, int OP>
 SVL_DEVINL void mx_pair_producer(const Mxf4PairParams& p, const PairPlace& w, uint8_t* stages, uint64_t* full,
                                  uint64_t* empty, volatile int* abort) {
   using C = PairCfg<COLS>;
@@ -120,12 +123,16 @@ SVL_DEVINL void mx_pair_producer(const Mxf4PairParams& p, const PairPlace& w, ui
     for (int k = w.s0; k < w.s1; ++k, next()) {
       if (!mbar_wait(&empty[s], ph, abort)) return mx_abort(abort, p.g.status);
       uint8_t* st = stages + s * C::kStageBytes;
-      if (w.rank == 0) mbar_arrive_expect_tx(&full[s], 2 * C::kStageBytes);
       const uint32_t fb = mapa_shared(&full[s], w.leader);
-      tma_load_2d_pair(st, &p.a, fb, k * 128, m0);
-      tma_load_2d_pair(st + C::kCodesA, &p.b, fb, k * 128, n0);
-      tma_load_2d_pair(st + C::kCodesA + C::kCodesB, &p.a_scale, fb, k * 256, m0 >> 7);
-      tma_load_2d_pair(st + C::kCodesA + C::kCodesB + C::kScalesA, &p.b_scale, fb, k * 256, ti.n0 >> 7);
+      if constexpr (OP == 0) {
+        if (w.rank == 0) mbar_arrive_expect_tx(&full[s], 2 * (C::kCodesA + C::kScalesA));
+        tma_load_2d_pair(st, &p.a, fb, k * 128, m0);
+        tma_load_2d_pair(st + C::kCodesA + C::kCodesB, &p.a_scale, fb, k * 256, m0 >> 7);
+      } else {
+        if (w.rank == 0) mbar_arrive_expect_tx(&full[s], 2 * (C::kCodesB + C::kScalesB));
+        tma_load_2d_pair(st + C::kCodesA, &p.b, fb, k * 128, n0);
+        tma_load_2d_pair(st + C::kCodesA + C::kCodesB + C::kScalesA, &p.b_scale, fb, k * 256, ti.n0 >> 7);
+      }
     }
   }
   // the releases of the last stages (the leader's MMA commits) have arrived here
@@ -496,7 +503,7 @@ __global__ void __launch_bounds__(kPrThreads, 1) mxf4_pair_kernel(const __grid_c
   const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0);  // uniform over the warp
   if (threadIdx.x == 0) {
     for (int i = 0; i < C::kStages; ++i) {
-      mbar_init(&full[i], 1);
+      mbar_init(&full[i], 2);  // the leader's producers
       mbar_init(&empty[i], 1);
     }
     mbar_init(done, 1);
@@ -535,7 +542,9 @@ __global__ void __launch_bounds__(kPrThreads, 1) mxf4_pair_kernel(const __grid_c
 
   uint8_t* buffers = stages + C::kStages * C::kStageBytes + 1024;
   if (warp == 0) {
-    if (elect_one()) mx_pair_producer<COLS>(p, w, stages, full, empty, abort);
+    if (elect_one()) mx_pair_producer<COLS, 0>(p, w, stages, full, empty, abort);
+  } else if (warp == 10) {
+    if (elect_one()) mx_pair_producer<COLS, 1>(p, w, stages, full, empty, abort);
   } else if (warp == 1) {
     if (w.rank == 0 && elect_one()) mx_pair_mma<COLS>(p, w, stages, full, empty, done, taken, tmem, abort);
   } else if constexpr (SHARED) {
