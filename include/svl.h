@@ -345,7 +345,8 @@ size_t svl_mxf4_scale_size(int64_t rows, int32_t cols);
  * to nearest, ties to the even code. A block with a NaN or an infinity gets the
  * scale 255 and codes of zero. With inv_rms (device float32 [rows], or NULL) it
  * also writes 1 / sqrt(mean(src[r, :]^2) + eps): an RMSNorm's factor of the
- * whole row, which svl_gemm_mxf4 applies after the product (row_factor).
+ * whole row, which svl_gemm_mxf4 applies after the product (row_factor). Its sum
+ * is in float32, in an order that depends on rows and cols alone.
  * Nothing outside the rows is written, but for the zeros that fill up their last
  * block and their tiles of scales along the columns.
  * Requires cols and ld_src multiples of 8, ld_src >= cols, 16-byte aligned src
@@ -357,8 +358,8 @@ svl_status svl_quantize_rows_mxf4(const void* src, const void* gain, int64_t row
 
 /* The hidden rows of a gated MLP, quantised as they are made: the same of
  * x = gate / (1 + exp(-gate)) * up (float32, within 7 * 2^-23 of it; gates under
- * -87 may give 0). gate and up are bf16 rows, ld_gate and ld_up elements apart (they may be the two halves of
- * the rows of one product). */
+ * -87 may give 0). gate and up are bf16 rows, ld_gate and ld_up elements apart
+ * (they may be the two halves of the rows of one product). */
 svl_status svl_swiglu_rows_mxf4(const void* gate, int64_t ld_gate, const void* up, int64_t ld_up, int64_t rows,
                                 int32_t cols, void* dst, int64_t ld_dst, void* scale, void* stream);
 
@@ -375,9 +376,11 @@ svl_status svl_dequantize_rows_mxf4(const void* src, int64_t ld_src, const void*
  * float32 [M], or NULL for 1) and the sum with the residual (C's type, ld_residual
  * elements apart, or NULL for none) in float32, and one rounding to C's type
  * (SVL_OUT_F32 or SVL_OUT_BF16; ld_c elements apart). C may be the residual
- * itself, and overlaps no other argument. The result does not depend on what
- * else runs. Any M (0: nothing is done), N and K; ld_c and ld_residual at least N
- * (else SVL_ERR_INVALID_ARG). A device wait that ran out of time sets
+ * itself, and overlaps no other argument. The sum's order depends on M, N, K and
+ * the device alone, so a call's bits do not change from call to call. Any M (0:
+ * nothing is done), N and K; ld_c and ld_residual at least N, C and the residual
+ * aligned to their type (else SVL_ERR_INVALID_ARG; rows at multiples of 16 bytes
+ * are stored fastest). A device wait that ran out of time sets
  * SVL_DEV_TIMEOUT in *status (device uint32, or NULL). */
 #define SVL_OUT_F32 0
 #define SVL_OUT_BF16 1

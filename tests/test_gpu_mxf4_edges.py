@@ -1,5 +1,8 @@
 """MXFP4 calls that the documentation allows and nothing else makes: results at any address, offsets past 32 bits, several
 host threads, other streams, graphs beside each other."""
+import os
+import subprocess
+import sys
 import threading
 
 import numpy as np
@@ -168,6 +171,42 @@ def test_graphs_beside_each_other():
     torch.cuda.synchronize()
     for (_, out), want in zip(chains, wants):
         assert torch.equal(out, want)
+
+
+FIRST = """
+import torch
+from paper_2607_20357_gb300 import svl
+BF16, U8 = torch.bfloat16, torch.uint8
+m, n, k = %d, 512, %d
+x, w = torch.randn(m, k, device="cuda").to(BF16), torch.randn(n, k, device="cuda").to(BF16)
+held = [(torch.zeros(r, k // 2, dtype=U8, device="cuda"),
+         torch.zeros(svl.svl_mxf4_scale_size(r, k), dtype=U8, device="cuda")) for r in (m, n)]
+out = torch.zeros(m, n, device="cuda")
+
+def run():
+    for src, (c, s) in zip((x, w), held):
+        svl.svl_quantize_rows_mxf4(src, src.shape[0], k, k, c, k // 2, s)
+    (a, sa), (b, sb) = held
+    svl.svl_gemm_mxf4(a, k // 2, sa, b, k // 2, sb, m, n, k, out, n, svl.SVL_OUT_F32)
+
+torch.cuda.synchronize()
+graph = torch.cuda.CUDAGraph()
+with torch.cuda.graph(graph):
+    run()
+graph.replay()
+torch.cuda.synchronize()
+first = out.clone()
+out.zero_()
+run()
+assert torch.equal(out, first) and out.abs().max() > 0
+"""
+
+
+@pytest.mark.parametrize("m,k", [(3, 4096), (60, 12288), (300, 1024), (300, 16384)])
+def test_a_process_whose_first_call_is_captured(m, k):
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    r = subprocess.run([sys.executable, "-c", FIRST % (m, k)], cwd=root, capture_output=True, text=True, timeout=120)
+    assert r.returncode == 0, r.stderr
 
 
 def test_the_same_matrix_twice():

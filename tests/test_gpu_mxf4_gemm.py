@@ -47,7 +47,8 @@ def whole(m, n, factor, residual, kept):
 
 # (M, N, K, bytes between rows of A and of B (None: dense), ld_c)
 SHAPES = [
-    (1, 1, 32, None, None, None), (1, 8, 8, None, None, None), (3, 5, 40, 48, 64, 9), (1, 128, 64, None, None, None),
+    (1, 1, 32, None, None, None), (5, 9, 1, None, None, None), (130, 40, 7, None, None, None), (1, 8, 8, None, None, None),
+    (3, 5, 40, 48, 64, 9), (1, 128, 64, None, None, None),
     (2, 129, 96, None, 80, 130), (16, 128, 128, None, None, None), (17, 200, 160, None, None, 203),
     (1, 4096, 4096, None, None, None), (5, 300, 1000, 512, 528, None), (31, 1000, 256, None, None, None),
     (33, 127, 288, None, None, 128), (48, 260, 512, 272, None, None), (64, 4096, 2048, None, None, None),
