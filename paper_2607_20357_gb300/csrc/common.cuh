@@ -493,6 +493,12 @@ SVL_DEVINL void tc_commit_pair(uint64_t* bar, uint16_t ctas = 3) {
       : "memory");
 }
 
+// The same on `bar` of this CTA alone, for what only the leader waits for.
+SVL_DEVINL void tc_commit_pair_here(uint64_t* bar) {
+  asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_u32(bar))
+               : "memory");
+}
+
 // Shared-memory matrix descriptor for a K-major operand written by TMA with
 // 128-byte swizzle: rows of 64 bf16 (128 B), 8-row atoms 1024 B apart.
 // Bits: start address >> 4 [0,14), leading byte offset >> 4 [16,30) (unused

@@ -127,25 +127,26 @@ SVL_DEVINL void mx_stage(uint32_t tmem, uint64_t dw, uint64_t dx, uint64_t ds, u
 
 SVL_DEVINL void mx_mma(const Mxf4Params& p, const Mxf4Tile& t, uint8_t* stages, uint64_t* full, uint64_t* empty,
                        uint64_t* done, uint32_t tmem, volatile int* abort) {
-  // scales in tensor memory behind the accumulator
-  const uint32_t sw = tmem + p.nt, sx = sw + 8;
+  uint32_t sw = tmem + p.nt;  // two sets of scales, used in turn, in tensor memory behind the accumulator
   const uint32_t id0 = idesc_mxf4(kMxW, p.nt, 0), id1 = idesc_mxf4(kMxW, p.nt, 1);
   const uint32_t base = smem_u32(stages);
   const uint64_t dw0 = smem_desc_sw128(base), dx0 = smem_desc_sw128(base + kMxWBytes);
   const uint64_t ds0 = smem_desc_scales(base + kMxWBytes + p.nt * 128);
   const uint32_t step = static_cast<uint32_t>(p.stage_bytes) >> 4;
   int slot = 0;
-  uint32_t ph = 0, at = 0;
+  uint32_t ph = 0, at = 0, odd = 0;
   for (int s = t.s0; s < t.s1; ++s) {
     if (!mbar_wait(&full[slot], ph, abort)) return mx_abort(abort, p.g.status);
     tc_fence_after();
-    const uint32_t accumulate = s > t.s0;
+    const uint32_t accumulate = s > t.s0, sx = sw + 8;
     const int left = p.g.K - s * kMxK;
     if (left >= kMxK)
       mx_stage<true>(tmem, dw0 + at, dx0 + at, ds0 + at, sw, sx, id0, id1, accumulate, 4);
     else  // none behind K's last block
       mx_stage<false>(tmem, dw0 + at, dx0 + at, ds0 + at, sw, sx, id0, id1, accumulate, (left + 63) >> 6);
     tc_commit(&empty[slot]);
+    sw = odd ? sw - 16 : sw + 16;
+    odd ^= 1;
     at += step;
     if (++slot == p.stages) {
       slot = 0;
@@ -451,12 +452,15 @@ __global__ void __launch_bounds__(kMxGemmThreads, 2) mxf4_tile_kernel(const __gr
 }
 
 cudaError_t launch_mxf4_gemm(const Mxf4Gemm& g, cudaStream_t s) {
-  // (Over a short K the results take most of the time, which pairs have more threads for, if a round of them is
-  // enough: 100 x 5,120 x 256 3.9 us here, 3.4 on pairs.)
-  if (g.M > kMxMaxX || (g.M > 64 && g.K <= 4 * kMxK && (g.N - 1) / 128 < mxf4_clusters(2))) return launch_mxf4_pair(g, s);
+  // More than 64 rows over a short K, where results take most of the time, and more than 96 over one that is not long
+  // go to pairs, if a round of them is enough: us here and there 100 x 5,120 x 256 3.9, 3.4; 128 x 4,096 x 4,096 8.0, 7.7.
+  const int k_stages = (g.K - 1) / kMxK + 1;
+  if (g.M > kMxMaxX ||
+      (((g.M > 64 && k_stages <= 4) || (g.M > 96 && k_stages <= 20)) && (g.N - 1) / 128 < mxf4_clusters(2)))
+    return launch_mxf4_pair(g, s);
   Mxf4Params p;
   p.g = g;
-  const int nt = (g.M + 15) / 16 * 16, k_stages = (g.K - 1) / kMxK + 1;
+  const int nt = (g.M + 15) / 16 * 16;
   const int64_t tiles = (static_cast<int64_t>(g.N) + kMxW - 1) / kMxW;
   p.nt = nt;
   // A cluster shares K while all clusters run at once, an SM to a CTA (up to 16 columns: half an SM), and K has
@@ -487,7 +491,7 @@ cudaError_t launch_mxf4_gemm(const Mxf4Gemm& g, cudaStream_t s) {
   auto fours = [&](const void* q, int64_t ld) { return !((reinterpret_cast<uintptr_t>(q) | (ld * size)) % (4 * size)); };
   p.wide = g.N % 4 == 0 && fours(g.c, g.ld_c) && (!g.residual || fours(g.residual, g.ld_residual));
   p.tmem_cols = 32;
-  while (p.tmem_cols < static_cast<uint32_t>(nt + 16)) p.tmem_cols *= 2;
+  while (p.tmem_cols < static_cast<uint32_t>(nt + 32)) p.tmem_cols *= 2;
   const uint64_t bytes = static_cast<uint64_t>(mxf4_row_bytes(g.K));
   if (!make_byte_map(&p.w, g.b, g.N, bytes, g.ld_b, kMxW) ||
       !make_byte_map(&p.x, g.a, g.M, bytes, g.ld_a, static_cast<uint32_t>(nt)))

@@ -13,18 +13,19 @@
 // for products whose tiles of 256 would leave SMs without work, have two
 // accumulators side by side.
 //
-// Barriers: full[s] (leader's: both CTAs' loads of stage s have landed), empty[s]
-// (in both CTAs: the MMAs have read stage s), done (in both: a tile's MMAs are
-// complete), taken (leader's: both epilogues have read the overlap, so the
+// Barriers: full[s] (leader's: both CTAs' loads of stage s have landed), ready[i]
+// (leader's: a stage's scales are in set i), empty[s] (in both CTAs: the MMAs have
+// read stage s), done (in both: a tile's MMAs are complete), taken (leader's: both epilogues have read the overlap, so the
 // tile before is read altogether).
 //
 // Where tiles are few, clusters of two or four pairs share a tile's K.
 //
-// What bounds it is shared memory, 128 bytes a cycle: a stage of 256 columns of K
-// writes 35 KB and its MMAs read 32, 547 cycles where the MMAs alone take 512 (533
-// measured without loads, 594 with them). An MMA over more of K at a time would
-// change neither. 10,240 x 22,016 x 4,096 runs at 6.9 PFLOP/s for a moment and at
-// 6.4 under the power cap.
+// What bounds tiles of 256 is shared memory, 128 bytes a cycle: a stage of 256
+// columns of K writes 35 KB and its MMAs read 32, 547 cycles where the MMAs alone
+// take 512 (533 measured without loads, 580 with them). An MMA over more of K at a
+// time would change neither. Tiles of 128 take 450 cycles a stage: their issue
+// (some 50 cycles an MMA of a pair) and loads. 10,240 x 22,016 x 4,096 runs at
+// 6.9 PFLOP/s for a moment and at 6.4 under the power cap.
 #include <algorithm>
 #include <atomic>
 
@@ -36,7 +37,8 @@ constexpr int kPrK = 256;           // values of K per stage: a 128-byte swizzle
 constexpr int kPrRows = 256;        // rows of A per tile
 constexpr int kPrChunk = 32 * 128;  // bytes of an epilogue chunk: 32 rows of 128 bytes
 constexpr int kPrOutWarps = 8;      // two for each quarter of the lanes, with every other chunk of columns
-constexpr int kPrThreads = 96 + 32 * kPrOutWarps;  // warps 0 and 10 load A and B, warp 1 MMAs (leader), 2-9 epilogue
+// warps 0 and 10 load A and B, warp 11 copies scales and warp 1 MMAs (both the leader's), 2-9 epilogue
+constexpr int kPrThreads = 128 + 32 * kPrOutWarps;
 constexpr int kPrGroup = 8;  // tiles of rows that are walked together
 // The epilogue warps' second buffers are the end of the stages (behind shares of K, 96 KB at most), so many bytes
 // in front of their first.
@@ -52,9 +54,11 @@ struct PairCfg {
   static constexpr int kStageBytes = kCodesA + kCodesB + kScalesA + kScalesB;
   static constexpr int kStages = COLS == 256 ? 5 : 7;
   static constexpr int kSmem = 1024 + kStages * kStageBytes + 1024 + kPrOutWarps * kPrChunk;
-  // tensor memory: two sets of scales, used in turn, at the end; the second accumulator in front of them or of its own
+  // tensor memory: sets of scales, used in turn, at the end; the second accumulator in front of them or of its own
+  static constexpr bool kApart = COLS == 128;  // a thread of its own copies them there
+  static constexpr int kSets = kApart ? 4 : 2;
   static constexpr int kSet = 8 + COLS / 16;
-  static constexpr int kSecondAcc = COLS == 256 ? 512 - 2 * kSet - COLS : COLS;
+  static constexpr int kSecondAcc = COLS == 256 ? 512 - kSets * kSet - COLS : COLS;
   static constexpr int kOverlap = COLS - kSecondAcc;
   static_assert(kSmem <= 232448, "shared memory per CTA");
   static_assert(kStages * kStageBytes - kPrOutWarps * kPrChunk >= 96 * 1024, "second buffers");
@@ -145,52 +149,104 @@ SVL_DEVINL uint32_t pair_acc(uint32_t tmem, int it) {
   return tmem + ((it & 1) ? PairCfg<COLS>::kSecondAcc : 0);
 }
 
+// Copies a stage's scales (descriptor d) to a set in tensor memory: A's two tiles of
+// 128 columns of K (4 tensor memory columns each), then B's (4 per 128 rows).
+template <int COLS>
+SVL_DEVINL void pair_copy_scales(uint64_t d, uint32_t sa, bool two) {
+  const uint32_t sb = sa + 8;
+#pragma unroll
+  for (int j = 0; j < 2; ++j) {
+    if (j == 0 || two) {
+      tc_copy_scales_pair(sa + 4 * j, d + j * (kMxTileBytes >> 4));
+#pragma unroll
+      for (int c = 0; c < COLS / 128; ++c)
+        tc_copy_scales_pair(sb + (COLS / 32) * j + 4 * c,
+                            d + ((PairCfg<COLS>::kScalesA + (2 * c + j) * kMxTileBytes) >> 4));
+    }
+  }
+}
+
+// Tiles of 128 rows of B: a thread of its own copies the scales of each stage to the
+// next of kSets sets, when the MMAs that read that set before are complete
+// (their stage's release). The MMAs of a stage take half the time of a larger
+// tile's, less than one thread needs to issue both (300 x 3,584 x 18,944 23.3 ->
+// 19.9 us); with tiles of 256 the way over another thread costs more (26.0 -> 29.4).
+template <int COLS>
+SVL_DEVINL void mx_pair_scales(const Mxf4PairParams& p, const PairPlace& w, uint8_t* stages, uint64_t* full,
+                               uint64_t* empty, uint64_t* ready, uint32_t tmem, volatile int* abort) {
+  using C = PairCfg<COLS>;
+  const uint64_t d0 = smem_desc_scales(smem_u32(stages) + C::kCodesA + C::kCodesB);
+  int s = 0, set = 0, before = 0;  // stage, set, the stage that had the set before
+  uint32_t ph = 0, before_ph = 0;
+  int lead = C::kSets;             // sets that nothing has used yet
+  for (int t = w.first; t < p.tiles; t += w.stride) {
+    for (int k = w.s0; k < w.s1; ++k) {
+      if (lead > 0) {
+        --lead;
+      } else {
+        if (!mbar_wait(&empty[before], before_ph, abort)) return mx_abort(abort, p.g.status);
+        if (++before == C::kStages) {
+          before = 0;
+          before_ph ^= 1;
+        }
+      }
+      if (!mbar_wait(&full[s], ph, abort)) return mx_abort(abort, p.g.status);
+      tc_fence_after();
+      pair_copy_scales<COLS>(d0 + static_cast<uint32_t>(s * (C::kStageBytes >> 4)),
+                             tmem + 512 - C::kSets * C::kSet + set * C::kSet, p.g.K - k * kPrK > 128);
+      tc_commit_pair_here(&ready[set]);
+      if (++s == C::kStages) {
+        s = 0;
+        ph ^= 1;
+      }
+      if (++set == C::kSets) set = 0;
+    }
+  }
+}
+
+// One thread of the leader issues the MMAs: when a stage's loads have landed, with
+// its copies of scales in front, or when its scales are there (and so its codes,
+// which their copies waited for).
 template <int COLS>
 SVL_DEVINL void mx_pair_mma(const Mxf4PairParams& p, const PairPlace& w, uint8_t* stages, uint64_t* full,
-                            uint64_t* empty, uint64_t* done, uint64_t* taken, uint32_t tmem, volatile int* abort) {
+                            uint64_t* ready, uint64_t* empty, uint64_t* done, uint64_t* taken, uint32_t tmem,
+                            volatile int* abort) {
   using C = PairCfg<COLS>;
   const uint32_t base = smem_u32(stages);
+  const uint64_t da0 = smem_desc_sw128(base), db0 = smem_desc_sw128(base + C::kCodesA);
+  const uint64_t ds0 = smem_desc_scales(base + C::kCodesA + C::kCodesB);
   constexpr uint32_t id0 = idesc_mxf4(kPrRows, COLS, 0), id1 = idesc_mxf4(kPrRows, COLS, 1);
   const uint16_t ctas = static_cast<uint16_t>(3u << w.leader);
-  int s = 0, it = 0;
-  uint32_t ph = 0, set = 0;
+  int s = 0, it = 0, set = 0;
+  uint32_t ph = 0, set_ph = 0;
   for (int t = w.first; t < p.tiles; t += w.stride, ++it) {
     if (it > 0 && !mbar_wait(taken, (it - 1) & 1, abort)) return mx_abort(abort, p.g.status);
     tc_fence_after();
     const uint32_t d = pair_acc<COLS>(tmem, it);
-    uint32_t accumulate = 0;
     for (int k = w.s0; k < w.s1; ++k) {
-      if (!mbar_wait(&full[s], ph, abort)) return mx_abort(abort, p.g.status);
+      if (!(C::kApart ? mbar_wait(&ready[set], set_ph, abort) : mbar_wait(&full[s], ph, abort)))
+        return mx_abort(abort, p.g.status);
       tc_fence_after();
-      const uint32_t st = base + s * C::kStageBytes, sc = st + C::kCodesA + C::kCodesB;
-      // a set: A's two tiles of 128 columns of K (4 tensor memory columns each), then B's (4 per 128 rows)
-      const uint32_t sa = tmem + 512 - 2 * C::kSet + set * C::kSet, sb = sa + 8;
-      const int steps = min(4, (p.g.K - k * kPrK + 63) >> 6);  // 64 values of K an instruction
+      const uint32_t at = static_cast<uint32_t>(s * (C::kStageBytes >> 4));
+      const uint32_t sa = tmem + 512 - C::kSets * C::kSet + set * C::kSet, sb = sa + 8;
+      const uint64_t da = da0 + at, db = db0 + at;
+      const int left = p.g.K - k * kPrK;
+      if (!C::kApart) pair_copy_scales<COLS>(ds0 + at, sa, left > 128);
 #pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        if (2 * j < steps) {
-          tc_copy_scales_pair(sa + 4 * j, smem_desc_scales(sc + j * kMxTileBytes));
-#pragma unroll
-          for (int c = 0; c < COLS / 128; ++c)
-            tc_copy_scales_pair(sb + (COLS / 32) * j + 4 * c,
-                                smem_desc_scales(sc + C::kScalesA + (2 * c + j) * kMxTileBytes));
-        }
-      }
-      const uint64_t da = smem_desc_sw128(st), db = smem_desc_sw128(st + C::kCodesA);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        if (i < steps) {
+      for (int i = 0; i < 4; ++i) {  // 64 values of K an instruction
+        if (left > 64 * i)
           tc_mma_mxf4_pair(d, da + 2 * i, db + 2 * i, (i & 1) ? id1 : id0, sa + 4 * (i >> 1), sb + (COLS / 32) * (i >> 1),
-                           accumulate);
-          accumulate = 1;
-        }
+                           i > 0 || k > w.s0);
       }
       tc_commit_pair(&empty[s], ctas);
       if (++s == C::kStages) {
         s = 0;
         ph ^= 1;
       }
-      set ^= 1;
+      if (++set == C::kSets) {
+        set = 0;
+        set_ph ^= 1;
+      }
     }
     tc_commit_pair(done, ctas);
   }
@@ -495,7 +551,8 @@ __global__ void __launch_bounds__(kPrThreads, 1) mxf4_pair_kernel(const __grid_c
   uint64_t* taken = done + 1;
   uint64_t* free_bar = taken + 1;
   uint64_t* arrived = free_bar + 1;
-  uint64_t* loaded = arrived + 1;  // [epilogue warp][2]
+  uint64_t* ready = arrived + 1;   // [set of scales]
+  uint64_t* loaded = ready + 4;    // [epilogue warp][2]
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(loaded + 2 * kPrOutWarps);
   volatile int* abort = reinterpret_cast<volatile int*>(tmem_slot + 1);
   pdl_trigger();
@@ -506,6 +563,7 @@ __global__ void __launch_bounds__(kPrThreads, 1) mxf4_pair_kernel(const __grid_c
       mbar_init(&full[i], 2);  // the leader's producers
       mbar_init(&empty[i], 1);
     }
+    for (int i = 0; i < C::kSets; ++i) mbar_init(&ready[i], 1);
     mbar_init(done, 1);
     mbar_init(taken, 2 * kPrOutWarps);  // the epilogue warps of both CTAs
     for (int i = 0; i < 2 * kPrOutWarps; ++i) mbar_init(&loaded[i], 1);
@@ -546,7 +604,9 @@ __global__ void __launch_bounds__(kPrThreads, 1) mxf4_pair_kernel(const __grid_c
   } else if (warp == 10) {
     if (elect_one()) mx_pair_producer<COLS, 1>(p, w, stages, full, empty, abort);
   } else if (warp == 1) {
-    if (w.rank == 0 && elect_one()) mx_pair_mma<COLS>(p, w, stages, full, empty, done, taken, tmem, abort);
+    if (w.rank == 0 && elect_one()) mx_pair_mma<COLS>(p, w, stages, full, ready, empty, done, taken, tmem, abort);
+  } else if (warp == 11) {
+    if (C::kApart && w.rank == 0 && elect_one()) mx_pair_scales<COLS>(p, w, stages, full, empty, ready, tmem, abort);
   } else if constexpr (SHARED) {
     mx_pair_shares<F32, COLS>(p, w, done, free_bar, arrived, loaded, tmem, stages, buffers, abort);
   } else {
@@ -613,13 +673,16 @@ cudaError_t launch_mxf4_pair(const Mxf4Gemm& g, cudaStream_t s) {
   const int64_t m_tiles = (g.M - 1) / kPrRows + 1, wide = m_tiles * ((g.N - 1) / 256 + 1);
   const int64_t narrow = m_tiles * ((g.N - 1) / 128 + 1), pairs = std::max(1, mxf4_clusters(2));
   // Tiles of 128 rows of B where they take no more rounds of the device (4,096 rows of B, K 4,096, us for 256 and
-  // 128: 300 rows of A 9.3, 8.2; 800 rows 9.9, 12.9). Of 256, a cluster's pairs share K where all of the tiles'
-  // clusters run at once and K has the stages to make up for the sums' way, against tiles of 128 or, where those
-  // take longer, of 256. us for 128, and for 256 with 1, 2 and 4 pairs: 4,608 rows of B, K 11,008 (43 stages), 150 rows
-  // of A 15.3, 17.7, 14.0; 3,584 and 18,944 (74 stages), 150 rows 23.2, 26.4, 18.2, 14.8, 500 rows 23.5, 26.5, 19.0.
+  // 128: 300 rows of A 9.2, 7.7; 800 rows 9.9, 12.4). Of 256, a cluster's pairs share K where all of the tiles'
+  // clusters run at once and K has the stages to make up for the sums' way. us for 128, and for 256 with 2 and 4 pairs:
+  // 2,048 rows of B, K 4,096 (16 stages) 7.4, 8.8, 8.5; 4,608 and 11,008 (43 stages) 13.4, 14.0; 1,000 and 11,008 13.2,
+  // 12.9, 10.4; 3,584 and 18,944 (74 stages), 150 rows of A 20.0, 17.8, 14.2, 500 rows 20.1, 18.4.
   int cols = (narrow - 1) / pairs <= (wide - 1) / pairs ? 128 : 256, log_split = 0;
-  if ((g.K - 1) / kPrK + 1 >= (cols == 128 ? 36 : 16))
-    for (int l = 1; l <= 2 && wide <= mxf4_clusters(2 << l); ++l) log_split = l;
+  const int k_stages = (g.K - 1) / kPrK + 1;
+  if (k_stages >= 24 && wide <= mxf4_clusters(8))
+    log_split = 2;
+  else if (k_stages >= 50 && wide <= mxf4_clusters(4))
+    log_split = 1;
   if (log_split) cols = 256;
   const int64_t tiles = cols == 256 ? wide : narrow;
   if (narrow > INT32_MAX / 2) return cudaErrorInvalidValue;

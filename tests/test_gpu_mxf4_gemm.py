@@ -61,7 +61,9 @@ SHAPES = [
     (40, 77, 18944, None, None, 80), (24, 300, 2000, None, None, None), (50, 640, 12288, None, None, 645),
     (100, 640, 6000, None, None, None), (128, 300, 18944, None, None, None), (70, 20000, 320, None, None, None),
     (16, 20000, 512, None, None, None), (130, 700, 4128, None, None, 703), (300, 3584, 4352, None, None, None),
-    (520, 1300, 8192, None, None, None), (1100, 129, 640, None, None, 136), (1100, 2052, 256, None, None, 2056),
+    (520, 1300, 8192, None, None, None), (129, 20000, 96, None, None, None), (200, 39000, 288, None, None, None),
+    (250, 25000, 416, None, None, 25001), (300, 20100, 1040, None, None, 20104), (330, 21000, 128, None, None, None),
+    (384, 700, 8192, None, None, None), (290, 1100, 12288, None, None, None), (160, 1000, 18944, None, None, 1001), (1100, 129, 640, None, None, 136), (1100, 2052, 256, None, None, 2056),
 ]
 
 
