@@ -1,6 +1,7 @@
 """Sizes and refusals of the MXFP4 entry points (no GPU needed): nothing is launched and no pointer below is followed."""
 import numpy as np
 import pytest
+import torch
 
 from paper_2607_20357_gb300 import svl
 from tests import mxf4_reference as R
@@ -133,3 +134,18 @@ def test_product(svl_lib):
     before = svl.svl_launch_count()
     svl.svl_gemm_mxf4(P, 32, P, P, 32, P, 0, 8, 64, P, 8, svl.SVL_OUT_F32, stream=0)
     assert svl.svl_launch_count() == before
+
+
+def test_arguments_of_other_types(svl_lib):
+    """Tensors and plain ints go as they are, addresses and other integers are converted, alone or beside them."""
+    x = torch.zeros(4096, dtype=torch.uint8)  # (a CPU tensor: nothing is launched for no rows)
+    at = x.data_ptr()
+    assert at % 16 == 0
+    for p in (x, at):
+        for i in (int, np.int32, np.int64):
+            svl.svl_dequantize_rows_mxf4(p, i(32), x, i(0), i(64), x, i(64), stream=0)
+            svl.svl_quantize_rows_mxf4(p, i(0), 64, i(64), at, 32, x, gain=p, inv_rms=x, eps=np.float32(1e-5), stream=0)
+            svl.svl_swiglu_rows_mxf4(x, i(64), p, 64, i(0), 64, x, 32, p, stream=0)
+            svl.svl_gemm_mxf4(p, 32, x, p, i(32), x, i(0), 8, i(64), x, 8, svl.SVL_OUT_BF16, row_factor=x, residual=p,
+                              ld_residual=i(8), status=x, stream=0)
+    assert code(svl.svl_gemm_mxf4, x, np.int64(24), x, x, 32, x, 4, 8, 64, x, 8, 0) == INVALID
