@@ -9,9 +9,9 @@
 // e2m1 value). e = E - 2 throughout would cut a block's largest values, those
 // between 6 and 8 * 2^e, down to 6; the mean square error of normal values is the
 // same (0.0134 of their square, 0.0132 with the cut), but it shrinks outliers by
-// up to a quarter, always in one direction. Scaling by a power of two is exact, so the code is the one
-// rounding. A block with a NaN or an infinity becomes the scale 255 (NaN) and
-// codes of zero.
+// up to a quarter, always in one direction. Scaling by a power of two is exact,
+// so the code is the one rounding. A block with a NaN or an infinity becomes the
+// scale 255 (NaN) and codes of zero.
 //
 // All of it is bound by memory (2 bytes in, 17/32 out per value; SwiGLU 4 in), if
 // a value costs no more than some ten issue slots: hence sixteen values a
@@ -19,8 +19,6 @@
 // 18,944 x 3,584: rows 27.2 us (6.3 TB/s), with a gain 28.6 and with 1/rms 31.5,
 // SwiGLU 48.2 (6.4 TB/s), reading back 32.7 (5.3 TB/s, four fifths of it writes).
 #include <algorithm>
-
-#include <cuda_fp16.h>
 
 #include "mxf4.cuh"
 
@@ -107,8 +105,8 @@ SVL_DEVINL void load_gains(const Mxf4Rows& a, int u, uint4* gain) {
 }
 
 // gate / (1 + exp(-gate)) * up of two values, within 7 * 2^-23 of it (gates
-// whose exponential passes 2^126 give 0). With log2(e) = H + L, H of 15 bits:
-// exp(-g) = 2^(-gH) * exp(-g L ln 2). A bf16 gate times H is exact, and the
+// whose exponential passes 2^126 give 0). With log2(e) = H + L, H of 15 bits (a
+// constant split as Cody and Waite do): exp(-g) = 2^(-gH) * exp(-g L ln 2). A bf16 gate times H is exact, and the
 // second factor is 1 - g L ln 2 within 2^-23 for every g that leaves exp(-g) to
 // count. Seven operations a value where expf and a division took 80 us for
 // 5,403 x 11,008 rows, twice what the memory takes.
@@ -231,7 +229,7 @@ __global__ void __launch_bounds__(kMxThreads, 4) mxf4_quantize_kernel(Mxf4Rows a
         for (int q = 0; q < AT_ONCE; ++q) sum[q] += __shfl_xor_sync(0xffffffffu, sum[q], off);
       }
       if (group > 32) {
-        // (alternate, so that one barrier a round is enough)
+        // (alternate, so that one barrier each time is enough)
         if ((threadIdx.x & 31) == 0) {
 #pragma unroll
           for (int q = 0; q < AT_ONCE; ++q) red[n & 1][q][threadIdx.x >> 5] = sum[q];
@@ -355,8 +353,8 @@ cudaError_t launch_mxf4_quantize(Mxf4Source source, const Mxf4Rows& a, cudaStrea
   // Two rows at a time where a row is a single step, so that each thread has more than one on its way, and where rows
   // share the loads of their gains. Not where the SMs (four CTAs each) would then pass over more rows in all: 60,000 x
   // 256 7.9 us instead of 10.1, 18,944 x 3,584 with gains 28.6 instead of 31.7, but 5,403 x 11,008 33.4 instead of 30.5.
-  const int64_t round = static_cast<int64_t>(kMxThreads / group) * 4 * a.num_sms;
-  const int64_t ones = (a.rows + round - 1) / round, twos = (a.rows + 2 * round - 1) / (2 * round);
+  const int64_t wave = static_cast<int64_t>(kMxThreads / group) * 4 * a.num_sms;
+  const int64_t ones = (a.rows + wave - 1) / wave, twos = (a.rows + 2 * wave - 1) / (2 * wave);
   const bool step = units <= group && ones > 2, fits = ones > 1 && 2 * twos <= ones;
   switch (source) {
     case MX_ROWS: return step ? launch_quantize<MX_ROWS, 2>(a, group, s) : launch_quantize<MX_ROWS, 1>(a, group, s);

@@ -83,8 +83,8 @@ cudaError_t launch_mxf4_pair(const Mxf4Gemm& g, cudaStream_t s);
 // How many clusters of 2, 4 or 8 CTAs the device runs at once, an SM to a CTA.
 int mxf4_clusters(int ctas);
 
-// Lets `kernel` have `bytes` of shared memory, the same in every call. Asked of the
-// driver once per device (0.3 us of a call's 3.6); `devices`: the kernel's own.
+// Lets `kernel` have `bytes` of shared memory, the same in every call. Set once
+// per device (0.3 us of a call's 3.6); `devices`: the kernel's own.
 inline cudaError_t mxf4_allow_smem(const void* kernel, int bytes, std::atomic<uint64_t>* devices) {
   int dev = 0;
   cudaError_t e = cudaGetDevice(&dev);

@@ -453,7 +453,7 @@ __global__ void __launch_bounds__(kMxGemmThreads, 2) mxf4_tile_kernel(const __gr
 
 cudaError_t launch_mxf4_gemm(const Mxf4Gemm& g, cudaStream_t s) {
   // More than 64 rows over a short K, where results take most of the time, and more than 96 over one that is not long
-  // go to pairs, if a round of them is enough: us here and there 100 x 5,120 x 256 3.9, 3.4; 128 x 4,096 x 4,096 8.0, 7.7.
+  // go to pairs, if one wave of them is enough: us here and there 100 x 5,120 x 256 3.9, 3.4; 128 x 4,096 x 4,096 8.0, 7.7.
   const int k_stages = (g.K - 1) / kMxK + 1;
   if (g.M > kMxMaxX ||
       (((g.M > 64 && k_stages <= 4) || (g.M > 96 && k_stages <= 20)) && (g.N - 1) / 128 < mxf4_clusters(2)))

@@ -672,7 +672,7 @@ cudaError_t launch_mxf4_pair(const Mxf4Gemm& g, cudaStream_t s) {
   p.g = g;
   const int64_t m_tiles = (g.M - 1) / kPrRows + 1, wide = m_tiles * ((g.N - 1) / 256 + 1);
   const int64_t narrow = m_tiles * ((g.N - 1) / 128 + 1), pairs = std::max(1, mxf4_clusters(2));
-  // Tiles of 128 rows of B where they take no more rounds of the device (4,096 rows of B, K 4,096, us for 256 and
+  // Tiles of 128 rows of B where they take no more waves (4,096 rows of B, K 4,096, us for 256 and
   // 128: 300 rows of A 9.2, 7.7; 800 rows 9.9, 12.4). Of 256, a cluster's pairs share K where all of the tiles'
   // clusters run at once and K has the stages to make up for the sums' way. us for 128, and for 256 with 2 and 4 pairs:
   // 2,048 rows of B, K 4,096 (16 stages) 7.4, 8.8, 8.5; 4,608 and 11,008 (43 stages) 13.4, 14.0; 1,000 and 11,008 13.2,
