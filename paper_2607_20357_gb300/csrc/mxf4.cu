@@ -106,10 +106,10 @@ SVL_DEVINL void load_gains(const Mxf4Rows& a, int u, uint4* gain) {
 
 // gate / (1 + exp(-gate)) * up of two values, within 7 * 2^-23 of it (gates
 // whose exponential passes 2^126 give 0). With log2(e) = H + L, H of 15 bits (a
-// constant split as Cody and Waite do): exp(-g) = 2^(-gH) * exp(-g L ln 2). A bf16 gate times H is exact, and the
-// second factor is 1 - g L ln 2 within 2^-23 for every g that leaves exp(-g) to
-// count. Seven operations a value where expf and a division took 80 us for
-// 5,403 x 11,008 rows, twice what the memory takes.
+// constant split as Cody and Waite do): exp(-g) = 2^(-gH) * exp(-g L ln 2). A bf16
+// gate times H is exact, and the second factor is 1 - g L ln 2 within 2^-23 for
+// every g that leaves exp(-g) to count. Seven operations a value where expf and a
+// division took 80 us for 5,403 x 11,008 rows, twice what the memory takes.
 SVL_DEVINL uint64_t swiglu2(uint64_t gate, uint64_t up) {
   const uint64_t t = mul2(gate, both2(-1.44268798828125f));
   const uint64_t rest = fma2(gate, both2(-4.888495152143634e-6f), both2(1.f));
