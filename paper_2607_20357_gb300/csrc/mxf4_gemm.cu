@@ -14,7 +14,8 @@
 // the 8,300 cycles of 1 x 4,096 x 4,096).
 //
 // No CTA waits for another that has not started (a cluster's CTAs start together),
-// so CTAs of several calls that share an SM cannot wait in a circle.
+// and two on an SM find tensor memory for both (256 columns at most), so CTAs of
+// several calls that share an SM cannot wait in a circle.
 #include <algorithm>
 
 #include "mxf4.cuh"
@@ -29,7 +30,8 @@ constexpr int kMxMaxX = 128;    // most rows of A
 constexpr int kMxStoredX = 32;  // ... whose shares are stored one by one
 constexpr int kMxMaxStages = 12;
 constexpr int kMxSmem = 225 * 1024;
-constexpr int kMxBars = 1024;  // bytes of barriers behind the stages
+constexpr int kMxLeastSmem = 76 * 1024;  // three of them do not fit an SM, nor do their registers
+constexpr int kMxBars = 1024;            // bytes of barriers behind the stages
 // warp 0 loads B's codes, 7 its scales, 6 A, 1 MMAs; all of them see to the results
 constexpr int kMxGemmThreads = 256;
 
@@ -281,7 +283,6 @@ __global__ void __launch_bounds__(kMxGemmThreads, 2) mxf4_tile_kernel(const __gr
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(arrived + 1);
   volatile int* abort = reinterpret_cast<volatile int*>(tmem_slot + 1);
   const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
-  pdl_trigger();
   const Mxf4Tile t = mxf4_tile(p);
   const int split = 1 << p.log_split;
   const int mine = max(0, min(p.own, p.g.M - t.part * p.own));  // the columns of this CTA that exist
@@ -311,6 +312,9 @@ __global__ void __launch_bounds__(kMxGemmThreads, 2) mxf4_tile_kernel(const __gr
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = *tmem_slot;
+  // Not before: the next kernel's CTAs, which keep their tensor memory until this kernel is complete, could take what
+  // this CTA still has to get.
+  pdl_trigger();
 
   if (warp == 0) {
     if (elect_one()) mx_producer<MX_W>(p, t, stages, full, empty, abort);
@@ -496,7 +500,7 @@ cudaError_t launch_mxf4_gemm(const Mxf4Gemm& g, cudaStream_t s) {
   if (!make_byte_map(&p.w, g.b, g.N, bytes, g.ld_b, kMxW) ||
       !make_byte_map(&p.x, g.a, g.M, bytes, g.ld_a, static_cast<uint32_t>(nt)))
     return cudaErrorInvalidValue;
-  const int smem = p.bars_at + kMxBars + 1024;
+  const int smem = std::max(p.bars_at + kMxBars + 1024, kMxLeastSmem);
   void (*kernel)(Mxf4Params) = g.f32 ? mxf4_tile_kernel<true> : mxf4_tile_kernel<false>;
   static std::atomic<uint64_t> devices[2];
   cudaError_t e = mxf4_allow_smem(reinterpret_cast<const void*>(kernel), kMxSmem, &devices[g.f32]);

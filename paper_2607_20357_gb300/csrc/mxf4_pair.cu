@@ -555,7 +555,6 @@ __global__ void __launch_bounds__(kPrThreads, 1) mxf4_pair_kernel(const __grid_c
   uint64_t* loaded = ready + 4;    // [epilogue warp][2]
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(loaded + 2 * kPrOutWarps);
   volatile int* abort = reinterpret_cast<volatile int*>(tmem_slot + 1);
-  pdl_trigger();
   const PairPlace w = pair_place(p);
   const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0);  // uniform over the warp
   if (threadIdx.x == 0) {
@@ -595,6 +594,7 @@ __global__ void __launch_bounds__(kPrThreads, 1) mxf4_pair_kernel(const __grid_c
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
+  pdl_trigger();  // (the next kernel's CTAs take no tensor memory that this one still has to get)
   cluster_wait();  // the cluster's barriers exist before any load or arrive reaches them
   const uint32_t tmem = *tmem_slot;
 

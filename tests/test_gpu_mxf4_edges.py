@@ -228,3 +228,32 @@ def test_rows_beside_each_other():
         code, byte = R.quantised(x[i].double().numpy())
         np.testing.assert_array_equal(both[:, i].cpu().numpy(), R.packed(code))
         np.testing.assert_array_equal(scales[i].cpu().numpy(), R.laid_out(byte, 96, 0xEE))
+
+
+@pytest.mark.parametrize("m,k", [(1, 512), (12, 4096), (60, 2560), (128, 256)])
+def test_kernels_that_take_all_tensor_memory_behind_a_product(m, k):
+    """Products of few rows leave room on their SMs, where CTAs of the next kernel may start before they have ended."""
+    from tests.test_gpu_fp8 import TINY, Case, synth
+    case = Case(synth.reduced(TINY.dims, n_layers=1), TINY, seed=5, max_seq=256)
+    n = 19456  # a tile for every SM
+    a, sa, va = operand(1, m, k, None, 125, 128)
+    b, sb, vb = operand(2, n, k, None, 126, 129)
+    out, other = torch.empty(m, n, device="cuda"), torch.empty(300, 4096, device="cuda")
+    codes = torch.full((4096, 128), 0x38, dtype=U8, device="cuda")  # ones
+    ones = torch.ones(4096, device="cuda")
+
+    def run():
+        for _ in range(20):
+            svl.svl_gemm_mxf4(a, k // 2, sa, b, k // 2, sb, m, n, k, out, n, svl.SVL_OUT_F32)
+            svl.svl_gemm_e4m3(case.model.handle, codes, ones, codes, ones, 300, 4096, 128, other)
+    run()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        run()
+    out.zero_()
+    other.zero_()
+    graph.replay()
+    torch.cuda.synchronize()
+    assert torch.equal(out, (torch.from_numpy(va).cuda() @ torch.from_numpy(vb).cuda().t()).float())
+    assert (other == 128).all()
