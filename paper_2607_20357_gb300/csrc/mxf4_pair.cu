@@ -100,7 +100,7 @@ struct PairTile {
 template <int COLS>
 SVL_DEVINL PairTile pair_tile(const Mxf4PairParams& p, int t) {
   const int per = kPrGroup * p.n_tiles, g = t / per, r = t - g * per;
-  const int height = min(kPrGroup, p.m_tiles - g * kPrGroup);
+  const int height = max(1, min(kPrGroup, p.m_tiles - g * kPrGroup));  // (1: behind the last tile)
   PairTile ti;
   ti.m0 = (g * kPrGroup + r % height) * kPrRows;
   ti.n0 = r / height * COLS;
