@@ -346,13 +346,13 @@ size_t svl_mxf4_scale_size(int64_t rows, int32_t cols);
  * scale 255 and codes of zero. With inv_rms (device float32 [rows], or NULL) it
  * also writes 1 / sqrt(mean(src[r, :]^2) + eps): an RMSNorm's factor of the
  * whole row, which svl_gemm_mxf4 applies after the product (row_factor). Its sum
- * is in float32, in an order that depends on rows and cols alone.
+ * is in float32, in an order that depends on rows, cols and the device alone.
  * Nothing outside the rows is written, but for the zeros that fill up their last
  * block and their tiles of scales along the columns.
  * Requires cols and ld_src multiples of 8, ld_src >= cols, 16-byte aligned src
  * (and gain), ld_dst >= ceil(cols / 32) * 16, eps finite and not negative (else
- * SVL_ERR_INVALID_ARG). rows may be 0. Asynchronous on `stream`, as all calls
- * here. */
+ * SVL_ERR_INVALID_ARG). rows may be 0, what has no rows then NULL. Asynchronous
+ * on `stream`, as all calls here. */
 svl_status svl_quantize_rows_mxf4(const void* src, const void* gain, int64_t rows, int32_t cols, int64_t ld_src,
                                   void* dst, int64_t ld_dst, void* scale, float eps, float* inv_rms, void* stream);
 
@@ -378,10 +378,11 @@ svl_status svl_dequantize_rows_mxf4(const void* src, int64_t ld_src, const void*
  * (SVL_OUT_F32 or SVL_OUT_BF16; ld_c elements apart). C may be the residual
  * itself, and overlaps no other argument. The sum's order depends on M, N, K and
  * the device alone, so a call's bits do not change from call to call. Any M (0:
- * nothing is done), N and K; ld_c and ld_residual at least N, C and the residual
- * aligned to their type (else SVL_ERR_INVALID_ARG; rows at multiples of 16 bytes
- * are stored fastest). A device wait that ran out of time sets
- * SVL_DEV_TIMEOUT in *status (device uint32, or NULL). */
+ * nothing is done, and what has no rows may be NULL), N and K; ld_c and
+ * ld_residual at least N, C and the residual aligned to their type (else
+ * SVL_ERR_INVALID_ARG; rows at multiples of 16 bytes are stored fastest). A
+ * device wait that ran out of time sets SVL_DEV_TIMEOUT in *status (device
+ * uint32, or NULL). */
 #define SVL_OUT_F32 0
 #define SVL_OUT_BF16 1
 svl_status svl_gemm_mxf4(const void* A, int64_t ld_a, const void* a_scale, const void* B, int64_t ld_b,

@@ -1904,14 +1904,18 @@ svl_status svl_gemm_e4m3(svl_model* m, const void* A, const float* a_scale, cons
 namespace {
 constexpr int kMxMaxCols = 1 << 30;  // (column counts rounded up to a tile stay in 32 bits)
 
-bool mxf4_held(const void* codes, int64_t ld, const void* scale, int64_t cols) {
-  return codes && scale && aligned16(codes) && aligned16(scale) && ld >= mxf4_row_bytes(cols) && !(ld & 15);
+// (An empty tensor's address is null.)
+bool mxf4_held(const void* codes, int64_t ld, const void* scale, int64_t rows, int64_t cols) {
+  return ((codes && scale) || rows == 0) && aligned16(codes) && aligned16(scale) && ld >= mxf4_row_bytes(cols) &&
+         !(ld & 15);
 }
-bool rows_of_8(const void* p, int64_t ld, int32_t cols) { return p && aligned16(p) && ld >= cols && !(ld & 7); }
+bool rows_of_8(const void* p, int64_t ld, int64_t rows, int32_t cols) {
+  return (p || rows == 0) && aligned16(p) && ld >= cols && !(ld & 7);
+}
 
 // What quantising, SwiGLU and reading back check alike.
 svl_status mxf4_rows(int64_t rows, int32_t cols, const void* codes, int64_t ld_codes, const void* scale, int* sms) {
-  if (rows < 0 || cols <= 0 || (cols & 7) || !mxf4_held(codes, ld_codes, scale, cols)) return SVL_ERR_INVALID_ARG;
+  if (rows < 0 || cols <= 0 || (cols & 7) || !mxf4_held(codes, ld_codes, scale, rows, cols)) return SVL_ERR_INVALID_ARG;
   if (cols > kMxMaxCols || rows > INT64_MAX / 4 / cols) return SVL_ERR_UNSUPPORTED;
   if (rows > 0 && !(*sms = device_sms())) return SVL_ERR_CUDA;
   return SVL_OK;
@@ -1927,7 +1931,7 @@ svl_status svl_quantize_rows_mxf4(const void* src, const void* gain, int64_t row
                                   void* dst, int64_t ld_dst, void* scale, float eps, float* inv_rms, void* stream) {
   Mxf4Rows a;
   std::memset(&a, 0, sizeof(a));
-  if (!rows_of_8(src, ld_src, cols) || (gain && !aligned16(gain)) || (reinterpret_cast<uintptr_t>(inv_rms) & 3) ||
+  if (!rows_of_8(src, ld_src, rows, cols) || (gain && !aligned16(gain)) || (reinterpret_cast<uintptr_t>(inv_rms) & 3) ||
       (inv_rms && !(eps >= 0.f && std::isfinite(eps))))
     return SVL_ERR_INVALID_ARG;
   const svl_status st = mxf4_rows(rows, cols, dst, ld_dst, scale, &a.num_sms);
@@ -1952,7 +1956,7 @@ svl_status svl_swiglu_rows_mxf4(const void* gate, int64_t ld_gate, const void* u
                                 int32_t cols, void* dst, int64_t ld_dst, void* scale, void* stream) {
   Mxf4Rows a;
   std::memset(&a, 0, sizeof(a));
-  if (!rows_of_8(gate, ld_gate, cols) || !rows_of_8(up, ld_up, cols)) return SVL_ERR_INVALID_ARG;
+  if (!rows_of_8(gate, ld_gate, rows, cols) || !rows_of_8(up, ld_up, rows, cols)) return SVL_ERR_INVALID_ARG;
   const svl_status st = mxf4_rows(rows, cols, dst, ld_dst, scale, &a.num_sms);
   if (st != SVL_OK || rows == 0) return st;
   a.src = static_cast<const __nv_bfloat16*>(gate);
@@ -1973,7 +1977,7 @@ svl_status svl_dequantize_rows_mxf4(const void* src, int64_t ld_src, const void*
                                     void* dst, int64_t ld_dst, void* stream) {
   Mxf4Read a;
   std::memset(&a, 0, sizeof(a));
-  if (!rows_of_8(dst, ld_dst, cols)) return SVL_ERR_INVALID_ARG;
+  if (!rows_of_8(dst, ld_dst, rows, cols)) return SVL_ERR_INVALID_ARG;
   const svl_status st = mxf4_rows(rows, cols, src, ld_src, scale, &a.num_sms);
   if (st != SVL_OK || rows == 0) return st;
   a.codes = static_cast<const uint8_t*>(src);
@@ -1992,8 +1996,8 @@ svl_status svl_gemm_mxf4(const void* A, int64_t ld_a, const void* a_scale, const
                          const void* b_scale, int32_t M, int32_t N, int32_t K, const float* row_factor,
                          const void* residual, int64_t ld_residual, void* C, int64_t ld_c, int32_t type,
                          uint32_t* status, void* stream) {
-  if (M < 0 || N <= 0 || K <= 0 || !mxf4_held(A, ld_a, a_scale, K) || !mxf4_held(B, ld_b, b_scale, K) || !C ||
-      ld_c < N || (residual && ld_residual < N) || (type != SVL_OUT_F32 && type != SVL_OUT_BF16) ||
+  if (M < 0 || N <= 0 || K <= 0 || !mxf4_held(A, ld_a, a_scale, M, K) || !mxf4_held(B, ld_b, b_scale, N, K) ||
+      (!C && M > 0) || ld_c < N || (residual && ld_residual < N) || (type != SVL_OUT_F32 && type != SVL_OUT_BF16) ||
       (reinterpret_cast<uintptr_t>(row_factor) & 3) || (reinterpret_cast<uintptr_t>(status) & 3))
     return SVL_ERR_INVALID_ARG;
   const uintptr_t size = type == SVL_OUT_F32 ? 4 : 2;

@@ -149,3 +149,18 @@ def test_arguments_of_other_types(svl_lib):
             svl.svl_gemm_mxf4(p, 32, x, p, i(32), x, i(0), 8, i(64), x, 8, svl.SVL_OUT_BF16, row_factor=x, residual=p,
                               ld_residual=i(8), status=x, stream=0)
     assert code(svl.svl_gemm_mxf4, x, np.int64(24), x, x, 32, x, 4, 8, 64, x, 8, 0) == INVALID
+
+
+def test_empty_tensors(svl_lib):
+    """No rows: the tensors that hold them are empty, their addresses null."""
+    none, b = torch.empty(0, 32, dtype=torch.uint8), torch.zeros(4096, dtype=torch.uint8)
+    assert none.data_ptr() == 0 and svl.svl_mxf4_scale_size(0, 64) == 0
+    before = svl.svl_launch_count()
+    svl.svl_quantize_rows_mxf4(none, 0, 64, 64, none, 32, none, stream=0, gain=b, inv_rms=none)
+    svl.svl_swiglu_rows_mxf4(none, 128, none, 128, 0, 64, none, 32, none, stream=0)
+    svl.svl_dequantize_rows_mxf4(none, 32, none, 0, 64, none, 64, stream=0)
+    svl.svl_gemm_mxf4(none, 32, none, b, 32, b, 0, 8, 64, none, 8, svl.SVL_OUT_BF16, stream=0, row_factor=none)
+    assert svl.svl_launch_count() == before
+    assert code(svl.svl_gemm_mxf4, none, 32, none, none, 32, b, 0, 8, 64, none, 8, 0) == INVALID  # no weight
+    assert code(svl.svl_quantize_rows_mxf4, none, 0, 64, 64, none, 16, none) == INVALID
+    assert code(svl.svl_dequantize_rows_mxf4, none, 32, none, 1, 64, none, 64) == INVALID
