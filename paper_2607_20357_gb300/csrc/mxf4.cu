@@ -168,7 +168,8 @@ SVL_DEVINL void store_half(const Mxf4Rows& a, int64_t row, int u, int n_units, i
   if (b == 255) code = make_uint2(0, 0);
   if (row >= a.rows) return;
   if (u < n_held) *reinterpret_cast<uint2*>(codes + static_cast<int64_t>(u) * 8) = code;
-  if ((u & 1) == 0 && u < n_units) scale[static_cast<int64_t>(u >> 3) * kMxTileBytes + ((u >> 1) & 3)] = static_cast<uint8_t>(b);
+  if ((u & 1) == 0 && u < n_units)
+    scale[static_cast<int64_t>(u >> 3) * kMxTileBytes + ((u >> 1) & 3)] = static_cast<uint8_t>(b);
 }
 
 // A group of `group` threads (a power of two, 8 to kMxThreads) takes a row, or

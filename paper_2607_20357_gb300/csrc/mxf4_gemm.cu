@@ -190,7 +190,8 @@ SVL_DEVINL void mx_results(const Mxf4Params& p, const float* shares, int stride,
     const int64_t row_c = kWarps * p.g.ld_c * kSize, row_r = kWarps * p.g.ld_residual * kSize;
     const int64_t m = m0 + warp;
     char* to = static_cast<char*>(p.g.c) + (m * p.g.ld_c + n0 + 4 * lane) * kSize;
-    const char* from = resid ? static_cast<const char*>(p.g.residual) + (m * p.g.ld_residual + n0 + 4 * lane) * kSize : nullptr;
+    const char* from =
+        resid ? static_cast<const char*>(p.g.residual) + (m * p.g.ld_residual + n0 + 4 * lane) * kSize : nullptr;
     const float* factors = p.g.row_factor ? p.g.row_factor + m : nullptr;
     const float4* sums = reinterpret_cast<const float4*>(shares + warp * kMxW) + lane;
     for (int r = warp; r < rows; r += kBatch * kWarps) {
@@ -457,7 +458,8 @@ __global__ void __launch_bounds__(kMxGemmThreads, 2) mxf4_tile_kernel(const __gr
 
 cudaError_t launch_mxf4_gemm(const Mxf4Gemm& g, cudaStream_t s) {
   // More than 64 rows over a short K, where results take most of the time, and more than 96 over one that is not long
-  // go to pairs, if one wave of them is enough: us here and there 100 x 5,120 x 256 3.9, 3.4; 128 x 4,096 x 4,096 8.0, 7.7.
+  // go to pairs, if one wave of them is enough: us here and there 100 x 5,120 x 256 3.9, 3.4; 128 x 4,096 x 4,096 8.0,
+  // 7.7.
   const int k_stages = (g.K - 1) / kMxK + 1;
   if (g.M > kMxMaxX ||
       (((g.M > 64 && k_stages <= 4) || (g.M > 96 && k_stages <= 20)) && (g.N - 1) / 128 < mxf4_clusters(2)))

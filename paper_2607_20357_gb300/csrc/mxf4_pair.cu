@@ -15,8 +15,8 @@
 //
 // Barriers: full[s] (leader's: both CTAs' loads of stage s have landed), ready[i]
 // (leader's: a stage's scales are in set i), empty[s] (in both CTAs: the MMAs have
-// read stage s), done (in both: a tile's MMAs are complete), taken (leader's: both epilogues have read the overlap, so the
-// tile before is read altogether).
+// read stage s), done (in both: a tile's MMAs are complete), taken (leader's: both
+// epilogues have read the overlap, so the tile before is read altogether).
 //
 // Where tiles are few, clusters of two or four pairs share a tile's K.
 //
@@ -697,7 +697,8 @@ cudaError_t launch_mxf4_pair(const Mxf4Gemm& g, cudaStream_t s) {
       !make_scale_map(&p.b_scale, g.b_scale, g.N, g.K, static_cast<uint32_t>(cols / 128)))
     return cudaErrorInvalidValue;
   // Tensor stores want 16-byte rows, and end a row at a multiple of 16 bytes; anything else goes by plain ones.
-  p.tma = (static_cast<int64_t>(g.N) * (g.f32 ? 4 : 2)) % 16 == 0 && make_result_map(&p.c, g.c, g.f32, g.M, g.N, g.ld_c) &&
+  p.tma = (static_cast<int64_t>(g.N) * (g.f32 ? 4 : 2)) % 16 == 0 &&
+          make_result_map(&p.c, g.c, g.f32, g.M, g.N, g.ld_c) &&
           (!g.residual || make_result_map(&p.residual, g.residual, g.f32, g.M, g.N, g.ld_residual));
   PairKernel kernel = pair_kernel(log_split > 0, g.f32, cols);
   const int smem = cols == 256 ? PairCfg<256>::kSmem : PairCfg<128>::kSmem, ctas = 2 << log_split;
