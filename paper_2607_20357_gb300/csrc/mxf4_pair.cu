@@ -30,6 +30,7 @@
 #include <atomic>
 
 #include "mxf4.cuh"
+#include "result_slots.cuh"
 
 namespace svl {
 
@@ -293,7 +294,7 @@ struct PairChunks {
 // A warp's results on their way out: its buffer in shared memory, and the next
 // chunk of the residual, requested when the buffer is free. In the CTA's last tile
 // the stages are used up, and a second buffer in their place takes every other
-// chunk (a store holds its buffer for some 900 cycles).
+// chunk, the first one too (a store holds its buffer for some 900 cycles).
 template <bool F32, int COLS>
 struct PairOut {
   static constexpr int kCols = F32 ? 32 : 64;
@@ -303,8 +304,7 @@ struct PairOut {
   PairChunks<F32, COLS> ahead;
   volatile int* abort;
   uint32_t parity = 0;  // of each buffer's next wait
-  bool last = false;    // in the last tile
-  int slot = 0;
+  ResultSlots slots;
   SVL_DEVINL PairOut(const Mxf4PairParams& params, const PairChunks<F32, COLS>& chunks, uint8_t* first, uint64_t* bars,
                      volatile int* flag)
       : p(params), own(first), loaded(bars), ahead(chunks), abort(flag) {
@@ -320,7 +320,7 @@ struct PairOut {
   }
   // The last tile's MMAs are complete.
   SVL_DEVINL void enter_last() {
-    last = true;
+    slots.enter_last(p.g.residual != nullptr);
     if (p.g.residual && p.tma && (threadIdx.x & 31) == 0) request(1);
   }
   // The chunk from column n0 and row row0 on: the factor and the sum with the
@@ -329,6 +329,7 @@ struct PairOut {
     const int lane = threadIdx.x & 31;
     const bool resid = p.g.residual != nullptr;
     if (p.tma) {
+      const int slot = slots.slot;
       uint8_t* const at = buffer(slot);
       if (resid) {
         const bool got = mbar_wait(&loaded[slot], (parity >> slot) & 1, abort);
@@ -337,7 +338,7 @@ struct PairOut {
         if (!__all_sync(0xffffffffu, got)) return false;
       } else {
         if (lane == 0) {  // the store before (in the last tile, the one before that) has read the buffer
-          if (last)
+          if (slots.unread())
             bulk_wait_read1();
           else
             bulk_wait_read0();
@@ -381,7 +382,7 @@ struct PairOut {
           request(slot);
         }
       }
-      if (last) slot ^= 1;
+      slots.stored();
       return true;
     }
     // rows of any alignment: turned in shared memory, a row of the chunk by a warp's consecutive lanes
