@@ -403,8 +403,9 @@ SVL_DEVINL void mbar_arrive_cluster(uint32_t cluster_addr) {
   asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
 }
 
-// The same without release: for an arrival that orders tensor memory reads (complete
-// after tcgen05.wait::ld) before another thread's MMAs, and no memory accesses. Waiting
+// The same without release: for an arrival behind tensor memory reads (complete after
+// tcgen05.wait::ld, and fenced) or MMAs' reads of shared memory (complete where their
+// commit has arrived), and no accesses of the thread's own. Waiting
 // for the warp's earlier stores costs some 1,200 cycles behind a tile's results.
 SVL_DEVINL void mbar_arrive_cluster_relaxed(uint32_t cluster_addr) {
   asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");

@@ -432,6 +432,14 @@ struct PairWarp {
   SVL_DEVINL uint32_t lanes() const { return static_cast<uint32_t>(q * 32) << 16; }
 };
 
+// A warp has read what the next MMAs write over: its reads of tensor memory are
+// complete, and the fence keeps them in front of the arrival, which orders nothing else.
+SVL_DEVINL void hand_over(uint32_t taken, int lane) {
+  tc_fence_before();
+  __syncwarp();
+  if (lane == 0) mbar_arrive_cluster_relaxed(taken);
+}
+
 template <bool F32, int COLS>
 SVL_DEVINL void mx_pair_epilogue(const Mxf4PairParams& p, const PairPlace& w, uint64_t* done, uint64_t* taken,
                                  uint64_t* loaded, uint32_t tmem, uint8_t* buffers, volatile int* abort) {
@@ -456,16 +464,14 @@ SVL_DEVINL void mx_pair_epilogue(const Mxf4PairParams& p, const PairPlace& w, ui
     const int in_overlap = min(
         ch.n, (ch.it & 1) ? (C::kOverlap + kCols - 1) / kCols : ch.n - (COLS - C::kOverlap) / kCols);
     bool handed = ch.i >= in_overlap;
-    if (handed && me.lane == 0) mbar_arrive_cluster_relaxed(release);
+    if (handed) hand_over(release, me.lane);  // (for its reads of the tile before)
     for (; ch.i < ch.n; ch.i += 2) {
       float v[kCols];
       const int col = ch.column();
 #pragma unroll
       for (int c = 0; c < kCols; c += 32) tmem_ld32(acc + col + c, v + c);
       if (!handed && ch.i + 2 >= in_overlap) {
-        tc_fence_before();
-        __syncwarp();
-        if (me.lane == 0) mbar_arrive_cluster_relaxed(release);
+        hand_over(release, me.lane);
         handed = true;
       }
       if (!out.chunk(v, factor, ch.n0 + col, ch.row0)) return mx_abort(abort, p.g.status);
