@@ -457,14 +457,16 @@ SVL_DEVINL void mx_pair_epilogue(const Mxf4PairParams& p, const PairPlace& w, ui
     __syncwarp();
     if (!__all_sync(0xffffffffu, ok)) return mx_abort(abort, p.g.status);
     tc_fence_after();
-    if (ch.t + w.stride >= p.tiles) out.enter_last();
+    const bool last = ch.t + w.stride >= p.tiles;
+    if (last) out.enter_last();
     const uint32_t acc = pair_acc<COLS>(tmem, ch.it) + me.lanes();
     // Chunks that hold the overlap come first; a warp hands over when it has read the last of its own. (Where the
-    // tile's columns end before the overlap, there is none.)
+    // tile's columns end before the overlap, there is none.) Behind the last tile nothing waits for an arrival, and the
+    // leader, to whose shared memory it goes, might have ended.
     const int in_overlap = min(
         ch.n, (ch.it & 1) ? (C::kOverlap + kCols - 1) / kCols : ch.n - (COLS - C::kOverlap) / kCols);
-    bool handed = ch.i >= in_overlap;
-    if (handed) hand_over(release, me.lane);  // (for its reads of the tile before)
+    bool handed = last || ch.i >= in_overlap;
+    if (handed && !last) hand_over(release, me.lane);  // (for its reads of the tile before)
     for (; ch.i < ch.n; ch.i += 2) {
       float v[kCols];
       const int col = ch.column();
