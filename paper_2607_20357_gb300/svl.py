@@ -199,14 +199,10 @@ def _p(x):
     return x.data_ptr() if isinstance(x, torch.Tensor) else int(x)
 
 
-_cuda_ready = False  # CUDA is initialised (it stays so; asking torch each time costs 0.1 us)
-
-
 def _stream(stream):
-    global _cuda_ready
     if stream is None:
-        if _cuda_ready or torch.cuda.is_initialized():
-            _cuda_ready = True
+        # (asked each time: a forked child has no CUDA, whatever its parent had, and gets torch's error below)
+        if torch.cuda.is_initialized():
             # the current stream's handle without a Stream object (2 us less per call)
             return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
         stream = torch.cuda.current_stream()
