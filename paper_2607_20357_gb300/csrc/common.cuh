@@ -185,8 +185,6 @@ SVL_DEVINL void bulk_commit() { asm volatile("cp.async.bulk.commit_group;" ::: "
 SVL_DEVINL void bulk_wait_read0() { asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory"); }
 // ... of every committed store but the most recent one
 SVL_DEVINL void bulk_wait_read1() { asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory"); }
-// ... but the two most recent ones
-SVL_DEVINL void bulk_wait_read2() { asm volatile("cp.async.bulk.wait_group.read 2;" ::: "memory"); }
 // every committed store is complete
 SVL_DEVINL void bulk_wait0() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
 

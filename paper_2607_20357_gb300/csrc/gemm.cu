@@ -340,19 +340,6 @@ SVL_DEVINL void store_bf16(__nv_bfloat16* dst, const float* v, int n /*16 or 32*
   }
 }
 
-SVL_DEVINL void load_bf16(const __nv_bfloat16* src, float* v, int n) {
-  const uint4* s = reinterpret_cast<const uint4*>(src);
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    if (i * 8 < n) {
-      uint4 u = s[i];
-      float2 a = unpack_bf16x2(u.x), b = unpack_bf16x2(u.y), c = unpack_bf16x2(u.z), d = unpack_bf16x2(u.w);
-      v[8 * i + 0] = a.x; v[8 * i + 1] = a.y; v[8 * i + 2] = b.x; v[8 * i + 3] = b.y;
-      v[8 * i + 4] = c.x; v[8 * i + 5] = c.y; v[8 * i + 6] = d.x; v[8 * i + 7] = d.y;
-    }
-  }
-}
-
 // 1 / rms of this row of the residual stream, from its partial sums of squares
 SVL_DEVINL float row_rms_scale(const GemmParams& p, int row) {
   float s = 0.f;
