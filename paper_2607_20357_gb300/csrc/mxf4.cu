@@ -16,8 +16,8 @@
 // All of it is bound by memory (2 bytes in, 17/32 out per value; SwiGLU 4 in), if
 // a value costs no more than some ten issue slots: hence sixteen values a
 // thread, whose block and row are found once, and operations on pairs.
-// 18,944 x 3,584: rows 27.2 us (6.3 TB/s), with a gain 28.6 and with 1/rms 31.5,
-// SwiGLU 48.2 (6.4 TB/s), reading back 32.7 (5.3 TB/s, four fifths of it writes).
+// 18,944 x 3,584: rows 27.9 us (6.2 TB/s), with a gain 28.6, with 1/rms 30.5, with
+// both 31.4, SwiGLU 48.2 (6.4 TB/s), reading back 32.3 (5.3 TB/s, four fifths of it writes).
 #include <algorithm>
 
 #include "mxf4.cuh"
@@ -325,11 +325,13 @@ __global__ void __launch_bounds__(kMxThreads) mxf4_dequantize_kernel(Mxf4Read a,
   }
 }
 
-// Threads per row: a warp, less for narrow rows (no lanes without values), more
+// Threads per row: a warp, less for narrow rows (fewer lanes without values), more
 // while the rows' groups have not `threads` in all, twice what the SMs hold when
-// quantising, four times when reading back (5,403 x 11,008 quantised in 25.5 us, 29.9
-// with half as many, 25.2 and with 1/rms 46 instead of 36 with four times as many;
-// read back in 28.9, 31.4 with half, 29.5 with twice as many).
+// quantising, four times when reading back. us with half as many threads, as many, and
+// two and four times as many: 5,403 x 11,008 quantised 30.7, 26.3, 27.5, 26.0, with
+// 1/rms 31.9, 28.4, 31.6, 31.7, with a gain too 45.3, 32.1, 34.6, 36.5, read back 31.0,
+// 28.8, 29.4, 29.5; 18,944 x 3,584 with 1/rms 30.5, 30.5, 35.4, 41.1; 2,000 x 18,944 with
+// 1/rms 19.2, 20.2, 20.3, 20.2.
 static int group_for(int64_t rows, int64_t units, int threads) {
   int group = 8;
   while (group < 32 && group < units) group *= 2;
@@ -353,7 +355,8 @@ cudaError_t launch_mxf4_quantize(Mxf4Source source, const Mxf4Rows& a, cudaStrea
   const int group = group_for(a.rows, units, 2048 * a.num_sms);
   // Two rows at a time where a row is a single step, so that each thread has more than one on its way, and where rows
   // share the loads of their gains. Not where the SMs (four CTAs each) would then pass over more rows in all: 60,000 x
-  // 256 7.9 us instead of 10.1, 18,944 x 3,584 with gains 28.6 instead of 31.7, but 5,403 x 11,008 33.4 instead of 30.5.
+  // 256 7.9 us instead of 9.9, 18,944 x 3,584 with gains 28.6 instead of 31.7, but 5,403 x 11,008 33.3 instead of 30.4.
+  // (Rows without gains are left at one: 18,944 x 3,584 27.6 and 27.9, but 5,403 x 11,008 31.9 and 26.3.)
   const int64_t wave = static_cast<int64_t>(kMxThreads / group) * 4 * a.num_sms;
   const int64_t ones = (a.rows + wave - 1) / wave, twos = (a.rows + 2 * wave - 1) / (2 * wave);
   const bool step = units <= group && ones > 2, fits = ones > 1 && 2 * twos <= ones;
@@ -371,7 +374,7 @@ cudaError_t launch_mxf4_quantize(Mxf4Source source, const Mxf4Rows& a, cudaStrea
 
 cudaError_t launch_mxf4_dequantize(const Mxf4Read& a, cudaStream_t s) {
   const int group = group_for(a.rows, a.cols / 8, 4096 * a.num_sms);
-  // four steps of a row, or four rows of one step (60,000 x 256 8.1 us instead of 10.1)
+  // four steps of a row, or four rows of one step (60,000 x 256 8.0 us instead of 10.1)
   if (a.cols / 8 <= group && a.rows > static_cast<int64_t>(kMxThreads / group) * 8 * a.num_sms)
     return launch_pdl(mxf4_dequantize_kernel<1, 4>, grid_for((a.rows + 3) / 4, group, a.num_sms), kMxThreads, 0, s, a,
                       group);

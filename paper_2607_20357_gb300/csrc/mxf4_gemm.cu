@@ -470,9 +470,11 @@ cudaError_t launch_mxf4_gemm(const Mxf4Gemm& g, cudaStream_t s) {
   const int64_t tiles = (static_cast<int64_t>(g.N) + kMxW - 1) / kMxW;
   p.nt = nt;
   // A cluster shares K while all clusters run at once, an SM to a CTA (up to 16 columns: half an SM), and K has
-  // the stages to make up for the sums' way. us for 1, 2, 4, 8 CTAs at 4,096 rows of B, K 4,096 (16 stages): 6.6,
-  // 5.2, 4.9, 4.6 for 1 row of A; 7.1, 6.6, 6.7, 7.1 for 40; 8.0, 8.5, 8.6 for 100. 3,584 and 18,944 (74 stages):
-  // 19.2, 11.5, 8.7, 8.4; 19.8, 12.9, 10.1, 10.8; 21.3, 15.4, 12.4.
+  // the stages to make up for the sums' way. us for at most 1, 2, 4 CTAs at 4,096 rows of B, K 4,096 (16 stages): 6.3,
+  // 5.0, 4.7 for 1 row of A; 6.6, 6.0, 5.3 for 32; 6.8, 6.5, 6.8 for 48; 7.0, 6.9, 7.7 for 64; 7.4, 8.0, 8.2 for 96;
+  // 8.0, 9.2, 9.6 for 128. K 2,048: 4.6, 4.0, 3.8; 4.9, 5.2, 4.5; 5.2, 5.9, 6.0; 5.4, 6.6, 6.9; 5.8, 7.2, 9.0; 6.2,
+  // 8.3, 8.8. 3,584 and 18,944 (74 stages): 18.4, 11.1, 8.5; 18.6, 12.0, 9.1; 18.9, 12.5, 10.1; 19.0, 13.0, 10.4; 19.7,
+  // 14.3, 11.7; 20.7, 15.7, 13.5. Where the rule is off: 96 by 2,048, K 8,192, 10.7, 9.0 (taken), 8.1.
   const int per_cta = nt <= kMxStoredX ? 2 : nt <= 64 ? 10 : 21;
   int split = 1;
   while (split < 8 && k_stages >= per_cta * split && tiles <= (nt <= 16 ? 2 : 1) * mxf4_clusters(2 * split)) split *= 2;

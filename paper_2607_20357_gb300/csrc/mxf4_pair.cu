@@ -20,12 +20,13 @@
 //
 // Where tiles are few, clusters of two or four pairs share a tile's K.
 //
-// What bounds tiles of 256 is shared memory, 128 bytes a cycle: a stage of 256
-// columns of K writes 35 KB and its MMAs read 32, 547 cycles where the MMAs alone
-// take 512 (533 measured without loads, 580 with them). An MMA over more of K at a
-// time would change neither. Tiles of 128 take 450 cycles a stage: their issue
-// (some 50 cycles an MMA of a pair) and loads. 10,240 x 22,016 x 4,096 runs at
-// 6.9 PFLOP/s for a moment and at 6.4 under the power cap.
+// What bounds tiles of 256: a stage of 256 columns of K takes 594 cycles. Its MMAs
+// alone take 512 (65,536 operations a cycle and pair; 533 measured without loads), its
+// loads almost as long (35 KB an SM; 478 measured with one MMA of four and no copies of
+// scales), and the two do not overlap altogether. The MMA's form with 96 columns of K,
+// which has a higher rate, was not measured. Tiles of 128 take 450 cycles a stage: their
+// issue (some 50 cycles an MMA of a pair) and loads. 10,240 x 22,016 x 4,096 runs at 6.4
+// PFLOP/s call after call, under the power cap, and at 6.9 for a moment.
 #include <algorithm>
 #include <atomic>
 
